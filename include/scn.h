@@ -382,6 +382,154 @@ scn_status scn_maxpool_bwd(const scn_rulebook* rb, const uint8_t* argmax, const 
                            size_t ws_bytes, hipStream_t stream);
 
 /*
+ * Attention among the active sites.  A sample's rows are a sequence of tokens:
+ * they lie together, in key order, and a site's lattice coordinates are its
+ * position.  The calls below take features in fp32 or bf16 and hold every sum,
+ * statistic and gradient accumulation in fp32 (fp32 operands are multiplied
+ * split into three bf16 values, as in scn_conv_fwd; results that come out
+ * infinite or NaN are formed again term by term in fp32 over visible sites
+ * only, so what a masked site holds never shows).  All of them are
+ * deterministic, launch on `stream` and neither wait nor allocate.
+ */
+#define SCN_F32 0
+#define SCN_BF16 1
+
+/* Rows of heads: channel c of head h of row t at ((T*)p)[t*row + h*head + c].
+ * p is a device pointer, 16-byte aligned; row and head are strides in elements,
+ * multiples of 16 bytes.  The parts of a matrix that holds queries, keys and
+ * values side by side are such views. */
+typedef struct scn_heads {
+  void* p;
+  int64_t row, head;
+} scn_heads;
+
+/* The same per stream: ((T*)p)[s*stream + t*row + h*head + c]. */
+typedef struct scn_cache {
+  void* p;
+  int64_t stream, row, head;
+} scn_cache;
+
+/*
+ * Row ranges of the samples: ranges[b] = rows of samples below b, b in
+ * [0, batch], so sample b's rows are [ranges[b], ranges[b+1]).
+ *  coords  device int32[n][width], column 0 the sample, ascending (the rows
+ *          of scn_rulebook_out_coords).
+ *  ranges  device int32[batch + 1] (written).
+ * Errors: SCN_ERR_INVALID (null, n < 0, width or batch < 1), SCN_ERR_OVERFLOW
+ * (n above 2^30), SCN_ERR_HIP.
+ */
+scn_status scn_site_ranges(const int32_t* coords, int64_t n, int32_t width, int32_t batch,
+                           int32_t* ranges, hipStream_t stream);
+
+/*
+ * Norm of queries and keys for each head, and their rotation by the site's
+ * coordinates, in one pass.  For a row t and each head x[0..D) of q (weights
+ * wq) and k (wk):
+ *   u_c = w_c x_c / sqrt(mean_c x_c^2 + eps)
+ *   y_2j   = u_2j cos a_j - u_2j+1 sin a_j
+ *   y_2j+1 = u_2j sin a_j + u_2j+1 cos a_j,   a_j = coords[t][1 + axis(j)] freq[j]
+ * The pairs j are dealt to the axes in order: the first sections[0] pairs turn
+ * with coordinate 1 of the site, the next sections[1] with coordinate 2, ..;
+ * pairs past the last section are not rotated.  Angles are reduced in 64 bits.
+ *  type      SCN_F32 or SCN_BF16, of q, k and the results.
+ *  n, D, Hq, Hk   rows, channels of a head (a multiple of 8, at most 128),
+ *            heads of q and of k (Hk may be 0: k, wk and kr are then not read).
+ *  wq, wk    device float[D], or NULL for ones.
+ *  coords    device int32[n][width], column 0 (the sample) unused.
+ *  freq      device float[D/2], radians per lattice step.
+ *  sections  host int32[width - 1], each >= 0, of sum <= D/2.
+ *  qr, kr    written; may be q and k themselves.
+ * Errors: SCN_ERR_INVALID, SCN_ERR_UNSUPPORTED (D), SCN_ERR_OVERFLOW (n above
+ * 2^30), SCN_ERR_HIP.
+ */
+scn_status scn_norm_rotate_fwd(int32_t type, int64_t n, int32_t D, int32_t Hq, int32_t Hk,
+                               const scn_heads* q, const scn_heads* k, const float* wq,
+                               const float* wk, float eps, const int32_t* coords, int32_t width,
+                               const float* freq, const int32_t* sections, const scn_heads* qr,
+                               const scn_heads* kr, hipStream_t stream);
+
+/* Bytes of device workspace scn_norm_rotate_bwd needs. */
+size_t scn_norm_rotate_bwd_workspace_bytes(int64_t n, int32_t D, int32_t Hq, int32_t Hk);
+
+/*
+ * Gradients of scn_norm_rotate_fwd for given dqr, dkr: dq, dk (of the type) and
+ * dwq, dwk (device float[D], sums over rows and heads; NULL: not computed).
+ * dq may be dqr, and dk dkr.  Errors: as the forward, and SCN_ERR_WORKSPACE.
+ */
+scn_status scn_norm_rotate_bwd(int32_t type, int64_t n, int32_t D, int32_t Hq, int32_t Hk,
+                               const scn_heads* q, const scn_heads* k, const float* wq,
+                               const float* wk, float eps, const int32_t* coords, int32_t width,
+                               const float* freq, const int32_t* sections, const scn_heads* dqr,
+                               const scn_heads* dkr, const scn_heads* dq, const scn_heads* dk,
+                               float* dwq, float* dwk, void* ws, size_t ws_bytes,
+                               hipStream_t stream);
+
+/*
+ * Attention within each sample.  With i, j the places of two rows in their
+ * sample, query head h and its key head h / (Hq/Hk):
+ *   i sees j  iff  j <= i + right  and  (j >= i - left  or  j < sinks)
+ *   s_ij = scale <q_i, k_j>,  lse_i = log sum_{j seen} exp s_ij
+ *   o_i  = sum_{j seen} exp(s_ij - lse_i) v_j
+ * left and right: negative for no bound.  right = 0 is causal; the first
+ * `sinks` rows of a sample stay visible to all that follow them.
+ *  n, ranges  rows, and device int32[batch + 1] as scn_site_ranges gives
+ *             (ascending; rows outside every range are not written).
+ *  D, Hq, Hk  channels of a head (a multiple of 8, at most 128), query heads,
+ *             key and value heads (Hq a multiple of Hk).
+ *  o          of the type (written);  lse  device float[Hq][n] (written), or NULL.
+ * Errors: SCN_ERR_INVALID (also a scale that is not positive and finite),
+ * SCN_ERR_UNSUPPORTED (D), SCN_ERR_OVERFLOW (n above 2^30), SCN_ERR_HIP.
+ */
+scn_status scn_attn_fwd(int32_t type, int64_t n, int32_t batch, const int32_t* ranges, int32_t D,
+                        int32_t Hq, int32_t Hk, const scn_heads* q, const scn_heads* k,
+                        const scn_heads* v, float scale, int64_t left, int64_t right,
+                        int64_t sinks, const scn_heads* o, float* lse, hipStream_t stream);
+
+/* Bytes of device workspace scn_attn_bwd needs. */
+size_t scn_attn_bwd_workspace_bytes(int64_t n, int32_t batch, int32_t D, int32_t Hq, int32_t Hk,
+                                    int64_t left, int64_t sinks);
+
+/*
+ * Gradients of scn_attn_fwd (o and lse are its results) for a given do:
+ *   p_ij = exp(s_ij - lse_i),  ds_ij = p_ij (<do_i, v_j> - <do_i, o_i>)
+ *   dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_i ds_ij q_i,
+ *   dv_j = sum_i p_ij do_i
+ * over the pairs seen; dk and dv sum over their head's query heads too.
+ * Errors: as scn_attn_fwd, and SCN_ERR_WORKSPACE.
+ */
+scn_status scn_attn_bwd(int32_t type, int64_t n, int32_t batch, const int32_t* ranges, int32_t D,
+                        int32_t Hq, int32_t Hk, const scn_heads* q, const scn_heads* k,
+                        const scn_heads* v, const scn_heads* o, const float* lse,
+                        const scn_heads* d_o, float scale, int64_t left, int64_t right,
+                        int64_t sinks, const scn_heads* dq, const scn_heads* dk,
+                        const scn_heads* dv, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* Bytes of device workspace scn_attn_step needs. */
+size_t scn_attn_step_workspace_bytes(int32_t streams, int64_t capacity, int32_t D, int32_t Hq,
+                                     int32_t Hk, int64_t left, int64_t sinks);
+
+/*
+ * Attention of one new token of each stream, over the stream's last tokens and
+ * its first `sinks`.  A stream's cache holds `capacity` rows: position p lies in
+ * row p < sinks ? p : sinks + (p - sinks) mod (capacity - sinks), so the sinks
+ * stay and the rest is a ring.  Stream s has written length[s] tokens; the new
+ * one takes position p = length[s]: its k and v rows are written to the caches,
+ * and its query sees the positions j <= p with j < sinks or j >= p - reach,
+ * reach = min(left, capacity - sinks - 1) (negative left: no bound of its own).
+ * Cache rows that hold no such position are not read.  The caller advances
+ * length (a negative one counts as 0).
+ *  q, k, v   row s is stream s's new token;  o  written.
+ *  capacity  > sinks.
+ * Errors: as scn_attn_fwd, and SCN_ERR_WORKSPACE; SCN_ERR_OVERFLOW for more than
+ * 65535 streams or a capacity above 2^30.
+ */
+scn_status scn_attn_step(int32_t type, int32_t streams, int64_t capacity, int32_t D, int32_t Hq,
+                         int32_t Hk, const scn_heads* q, const scn_heads* k, const scn_heads* v,
+                         const scn_cache* k_cache, const scn_cache* v_cache,
+                         const int32_t* length, float scale, int64_t left, int64_t sinks,
+                         const scn_heads* o, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/*
  * Device memory the library allocates for itself: rulebook storage and the
  * temporaries of scn_rulebook_build* and scn_conv_fwd (workspaces of the
  * backward passes are the caller's).  By default it comes from the library's

@@ -10,6 +10,9 @@ from ._lib import (  # noqa: F401
     SCN_RELU,
     Rulebook,
     ScnError,
+    attn_bwd,
+    attn_fwd,
+    attn_step,
     build_chain,
     build_rulebook,
     build_rulebook_nd,
@@ -20,7 +23,11 @@ from ._lib import (  # noqa: F401
     maxpool_bwd,
     maxpool_fwd,
     next_rulebook,
+    norm_rotate_bwd,
+    norm_rotate_fwd,
+    rotation_freqs,
     set_allocator,
     set_dense_forward,
+    site_ranges,
     version,
 )

@@ -36,7 +36,10 @@ EXPORTED = (
     "scn_maxpool_bwd_workspace_bytes", "scn_maxpool_bwd", "scn_set_allocator",
     "scn_set_dense_forward", "scn_last_error", "scn_version", "scn_conv_fwd_noalloc",
     "scn_conv_fwd_noalloc_max_bytes", "scn_set_kernel_timer", "scn_ceiling_copy",
-    "scn_ceiling_mfma_f32", "scn_ceiling_mfma_bf16",
+    "scn_ceiling_mfma_f32", "scn_ceiling_mfma_bf16", "scn_site_ranges", "scn_norm_rotate_fwd",
+    "scn_norm_rotate_bwd_workspace_bytes", "scn_norm_rotate_bwd", "scn_attn_fwd",
+    "scn_attn_bwd_workspace_bytes", "scn_attn_bwd", "scn_attn_step_workspace_bytes",
+    "scn_attn_step",
 )
 
 _ALLOC_FN = ctypes.CFUNCTYPE(ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p, ctypes.c_void_p)
@@ -61,6 +64,15 @@ class _Info(ctypes.Structure):
                 ("out_grid_nd", ctypes.c_int64 * 5)]
 
 
+class _Heads(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("row", ctypes.c_int64), ("head", ctypes.c_int64)]
+
+
+class _Cache(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("stream", ctypes.c_int64), ("row", ctypes.c_int64),
+                ("head", ctypes.c_int64)]
+
+
 _lib = None
 
 
@@ -76,7 +88,7 @@ def lib() -> ctypes.CDLL:
     L = ctypes.CDLL(LIB_PATH)
     P, i32, i64, u32, sz = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_uint32,
                             ctypes.c_size_t)
-    st = ctypes.c_int
+    st, f32 = ctypes.c_int, ctypes.c_float
     sig = {
         "scn_rulebook_build": (st, [P, i64, P, i32, i32, P, ctypes.POINTER(P)]),
         "scn_rulebook_build_lattice": (st, [P, i64, P, i32, i32, i32, P, ctypes.POINTER(P)]),
@@ -102,6 +114,20 @@ def lib() -> ctypes.CDLL:
         "scn_maxpool_fwd": (st, [P, P, P, i32, P, P, P, P]),
         "scn_maxpool_bwd_workspace_bytes": (sz, [P, i32]),
         "scn_maxpool_bwd": (st, [P, P, P, P, i32, P, P, P, sz, P]),
+        "scn_site_ranges": (st, [P, i64, i32, i32, P, P]),
+        "scn_norm_rotate_fwd": (st, [i32, i64, i32, i32, i32, P, P, P, P, f32, P, i32, P, P, P, P,
+                                     P]),
+        "scn_norm_rotate_bwd_workspace_bytes": (sz, [i64, i32, i32, i32]),
+        "scn_norm_rotate_bwd": (st, [i32, i64, i32, i32, i32, P, P, P, P, f32, P, i32, P, P, P, P,
+                                     P, P, P, P, P, sz, P]),
+        "scn_attn_fwd": (st, [i32, i64, i32, P, i32, i32, i32, P, P, P, f32, i64, i64, i64, P, P,
+                              P]),
+        "scn_attn_bwd_workspace_bytes": (sz, [i64, i32, i32, i32, i32, i64, i64]),
+        "scn_attn_bwd": (st, [i32, i64, i32, P, i32, i32, i32, P, P, P, P, P, P, f32, i64, i64,
+                              i64, P, P, P, P, sz, P]),
+        "scn_attn_step_workspace_bytes": (sz, [i32, i64, i32, i32, i32, i64, i64]),
+        "scn_attn_step": (st, [i32, i32, i64, i32, i32, i32, P, P, P, P, P, P, f32, i64, i64, P,
+                               P, sz, P]),
         "scn_set_allocator": (None, [_ALLOC_FN, _FREE_FN, P]),
         "scn_set_dense_forward": (st, [i64, i32]),
         "scn_last_error": (ctypes.c_char_p, []),
@@ -357,6 +383,246 @@ def maxpool_bwd(rb: Rulebook, argmax: torch.Tensor, dy: torch.Tensor,
                                  _ptr(dg_in), _ptr(ws), ws.numel(), ctypes.c_void_p(_stream())),
            "scn_maxpool_bwd")
     return dx, dg_in
+
+
+# ---------------------------------------------------------------------------
+# attention among the active sites
+# ---------------------------------------------------------------------------
+
+SCN_TYPE = {torch.float32: 0, torch.bfloat16: 1}
+
+
+def _head_rows(t: torch.Tensor, like: Optional[torch.Tensor], shape, name: str) -> torch.Tensor:
+    """A [rows, heads, D] tensor (any strides with contiguous channels) of the
+    type and device of `like`."""
+    if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
+        raise TypeError(f"{name} must be a CUDA (HIP) tensor")
+    if t.dtype not in SCN_TYPE:
+        raise TypeError(f"{name} must be float32 or bfloat16, got {t.dtype}")
+    if like is not None and (t.dtype != like.dtype or t.device != like.device):
+        raise TypeError(f"{name} must be {like.dtype} on {like.device}, got {t.dtype} on {t.device}")
+    if t.dim() != len(shape) or any(s is not None and s != n for s, n in zip(shape, t.shape)):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.numel() and t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name} must have contiguous channels")
+    return t
+
+
+def _heads(t: Optional[torch.Tensor]):
+    """ctypes view of a [rows, heads, D] tensor.  A stride that no element is
+    reached by (one row, one head) is passed as 0, whatever torch holds there."""
+    if t is None:
+        return None
+    row = t.stride(0) if t.shape[0] > 1 else 0
+    head = t.stride(1) if t.shape[1] > 1 else 0
+    return ctypes.byref(_Heads(t.data_ptr(), row, head))
+
+
+def _cache(t: torch.Tensor):
+    st = [t.stride(i) if t.shape[i] > 1 else 0 for i in range(3)]
+    return ctypes.byref(_Cache(t.data_ptr(), *st))
+
+
+def _out_rows(t: Optional[torch.Tensor], like: torch.Tensor, shape, name: str) -> torch.Tensor:
+    if t is None:
+        return torch.empty(shape, dtype=like.dtype, device=like.device)
+    return _head_rows(t, like, shape, name)
+
+
+def _bytes(n: int, device) -> torch.Tensor:
+    return torch.empty(max(int(n), 1), dtype=torch.uint8, device=device)
+
+
+def site_ranges(coords: torch.Tensor, batch: int) -> torch.Tensor:
+    """Row ranges of the samples of key-ordered sites (``scn_site_ranges``):
+    int32 [batch + 1] with sample b's rows at [ranges[b], ranges[b + 1]).
+    ``coords`` is int32 [n, ndim + 1], the sample first (``Rulebook.out_coords``)."""
+    if not isinstance(coords, torch.Tensor) or coords.dim() != 2:
+        raise ValueError("coords must be a 2D tensor")
+    _dev_tensor(coords, torch.int32, tuple(coords.shape), "coords")
+    if batch < 1:
+        raise ValueError("batch must be at least 1")
+    r = torch.empty(batch + 1, dtype=torch.int32, device=coords.device)
+    _check(lib().scn_site_ranges(_ptr(coords), coords.shape[0], coords.shape[1], int(batch),
+                                 _ptr(r), ctypes.c_void_p(_stream())), "scn_site_ranges")
+    return r
+
+
+def rotation_freqs(dim: int, sections: Sequence[int], base: float = 100.0,
+                   device="cuda") -> torch.Tensor:
+    """Frequencies of the rotation for ``norm_rotate_fwd``: float32 [dim / 2],
+    the pairs of each axis from 1 radian per lattice step down in a geometric
+    series towards 1 / base; pairs past the sections 0."""
+    if any(m < 0 for m in sections) or sum(sections) > dim // 2:
+        raise ValueError(f"sections {tuple(sections)} must hold at most {dim // 2} pairs")
+    f = [float(base) ** (-j / m) for m in sections for j in range(m)]
+    return torch.tensor(f + [0.0] * (dim // 2 - len(f)), dtype=torch.float32, device=device)
+
+
+def _norm_args(q, k, wq, wk, coords, freq, sections):
+    _head_rows(q, None, (None, None, None), "q")
+    n, hq, d = (int(v) for v in q.shape)
+    hk = 0
+    if k is not None:
+        _head_rows(k, q, (n, None, d), "k")
+        hk = int(k.shape[1])
+    for w, name in ((wq, "wq"), (wk, "wk")):
+        if w is not None:
+            _dev_tensor(w, torch.float32, (d,), name)
+    _dev_tensor(coords, torch.int32, (n, len(sections) + 1), "coords")
+    _dev_tensor(freq, torch.float32, (d // 2,), "freq")
+    sec = (ctypes.c_int32 * max(1, len(sections)))(*[int(m) for m in sections])
+    return n, hq, hk, d, sec
+
+
+def norm_rotate_fwd(q: torch.Tensor, k: Optional[torch.Tensor], wq: Optional[torch.Tensor],
+                    wk: Optional[torch.Tensor], coords: torch.Tensor, freq: torch.Tensor,
+                    sections: Sequence[int], eps: float = 1e-6, out=(None, None)):
+    """Norm of each head's queries and keys and their rotation by the sites'
+    coordinates (``scn_norm_rotate_fwd``).  q [n, Hq, D], k [n, Hk, D] (or
+    None), float32 or bfloat16, any row and head strides; wq, wk float32 [D] or
+    None; coords int32 [n, 1 + axes]; freq float32 [D / 2]; sections the pairs
+    of each axis.  Returns (qr, kr), in ``out`` where given (q and k themselves
+    may be)."""
+    n, hq, hk, d, sec = _norm_args(q, k, wq, wk, coords, freq, sections)
+    qr = _out_rows(out[0], q, (n, hq, d), "out[0]")
+    kr = None if k is None else _out_rows(out[1], q, (n, hk, d), "out[1]")
+    _check(lib().scn_norm_rotate_fwd(
+        SCN_TYPE[q.dtype], n, d, hq, hk, _heads(q), _heads(k), _ptr(wq), _ptr(wk), float(eps),
+        _ptr(coords), len(sections) + 1, _ptr(freq), sec, _heads(qr), _heads(kr),
+        ctypes.c_void_p(_stream())), "scn_norm_rotate_fwd")
+    return qr, kr
+
+
+def norm_rotate_bwd(q: torch.Tensor, k: Optional[torch.Tensor], wq: Optional[torch.Tensor],
+                    wk: Optional[torch.Tensor], coords: torch.Tensor, freq: torch.Tensor,
+                    sections: Sequence[int], dqr: torch.Tensor, dkr: Optional[torch.Tensor],
+                    eps: float = 1e-6, need=("dwq", "dwk"), out=(None, None),
+                    ws: Optional[torch.Tensor] = None):
+    """Gradients of ``norm_rotate_fwd``: a dict with dq, dk (in ``out`` where
+    given; dqr and dkr themselves may be) and the requested ones of dwq, dwk."""
+    n, hq, hk, d, sec = _norm_args(q, k, wq, wk, coords, freq, sections)
+    _head_rows(dqr, q, (n, hq, d), "dqr")
+    res = {"dq": _out_rows(out[0], q, (n, hq, d), "out[0]")}
+    if k is not None:
+        _head_rows(dkr, q, (n, hk, d), "dkr")
+        res["dk"] = _out_rows(out[1], q, (n, hk, d), "out[1]")
+    else:
+        dkr = None
+    for name in ("dwq", "dwk"):
+        if name in need and (name == "dwq" or k is not None):
+            res[name] = torch.empty(d, dtype=torch.float32, device=q.device)
+    if ws is None:
+        ws = _bytes(lib().scn_norm_rotate_bwd_workspace_bytes(n, d, hq, hk), q.device)
+    _check(lib().scn_norm_rotate_bwd(
+        SCN_TYPE[q.dtype], n, d, hq, hk, _heads(q), _heads(k), _ptr(wq), _ptr(wk), float(eps),
+        _ptr(coords), len(sections) + 1, _ptr(freq), sec, _heads(dqr), _heads(dkr),
+        _heads(res["dq"]), _heads(res.get("dk")), _ptr(res.get("dwq")), _ptr(res.get("dwk")),
+        _ptr(ws), ws.numel(), ctypes.c_void_p(_stream())), "scn_norm_rotate_bwd")
+    return res
+
+
+def _bound(w: Optional[int], name: str) -> int:
+    if w is None:
+        return -1
+    if w < 0:
+        raise ValueError(f"{name} must be None (no bound) or at least 0, got {w}")
+    return int(w)
+
+
+def _attn_args(q, k, v, ranges, left, right, sinks, scale):
+    _head_rows(q, None, (None, None, None), "q")
+    n, hq, d = (int(x) for x in q.shape)
+    _head_rows(k, q, (n, None, d), "k")
+    hk = int(k.shape[1])
+    _head_rows(v, q, (n, hk, d), "v")
+    if hk < 1 or hq % hk:
+        raise ValueError(f"{hq} query heads cannot share {hk} key heads evenly")
+    batch = int(ranges.shape[0]) - 1 if ranges.dim() == 1 else 0
+    if batch < 1:
+        raise ValueError("ranges must hold at least two bounds")
+    _dev_tensor(ranges, torch.int32, (batch + 1,), "ranges")
+    if sinks < 0:
+        raise ValueError(f"sinks must be at least 0, got {sinks}")
+    scale = d ** -0.5 if scale is None else float(scale)
+    return n, hq, hk, d, batch, scale, _bound(left, "left"), _bound(right, "right"), int(sinks)
+
+
+def attn_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, ranges: torch.Tensor,
+             left: Optional[int] = None, right: Optional[int] = None, sinks: int = 0,
+             scale: Optional[float] = None, out: Optional[torch.Tensor] = None):
+    """Attention within each sample (``scn_attn_fwd``).  q [n, Hq, D], k and v
+    [n, Hk, D], float32 or bfloat16, any row and head strides; ``ranges`` from
+    ``site_ranges``.  Row i of a sample sees row j if j <= i + right and
+    (j >= i - left or j < sinks); None is no bound, right=0 causal.  scale is
+    D ** -0.5 unless given.  Returns (o [n, Hq, D], lse float32 [Hq, n])."""
+    n, hq, hk, d, batch, scale, l, r, sinks = _attn_args(q, k, v, ranges, left, right, sinks,
+                                                         scale)
+    o = _out_rows(out, q, (n, hq, d), "out")
+    lse = torch.empty((hq, n), dtype=torch.float32, device=q.device)
+    _check(lib().scn_attn_fwd(SCN_TYPE[q.dtype], n, batch, _ptr(ranges), d, hq, hk, _heads(q),
+                              _heads(k), _heads(v), scale, l, r, sinks, _heads(o), _ptr(lse),
+                              ctypes.c_void_p(_stream())), "scn_attn_fwd")
+    return o, lse
+
+
+def attn_bwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Tensor,
+             lse: torch.Tensor, do: torch.Tensor, ranges: torch.Tensor,
+             left: Optional[int] = None, right: Optional[int] = None, sinks: int = 0,
+             scale: Optional[float] = None, out=(None, None, None),
+             ws: Optional[torch.Tensor] = None):
+    """Gradients of ``attn_fwd`` (``scn_attn_bwd``): a dict with dq, dk and dv,
+    in ``out`` where given."""
+    n, hq, hk, d, batch, scale, l, r, sinks = _attn_args(q, k, v, ranges, left, right, sinks,
+                                                         scale)
+    _head_rows(o, q, (n, hq, d), "o")
+    _head_rows(do, q, (n, hq, d), "do")
+    _dev_tensor(lse, torch.float32, (hq, n), "lse")
+    res = {"dq": _out_rows(out[0], q, (n, hq, d), "out[0]"),
+           "dk": _out_rows(out[1], q, (n, hk, d), "out[1]"),
+           "dv": _out_rows(out[2], q, (n, hk, d), "out[2]")}
+    if ws is None:
+        ws = _bytes(lib().scn_attn_bwd_workspace_bytes(n, batch, d, hq, hk, l, sinks), q.device)
+    _check(lib().scn_attn_bwd(
+        SCN_TYPE[q.dtype], n, batch, _ptr(ranges), d, hq, hk, _heads(q), _heads(k), _heads(v),
+        _heads(o), _ptr(lse), _heads(do), scale, l, r, sinks, _heads(res["dq"]),
+        _heads(res["dk"]), _heads(res["dv"]), _ptr(ws), ws.numel(),
+        ctypes.c_void_p(_stream())), "scn_attn_bwd")
+    return res
+
+
+def attn_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor,
+              v_cache: torch.Tensor, length: torch.Tensor, left: Optional[int] = None,
+              sinks: int = 0, scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+              ws: Optional[torch.Tensor] = None):
+    """Attention of one new token of each stream (``scn_attn_step``).  q
+    [streams, Hq, D], k and v [streams, Hk, D]; the caches [streams, capacity,
+    Hk, D] (capacity > sinks; the rows past the sinks are a ring); length int32
+    [streams], the tokens written before.  Writes the new keys and values to the
+    caches and returns o [streams, Hq, D]; the caller advances length."""
+    _head_rows(q, None, (None, None, None), "q")
+    b, hq, d = (int(x) for x in q.shape)
+    _head_rows(k, q, (b, None, d), "k")
+    hk = int(k.shape[1])
+    _head_rows(v, q, (b, hk, d), "v")
+    if hk < 1 or hq % hk:
+        raise ValueError(f"{hq} query heads cannot share {hk} key heads evenly")
+    _head_rows(k_cache, q, (b, None, hk, d), "k_cache")
+    cap = int(k_cache.shape[1])
+    _head_rows(v_cache, q, (b, cap, hk, d), "v_cache")
+    _dev_tensor(length, torch.int32, (b,), "length")
+    if not 0 <= sinks < cap:
+        raise ValueError(f"sinks must lie in [0, capacity = {cap}), got {sinks}")
+    l = _bound(left, "left")
+    scale = d ** -0.5 if scale is None else float(scale)
+    o = _out_rows(out, q, (b, hq, d), "out")
+    if ws is None:
+        ws = _bytes(lib().scn_attn_step_workspace_bytes(b, cap, d, hq, hk, l, sinks), q.device)
+    _check(lib().scn_attn_step(
+        SCN_TYPE[q.dtype], b, cap, d, hq, hk, _heads(q), _heads(k), _heads(v), _cache(k_cache),
+        _cache(v_cache), _ptr(length), scale, l, int(sinks), _heads(o), _ptr(ws), ws.numel(),
+        ctypes.c_void_p(_stream())), "scn_attn_step")
+    return o
 
 
 def version() -> str:

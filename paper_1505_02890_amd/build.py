@@ -17,7 +17,8 @@ ROOT = os.path.dirname(HERE)
 LIB_PATH = os.path.join(HERE, "libscn.so")
 ARCH = "gfx950"
 
-SOURCES = ["common.hip", "rulebook.hip", "keyed.hip", "conv.hip", "tile.hip", "pool.hip", "ceiling.hip"]
+SOURCES = ["common.hip", "rulebook.hip", "keyed.hip", "conv.hip", "tile.hip", "pool.hip",
+           "ceiling.hip", "norm.hip", "attn_fwd.hip", "attn_bwd.hip", "attn_step.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 

@@ -1,0 +1,593 @@
+// Attention within samples, backward, in two passes that each own their sums, so that
+// nothing is added atomically: one over tiles of queries for dq (and <do, o>, which
+// the second pass needs), one over tiles of keys for dk and dv.  Both form the scores
+// again from q, k and the forward's log sums.
+//
+// Queries' pass, as the forward: S^T = K Q^T and dP^T = V dO^T with a query per lane,
+// dQ^T += K^T dS^T.  Keys' pass: S = Q K^T and dP = dO V^T with a key per lane,
+// dV^T += dO^T P and dK^T += Q^T dS.
+#include "attn.h"
+
+namespace scn {
+namespace {
+
+constexpr int RB = 128;        // rows of a block (32 a wave)
+constexpr int TB = 64;         // rows of the tiles that stream past them
+constexpr int NT = 256;
+constexpr int SC = 1024;       // queries of a sink share
+constexpr int SPLIT_SINKS = 256;
+
+template <int NS>
+struct BwdArgs {
+  typedef typename Elem<NS>::T T;
+  int64_t n;
+  int batch, D, Hq, Hk, group;
+  const int32_t* ranges;
+  Heads<const T> q, k, v, o, d_o;
+  Heads<T> dq, dk, dv;
+  const float* lse;  // [Hq][n]
+  float* delta;      // [Hq][n]
+  float* share;      // the sinks' shares [chunk][Hk][sinks][2][D], or null
+  float scale;
+  Window w;
+};
+
+// dq of one row once more in fp32, over the keys that it sees
+template <int NS>
+__device__ inline void dq_row(const BwdArgs<NS>& a, const Span& sp, int h, int i, float delta) {
+  typedef Elem<NS> E;
+  const int lane = threadIdx.x & 63;
+  const auto* const q = a.q.p + (sp.base + i) * a.q.row + h * a.q.head;
+  const auto* const g = a.d_o.p + (sp.base + i) * a.d_o.row + h * a.d_o.head;
+  const auto* const k = a.k.p + sp.base * a.k.row + (h / a.group) * a.k.head;
+  const auto* const v = a.v.p + sp.base * a.v.row + (h / a.group) * a.v.head;
+  const float lse = a.lse[h * a.n + sp.base + i];
+  const int lo = a.w.lo(i), hi = a.w.hi(i, sp.m), ns = min(a.w.sinks, lo);
+  const int cnt = ns + hi - lo + 1;
+  float o0 = 0.f, o1 = 0.f;
+  for (int x0 = 0; x0 < cnt; x0 += 64) {
+    float ds = 0.f;
+    if (x0 + lane < cnt) {
+      const int x = x0 + lane, j = x < ns ? x : lo + x - ns;
+      const float p = expf(row_dot<NS>(q, k + j * a.k.row, a.D) * a.scale - lse);
+      ds = p * (row_dot<NS>(g, v + j * a.v.row, a.D) - delta);
+    }
+    for (int y = 0; y < min(64, cnt - x0); ++y) {
+      const int x = x0 + y, j = x < ns ? x : lo + x - ns;
+      const float d = __shfl(ds, y);
+      if (lane < a.D) o0 = fmaf(d, E::get(k[j * a.k.row + lane]), o0);
+      if (64 + lane < a.D) o1 = fmaf(d, E::get(k[j * a.k.row + 64 + lane]), o1);
+    }
+  }
+  auto* const o = a.dq.p + (sp.base + i) * a.dq.row + h * a.dq.head;
+  if (lane < a.D) o[lane] = E::put(o0 * a.scale);
+  if (64 + lane < a.D) o[64 + lane] = E::put(o1 * a.scale);
+}
+
+// dk and dv of one row once more in fp32, over the queries that see it
+template <int NS>
+__device__ inline void dkv_row(const BwdArgs<NS>& a, const Span& sp, int hk, int j) {
+  typedef Elem<NS> E;
+  const int lane = threadIdx.x & 63;
+  const auto* const k = a.k.p + (sp.base + j) * a.k.row + hk * a.k.head;
+  const auto* const v = a.v.p + (sp.base + j) * a.v.row + hk * a.v.head;
+  const int lo = max(0, j - a.w.right);
+  const int hi = j < a.w.sinks ? sp.m - 1 : min(sp.m - 1, j + a.w.left);
+  float k0 = 0.f, k1 = 0.f, v0 = 0.f, v1 = 0.f;
+  for (int h = hk * a.group; h < (hk + 1) * a.group; ++h) {
+    const auto* const q = a.q.p + sp.base * a.q.row + h * a.q.head;
+    const auto* const g = a.d_o.p + sp.base * a.d_o.row + h * a.d_o.head;
+    for (int x0 = lo; x0 <= hi; x0 += 64) {
+      float p = 0.f, ds = 0.f;
+      const int i = x0 + lane;
+      if (i <= hi) {
+        const int64_t at = h * a.n + sp.base + i;
+        p = expf(row_dot<NS>(q + i * a.q.row, k, a.D) * a.scale - a.lse[at]);
+        ds = p * (row_dot<NS>(g + i * a.d_o.row, v, a.D) - a.delta[at]);
+      }
+      for (int y = 0; y < min(64, hi - x0 + 1); ++y) {
+        const float py = __shfl(p, y), dy = __shfl(ds, y);
+        const auto* const qi = q + (x0 + y) * a.q.row;
+        const auto* const gi = g + (x0 + y) * a.d_o.row;
+        if (lane < a.D) {
+          v0 = fmaf(py, E::get(gi[lane]), v0);
+          k0 = fmaf(dy, E::get(qi[lane]), k0);
+        }
+        if (64 + lane < a.D) {
+          v1 = fmaf(py, E::get(gi[64 + lane]), v1);
+          k1 = fmaf(dy, E::get(qi[64 + lane]), k1);
+        }
+      }
+    }
+  }
+  auto* const dk = a.dk.p + (sp.base + j) * a.dk.row + hk * a.dk.head;
+  auto* const dv = a.dv.p + (sp.base + j) * a.dv.row + hk * a.dv.head;
+  if (lane < a.D) {
+    dk[lane] = E::put(k0 * a.scale);
+    dv[lane] = E::put(v0);
+  }
+  if (64 + lane < a.D) {
+    dk[64 + lane] = E::put(k1 * a.scale);
+    dv[64 + lane] = E::put(v1);
+  }
+}
+
+template <int NS, int DP>
+__global__ void __launch_bounds__(NT, NS == 3 && DP > 32 ? 1 : 2) attn_dq_kernel(BwdArgs<NS> a) {
+  typedef Tile<NS, DP, TB> L;
+  typedef Elem<NS> E;
+  constexpr int NBUF = NS == 1 ? 2 : 1;
+  extern __shared__ char smem[];
+  const int tid = threadIdx.x, lane = tid & 63, n32 = lane & 31, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int h = blockIdx.x % a.Hq;
+  const Span sp = find_span<RB>(a.ranges, a.batch, a.n, blockIdx.x / a.Hq);
+  if (sp.first >= sp.m) return;
+  const int i0 = sp.first + wave * 32, i1 = min(i0 + 31, sp.m - 1);
+  const int i = min(i0 + n32, sp.m - 1);
+  const bool mine = i0 + n32 < sp.m;
+  const float c2 = a.scale * LOG2E;
+
+  Frag<NS> Q[DP / 16], G[DP / 16];
+  float delta = 0.f;
+  {
+    const auto* const q = a.q.p + (sp.base + i) * a.q.row + h * a.q.head;
+    const auto* const g = a.d_o.p + (sp.base + i) * a.d_o.row + h * a.d_o.head;
+    const auto* const o = a.o.p + (sp.base + i) * a.o.row + h * a.o.head;
+#pragma unroll
+    for (int s = 0; s < DP / 16; ++s) {
+      Q[s] = load_frag<NS>(q, s, a.D, lane);
+      G[s] = load_frag<NS>(g, s, a.D, lane);
+      const int c = 16 * s + 8 * half;
+      if (c < a.D)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) delta = fmaf(E::get(g[c + j]), E::get(o[c + j]), delta);
+    }
+  }
+  delta += other_half(delta);
+  const int64_t at = h * a.n + sp.base + i;
+  const float lse2 = a.lse[at] * LOG2E;
+  if (mine && half == 0) a.delta[at] = delta;
+  v16f dQ[DP / 32];
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d) dQ[d] = zero16();
+
+  const int lo = a.w.lo(sp.first), hi = a.w.hi(min(sp.first + RB, sp.m) - 1, sp.m);
+  const int ns = min(a.w.sinks, lo), nst = (ns + TB - 1) / TB;
+  const int ntile = nst + (hi - lo + TB) / TB;
+  const auto* const kp = a.k.p + sp.base * a.k.row + (h / a.group) * a.k.head;
+  const auto* const vp = a.v.p + sp.base * a.v.row + (h / a.group) * a.v.head;
+  Stage<NS, DP, TB, NT> sk, sv;
+  auto fetch = [&](int t) {
+    const int j0 = t < nst ? t * TB : lo + (t - nst) * TB, last = t < nst ? ns - 1 : hi;
+    sk.load(kp, a.k.row, j0, last, a.D, tid);
+    sv.load(vp, a.v.row, j0, last, a.D, tid);
+  };
+  fetch(0);
+  sk.store(smem, tid);
+  sv.store(smem + L::BYTES, tid);
+  __syncthreads();
+  for (int t = 0; t < ntile; ++t) {
+    if (t + 1 < ntile) fetch(t + 1);
+    char* const kt = smem + (NBUF == 2 ? (t & 1) * 2 * L::BYTES : 0);
+    char* const vt = kt + L::BYTES;
+    const bool sink = t < nst;
+    const int j0 = sink ? t * TB : lo + (t - nst) * TB, last = sink ? ns - 1 : hi;
+    const bool any = i0 <= i1 && j0 <= a.w.hi(i1, sp.m) &&
+                     (sink || j0 + TB > a.w.lo(i0) || j0 < a.w.sinks);
+    if (any) {
+      const bool all = j0 + TB - 1 <= last &&
+                       (sink || (j0 + TB - 1 <= i0 + a.w.right && j0 >= a.w.lo(i0 + 31)));
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        v16f S = zero16(), P = zero16();
+#pragma unroll
+        for (int s = 0; s < DP / 16; ++s) {
+          S = mma<NS>(L::rows(kt, 32 * b, s, lane), Q[s], S);
+          P = mma<NS>(L::rows(vt, 32 * b, s, lane), G[s], P);
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          float p = __builtin_amdgcn_exp2f(fmaf(S[r], c2, -lse2));
+          if (!all) {
+            const int j = j0 + 32 * b + 8 * (r / 4) + 4 * half + r % 4;
+            if (!(j <= last && (sink || a.w.sees(i, j)))) p = 0.f;
+          }
+          S[r] = p * (P[r] - delta);
+        }
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          float x[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) x[j] = S[8 * s + j];
+          const Frag<NS> X = to_frag<NS>(x);
+#pragma unroll
+          for (int d = 0; d < DP / 32; ++d)
+            dQ[d] = mma<NS>(L::cols(kt, 32 * b + 16 * s, d, lane), X, dQ[d]);
+        }
+      }
+    }
+    if (t + 1 < ntile) {
+      if (NBUF == 1) __syncthreads();
+      char* const nx = smem + (NBUF == 2 ? ((t & 1) ^ 1) * 2 * L::BYTES : 0);
+      sk.store(nx, tid);
+      sv.store(nx + L::BYTES, tid);
+      __syncthreads();
+    }
+  }
+  bool fine = true;
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d) fine &= finite16(dQ[d]);
+  if (mine) {
+    auto* const o = a.dq.p + (sp.base + i) * a.dq.row + h * a.dq.head;
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d) store_cols<NS>(o, dQ[d], a.scale, d, a.D, lane);
+  }
+  const uint64_t bad = __ballot(mine && !fine);
+  uint32_t rows = (uint32_t)bad | (uint32_t)(bad >> 32);
+  while (rows) {
+    const int r = __builtin_ctz(rows);
+    rows &= rows - 1;
+    dq_row<NS>(a, sp, h, i0 + r, __shfl(delta, r));
+  }
+}
+
+// What a wave with 32 keys does with 32 queries of a tile: dV += P^T dO, dK += dS^T Q
+// (transposed).  see(i, j) masks the pairs of query i0 + row and key j if `mask`.
+template <int NS, int DP, class See>
+__device__ inline void key_block(char* qt, char* gt, const float* lse2, const float* delta, int r0,
+                                 const Frag<NS> (&K)[DP / 16], const Frag<NS> (&V)[DP / 16],
+                                 float c2, bool mask, const See& see, v16f (&dK)[DP / 32],
+                                 v16f (&dV)[DP / 32]) {
+  typedef Tile<NS, DP, TB> L;
+  const int lane = threadIdx.x & 63, half = lane >> 5;
+  v16f S = zero16(), P = zero16();
+#pragma unroll
+  for (int s = 0; s < DP / 16; ++s) {
+    S = mma<NS>(L::rows(qt, r0, s, lane), K[s], S);
+    P = mma<NS>(L::rows(gt, r0, s, lane), V[s], P);
+  }
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    const v4f l = *reinterpret_cast<const v4f*>(lse2 + r0 + 8 * g + 4 * half);
+    const v4f e = *reinterpret_cast<const v4f*>(delta + r0 + 8 * g + 4 * half);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int r = 4 * g + j;
+      float p = __builtin_amdgcn_exp2f(fmaf(S[r], c2, -l[j]));
+      if (mask && !see(r0 + 8 * g + 4 * half + j)) p = 0.f;
+      S[r] = p;
+      P[r] = p * (P[r] - e[j]);
+    }
+  }
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    float x[8], y[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      x[j] = S[8 * s + j];
+      y[j] = P[8 * s + j];
+    }
+    const Frag<NS> X = to_frag<NS>(x), Y = to_frag<NS>(y);
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d) {
+      dV[d] = mma<NS>(L::cols(gt, r0 + 16 * s, d, lane), X, dV[d]);
+      dK[d] = mma<NS>(L::cols(qt, r0 + 16 * s, d, lane), Y, dK[d]);
+    }
+  }
+}
+
+// The tiles of queries that stream past a block's keys, over its query heads
+template <int NS, int DP, int THREADS>
+struct QueryTiles {
+  typedef Tile<NS, DP, TB> L;
+  static constexpr int BUF = 2 * L::BYTES + 2 * TB * 4;
+  Stage<NS, DP, TB, THREADS> q, g;
+  float lse2, delta;
+  __device__ inline void fetch(const BwdArgs<NS>& a, const Span& sp, int h, int i0, int last,
+                               int tid) {
+    q.load(a.q.p + sp.base * a.q.row + h * a.q.head, a.q.row, i0, last, a.D, tid);
+    g.load(a.d_o.p + sp.base * a.d_o.row + h * a.d_o.head, a.d_o.row, i0, last, a.D, tid);
+    if (tid < TB) {
+      const int64_t at = h * a.n + sp.base + min(i0 + tid, last);
+      lse2 = a.lse[at] * LOG2E;
+      delta = a.delta[at];
+    }
+  }
+  __device__ inline void store(char* b, int tid) const {
+    q.store(b, tid);
+    g.store(b + L::BYTES, tid);
+    if (tid < TB) {
+      float* const f = reinterpret_cast<float*>(b + 2 * L::BYTES);
+      f[tid] = lse2;
+      f[TB + tid] = delta;
+    }
+  }
+};
+
+// Sinks are seen by every later query, so a block that owned them would run far longer
+// than the others.  Their pairs past the window go here, in shares of SC queries:
+// block (chunk, sink tile of 32, key head), two waves with 32 queries of each tile.
+template <int NS, int DP>
+__global__ void __launch_bounds__(128, 1) attn_sink_kernel(BwdArgs<NS> a, int nst) {
+  typedef QueryTiles<NS, DP, 128> QT;
+  typedef typename QT::L L;
+  extern __shared__ char smem[];
+  const int tid = threadIdx.x, lane = tid & 63, n32 = lane & 31, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int hk = blockIdx.x % a.Hk, j0 = blockIdx.x / a.Hk % nst * 32;
+  const int chunk = blockIdx.x / a.Hk / nst;
+  const Span sp = find_span<SC>(a.ranges, a.batch, a.n, chunk);
+  const int ns = min(a.w.sinks, sp.m);
+  const int end = min(sp.first + SC, sp.m) - 1;         // the share's queries
+  const int first = max(sp.first, j0 + a.w.left + 1);   // ... past the window of j0
+  if (sp.first >= sp.m || j0 >= ns || first > end) return;
+  const int j = min(j0 + n32, ns - 1);
+  const float c2 = a.scale * LOG2E;
+  Frag<NS> K[DP / 16], V[DP / 16];
+#pragma unroll
+  for (int s = 0; s < DP / 16; ++s) {
+    K[s] = load_frag<NS>(a.k.p + (sp.base + j) * a.k.row + hk * a.k.head, s, a.D, lane);
+    V[s] = load_frag<NS>(a.v.p + (sp.base + j) * a.v.row + hk * a.v.head, s, a.D, lane);
+  }
+  v16f dK[DP / 32], dV[DP / 32];
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d) dK[d] = dV[d] = zero16();
+  QT st;
+  const int per = (end - first + TB) / TB, ntile = per * a.group;
+  st.fetch(a, sp, hk * a.group, first, end, tid);
+  for (int t = 0; t < ntile; ++t) {
+    st.store(smem, tid);
+    __syncthreads();
+    const int i0 = first + t % per * TB;
+    if (t + 1 < ntile)
+      st.fetch(a, sp, hk * a.group + (t + 1) / per, first + (t + 1) % per * TB, end, tid);
+    const float* const f = reinterpret_cast<const float*>(smem + 2 * L::BYTES);
+    auto see = [&](int r) { return i0 + r <= end && j < i0 + r - a.w.left; };
+    key_block<NS, DP>(smem, smem + L::BYTES, f, f + TB, 32 * wave, K, V, c2, true, see, dK, dV);
+    __syncthreads();
+  }
+  // the second wave's sums through LDS, then out
+  float* const x = reinterpret_cast<float*>(smem);
+  if (wave == 1)
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        x[(d * 16 + r) * 64 + lane] = dK[d][r];
+        x[((DP / 32 + d) * 16 + r) * 64 + lane] = dV[d][r];
+      }
+  __syncthreads();
+  if (wave == 1 || j0 + n32 >= ns) return;
+  float* const out =
+      a.share + (((int64_t)chunk * a.Hk + hk) * a.w.sinks + j) * 2 * a.D;
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int c = 32 * d + 8 * (r / 4) + 4 * half + r % 4;
+      if (c < a.D) {
+        out[c] = dK[d][r] + x[(d * 16 + r) * 64 + lane];
+        out[a.D + c] = dV[d][r] + x[((DP / 32 + d) * 16 + r) * 64 + lane];
+      }
+    }
+}
+
+template <int NS, int DP>
+__global__ void __launch_bounds__(NT, NS == 3 || DP > 64 ? 1 : 2) attn_dkv_kernel(BwdArgs<NS> a) {
+  typedef QueryTiles<NS, DP, NT> QT;
+  typedef typename QT::L L;
+  constexpr int NBUF = NS == 1 ? 2 : 1;
+  extern __shared__ char smem[];
+  const int tid = threadIdx.x, lane = tid & 63, n32 = lane & 31, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int hk = blockIdx.x % a.Hk;
+  const Span sp = find_span<RB>(a.ranges, a.batch, a.n, blockIdx.x / a.Hk);
+  if (sp.first >= sp.m) return;
+  const int j0 = sp.first + wave * 32, j1 = min(j0 + 31, sp.m - 1);  // the wave's keys
+  const int j = min(j0 + n32, sp.m - 1);
+  const float c2 = a.scale * LOG2E;
+  // sinks whose far queries other blocks have taken are ordinary keys here
+  const int sinks = a.share ? 0 : a.w.sinks;
+  const Window w{a.w.left, a.w.right, sinks};
+
+  Frag<NS> K[DP / 16], V[DP / 16];
+#pragma unroll
+  for (int s = 0; s < DP / 16; ++s) {
+    K[s] = load_frag<NS>(a.k.p + (sp.base + j) * a.k.row + hk * a.k.head, s, a.D, lane);
+    V[s] = load_frag<NS>(a.v.p + (sp.base + j) * a.v.row + hk * a.v.head, s, a.D, lane);
+  }
+  v16f dK[DP / 32], dV[DP / 32];
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d) dK[d] = dV[d] = zero16();
+
+  const int first = max(0, sp.first - w.right);
+  const int end = sp.first < sinks ? sp.m - 1
+                                   : min(sp.m - 1, min(sp.first + RB, sp.m) - 1 + w.left);
+  const int per = (end - first + TB) / TB, ntile = per * a.group;
+  QT st;
+  auto fetch = [&](int t) {
+    st.fetch(a, sp, hk * a.group + t / per, first + t % per * TB, end, tid);
+  };
+  fetch(0);
+  st.store(smem, tid);
+  __syncthreads();
+  for (int t = 0; t < ntile; ++t) {
+    if (t + 1 < ntile) fetch(t + 1);
+    char* const b = smem + (NBUF == 2 ? (t & 1) * QT::BUF : 0);
+    const float* const f = reinterpret_cast<const float*>(b + 2 * L::BYTES);
+#pragma unroll
+    for (int u = 0; u < TB / 32; ++u) {
+      const int i0 = first + t % per * TB + 32 * u, i1 = i0 + 31;
+      const bool any = j0 <= j1 && i0 <= end && j0 <= i1 + w.right &&
+                       (j1 >= i0 - w.left || j0 < sinks);
+      const bool all = i1 <= end && j0 + 31 <= i0 + w.right && j0 >= i1 - w.left;
+      auto see = [&](int r) {
+        const int i = i0 - 32 * u + r;
+        return i <= end && w.sees(i, j);
+      };
+      if (any)
+        key_block<NS, DP>(b, b + L::BYTES, f, f + TB, 32 * u, K, V, c2, !all, see, dK, dV);
+    }
+    if (t + 1 < ntile) {
+      if (NBUF == 1) __syncthreads();
+      st.store(smem + (NBUF == 2 ? ((t & 1) ^ 1) * QT::BUF : 0), tid);
+      __syncthreads();
+    }
+  }
+  const bool mine = j0 + n32 < sp.m;
+  const int far = (j & ~31) + a.w.left + 1;  // first query past the window of the sink tile
+  if (a.share && mine && j < a.w.sinks && far < sp.m) {
+    // the shares of these queries, in order
+    const int64_t chunk0 = sp.base / SC + sp.sample;
+    for (int c = far / SC; c < (sp.m + SC - 1) / SC; ++c) {
+      const float* const p = a.share + (((chunk0 + c) * a.Hk + hk) * a.w.sinks + j) * 2 * a.D;
+#pragma unroll
+      for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const int ch = 32 * d + 8 * g + 4 * half;
+          if (ch >= a.D) continue;
+          const v4f x = *reinterpret_cast<const v4f*>(p + ch);
+          const v4f y = *reinterpret_cast<const v4f*>(p + a.D + ch);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            dK[d][4 * g + e] += x[e];
+            dV[d][4 * g + e] += y[e];
+          }
+        }
+    }
+  }
+  bool fine = true;
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d) fine &= finite16(dK[d]) && finite16(dV[d]);
+  if (mine) {
+    auto* const dk = a.dk.p + (sp.base + j) * a.dk.row + hk * a.dk.head;
+    auto* const dv = a.dv.p + (sp.base + j) * a.dv.row + hk * a.dv.head;
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d) {
+      store_cols<NS>(dk, dK[d], a.scale, d, a.D, lane);
+      store_cols<NS>(dv, dV[d], 1.f, d, a.D, lane);
+    }
+  }
+  const uint64_t bad = __ballot(mine && !fine);
+  uint32_t rows = (uint32_t)bad | (uint32_t)(bad >> 32);
+  while (rows) {
+    const int r = __builtin_ctz(rows);
+    rows &= rows - 1;
+    dkv_row<NS>(a, sp, hk, j0 + r);
+  }
+}
+
+// Sinks get their own blocks when a window ends before them (a left bound) and they
+// are few; many sinks keep the blocks of their keys busy anyway.
+bool split_sinks(int64_t n, int64_t left, int64_t sinks) {
+  return left >= 0 && left < n && sinks > 0 && sinks <= SPLIT_SINKS;
+}
+int64_t sink_chunks(int64_t n, int batch) { return n / SC + batch; }
+
+template <int NS, int DP>
+scn_status launch(const BwdArgs<NS>& a, hipStream_t st) {
+  const int64_t tiles = a.n / RB + a.batch;
+  const int nst = (a.w.sinks + 31) / 32;
+  const int64_t shares = a.share ? sink_chunks(a.n, a.batch) * a.Hk * nst : 0;
+  if (std::max(tiles * a.Hq, shares) > INT32_MAX) {
+    set_error("scn_attn_bwd: more than 2^31 blocks of rows and heads");
+    return SCN_ERR_OVERFLOW;
+  }
+  {
+    constexpr size_t smem = (NS == 1 ? 4 : 2) * Tile<NS, DP, TB>::BYTES;
+    static LdsLimit limit;
+    auto fn = attn_dq_kernel<NS, DP>;
+    if (scn_status rc = allow_lds(reinterpret_cast<const void*>(fn), limit, smem)) return rc;
+    hipLaunchKernelGGL(fn, dim3((unsigned)(tiles * a.Hq)), dim3(NT), smem, st, a);
+    SCN_LAUNCH_CHECK();
+  }
+  if (a.share) {
+    constexpr size_t smem = std::max<size_t>(QueryTiles<NS, DP, 128>::BUF, DP * 2 * 32 * 4);
+    static LdsLimit limit;
+    auto fn = attn_sink_kernel<NS, DP>;
+    if (scn_status rc = allow_lds(reinterpret_cast<const void*>(fn), limit, smem)) return rc;
+    hipLaunchKernelGGL(fn, dim3((unsigned)shares), dim3(128), smem, st, a, nst);
+    SCN_LAUNCH_CHECK();
+  }
+  constexpr size_t smem = (NS == 1 ? 2 : 1) * QueryTiles<NS, DP, NT>::BUF;
+  static LdsLimit limit;
+  auto fn = attn_dkv_kernel<NS, DP>;
+  if (scn_status rc = allow_lds(reinterpret_cast<const void*>(fn), limit, smem)) return rc;
+  hipLaunchKernelGGL(fn, dim3((unsigned)(tiles * a.Hk)), dim3(NT), smem, st, a);
+  SCN_LAUNCH_CHECK();
+  return SCN_OK;
+}
+
+template <int NS>
+scn_status run(const BwdArgs<NS>& a, hipStream_t st) {
+  if (a.D <= 32) return launch<NS, 32>(a, st);
+  if (a.D <= 64) return launch<NS, 64>(a, st);
+  if (a.D <= 96) return launch<NS, 96>(a, st);
+  return launch<NS, 128>(a, st);
+}
+
+int64_t delta_floats(int64_t n, int Hq) { return (n * Hq + 63) & ~int64_t(63); }
+
+}  // namespace
+}  // namespace scn
+
+using namespace scn;
+
+extern "C" {
+
+size_t scn_attn_bwd_workspace_bytes(int64_t n, int32_t batch, int32_t D, int32_t Hq, int32_t Hk,
+                                    int64_t left, int64_t sinks) {
+  if (n <= 0 || n > ATTN_ROWS || batch < 1 || D < 1 || D > ATTN_D || Hq < 1 || Hk < 1 || sinks < 0)
+    return 0;
+  int64_t f = delta_floats(n, Hq);
+  if (split_sinks(n, left, sinks))
+    f += sink_chunks(n, batch) * Hk * std::min(sinks, n) * 2 * D;
+  return (size_t)f * 4;
+}
+
+scn_status scn_attn_bwd(int32_t type, int64_t n, int32_t batch, const int32_t* ranges, int32_t D,
+                        int32_t Hq, int32_t Hk, const scn_heads* q, const scn_heads* k,
+                        const scn_heads* v, const scn_heads* o, const float* lse,
+                        const scn_heads* d_o, float scale, int64_t left, int64_t right,
+                        int64_t sinks, const scn_heads* dq, const scn_heads* dk,
+                        const scn_heads* dv, void* ws, size_t ws_bytes, hipStream_t st) {
+  clear_error();
+  const char* const who = "scn_attn_bwd";
+  if (scn_status rc = check_attn(who, type, n, batch, ranges, D, Hq, Hk, scale)) return rc;
+  if (sinks < 0 || (n > 0 && !lse)) {
+    set_error("%s: negative number of sinks, or lse is null", who);
+    return SCN_ERR_INVALID;
+  }
+  if (n == 0) return SCN_OK;
+  const struct {
+    const scn_heads* h;
+    const char* name;
+  } all[] = {{q, "q"}, {k, "k"}, {v, "v"}, {o, "o"}, {d_o, "d_o"}, {dq, "dq"}, {dk, "dk"},
+             {dv, "dv"}};
+  for (const auto& x : all)
+    if (scn_status rc = check_heads(who, x.name, x.h, type)) return rc;
+  if (!ws || (reinterpret_cast<uintptr_t>(ws) & 15) != 0 ||
+      ws_bytes < scn_attn_bwd_workspace_bytes(n, batch, D, Hq, Hk, left, sinks)) {
+    set_error("%s: workspace missing, misaligned or too small", who);
+    return SCN_ERR_WORKSPACE;
+  }
+  float* const delta = static_cast<float*>(ws);
+  float* const share = split_sinks(n, left, sinks) ? delta + delta_floats(n, Hq) : nullptr;
+  const Window w{bound(left, n), bound(right, n), bound(sinks, n)};
+  if (type == SCN_BF16) {
+    typedef uint16_t T;
+    return run<1>(BwdArgs<1>{n, batch, D, Hq, Hk, Hq / Hk, ranges, view<const T>(q),
+                             view<const T>(k), view<const T>(v), view<const T>(o),
+                             view<const T>(d_o), view<T>(dq), view<T>(dk), view<T>(dv), lse, delta,
+                             share, scale, w}, st);
+  }
+  typedef float T;
+  return run<3>(BwdArgs<3>{n, batch, D, Hq, Hk, Hq / Hk, ranges, view<const T>(q),
+                           view<const T>(k), view<const T>(v), view<const T>(o),
+                           view<const T>(d_o), view<T>(dq), view<T>(dk), view<T>(dv), lse, delta,
+                           share, scale, w}, st);
+}
+
+}  // extern "C"
