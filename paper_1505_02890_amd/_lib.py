@@ -392,45 +392,84 @@ def maxpool_bwd(rb: Rulebook, argmax: torch.Tensor, dy: torch.Tensor,
 SCN_TYPE = {torch.float32: 0, torch.bfloat16: 1}
 
 
-def _head_rows(t: torch.Tensor, like: Optional[torch.Tensor], shape, name: str) -> torch.Tensor:
-    """A [rows, heads, D] tensor (any strides with contiguous channels) of the
-    type and device of `like`."""
+def _refuse_rows(t, dtype, device: int, shape, name: str):
+    """Why `_rows` or `_cache` did not take a tensor."""
     if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
         raise TypeError(f"{name} must be a CUDA (HIP) tensor")
     if t.dtype not in SCN_TYPE:
         raise TypeError(f"{name} must be float32 or bfloat16, got {t.dtype}")
-    if like is not None and (t.dtype != like.dtype or t.device != like.device):
-        raise TypeError(f"{name} must be {like.dtype} on {like.device}, got {t.dtype} on {t.device}")
-    if t.dim() != len(shape) or any(s is not None and s != n for s, n in zip(shape, t.shape)):
-        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-    if t.numel() and t.shape[-1] > 1 and t.stride(-1) != 1:
+    if t.dtype != dtype or t.get_device() != device:
+        raise TypeError(f"{name} must be {dtype} on cuda:{device}, got {t.dtype} on {t.device}")
+    raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+
+
+def _first(t: torch.Tensor, name: str):
+    """The shape [rows, heads, D], type and device that a call's other tensors
+    follow."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype not in SCN_TYPE:
+        _refuse_rows(t, None, -1, (), name)
+    if t.dim() != 3:
+        raise ValueError(f"{name} must have three dimensions, got {tuple(t.shape)}")
+    device = t.get_device()
+    if device != torch.cuda.current_device():
+        raise ValueError(f"{name} is on cuda:{device}, which is not the current device")
+    return t.shape, t.dtype, device
+
+
+def _rows(t: torch.Tensor, dtype, device: int, shape, name: str):
+    """ctypes view of a [rows, heads, D] tensor (any strides with contiguous
+    channels).  A stride that no element is reached by (one row, one head) is
+    passed as 0, whatever torch holds there."""
+    if not (isinstance(t, torch.Tensor) and t.dtype == dtype and t.is_cuda and
+            t.get_device() == device and t.shape == shape):
+        _refuse_rows(t, dtype, device, shape, name)
+    row, head, one = t.stride()
+    if one != 1 and shape[2] > 1:
         raise ValueError(f"{name} must have contiguous channels")
-    return t
+    return _Heads(t.data_ptr(), row if shape[0] > 1 else 0, head if shape[1] > 1 else 0)
 
 
-def _heads(t: Optional[torch.Tensor]):
-    """ctypes view of a [rows, heads, D] tensor.  A stride that no element is
-    reached by (one row, one head) is passed as 0, whatever torch holds there."""
+def _cache(t: torch.Tensor, dtype, device: int, shape, name: str):
+    """The same of a [streams, capacity, heads, D] cache."""
+    if not (isinstance(t, torch.Tensor) and t.dtype == dtype and t.is_cuda and
+            t.get_device() == device and t.shape == shape):
+        _refuse_rows(t, dtype, device, shape, name)
+    stream, row, head, one = t.stride()
+    if one != 1 and shape[3] > 1:
+        raise ValueError(f"{name} must have contiguous channels")
+    return _Cache(t.data_ptr(), stream if shape[0] > 1 else 0, row if shape[1] > 1 else 0,
+                  head if shape[2] > 1 else 0)
+
+
+def _out_rows(t: Optional[torch.Tensor], like: torch.Tensor, shape, name: str):
+    """(result, its view), allocated here unless given.  A given result must
+    not hold one element twice."""
+    if t is None:
+        t = torch.empty(shape, dtype=like.dtype, device=like.device)
+        return t, _Heads(t.data_ptr(), shape[1] * shape[2], shape[2])
+    v = _rows(t, like.dtype, like.get_device(), shape, name)
+    if t.numel() and (v.row == 0 and shape[0] > 1 or v.head == 0 and shape[1] > 1):
+        raise ValueError(f"{name} must not be expanded")
+    return t, v
+
+
+def _vector(t, dtype, device: int, shape, name: str):
+    """Device pointer of a contiguous tensor, or None."""
     if t is None:
         return None
-    row = t.stride(0) if t.shape[0] > 1 else 0
-    head = t.stride(1) if t.shape[1] > 1 else 0
-    return ctypes.byref(_Heads(t.data_ptr(), row, head))
+    if not (isinstance(t, torch.Tensor) and t.dtype == dtype and t.is_cuda and
+            t.get_device() == device and t.shape == shape and t.is_contiguous()):
+        _dev_tensor(t, dtype, shape, name)
+        raise TypeError(f"{name} must be on cuda:{device}, got {t.device}")
+    return t.data_ptr()
 
 
-def _cache(t: torch.Tensor):
-    st = [t.stride(i) if t.shape[i] > 1 else 0 for i in range(3)]
-    return ctypes.byref(_Cache(t.data_ptr(), *st))
-
-
-def _out_rows(t: Optional[torch.Tensor], like: torch.Tensor, shape, name: str) -> torch.Tensor:
-    if t is None:
-        return torch.empty(shape, dtype=like.dtype, device=like.device)
-    return _head_rows(t, like, shape, name)
+def _raw_stream(device: int) -> int:
+    return torch._C._cuda_getCurrentRawStream(device)
 
 
 def _bytes(n: int, device) -> torch.Tensor:
-    return torch.empty(max(int(n), 1), dtype=torch.uint8, device=device)
+    return torch.empty(n or 1, dtype=torch.uint8, device=device)
 
 
 def site_ranges(coords: torch.Tensor, batch: int) -> torch.Tensor:
@@ -460,19 +499,20 @@ def rotation_freqs(dim: int, sections: Sequence[int], base: float = 100.0,
 
 
 def _norm_args(q, k, wq, wk, coords, freq, sections):
-    _head_rows(q, None, (None, None, None), "q")
-    n, hq, d = (int(v) for v in q.shape)
+    shape, dtype, dev = _first(q, "q")
+    n, hq, d = shape
     hk = 0
+    vk = None
     if k is not None:
-        _head_rows(k, q, (n, None, d), "k")
-        hk = int(k.shape[1])
-    for w, name in ((wq, "wq"), (wk, "wk")):
-        if w is not None:
-            _dev_tensor(w, torch.float32, (d,), name)
-    _dev_tensor(coords, torch.int32, (n, len(sections) + 1), "coords")
-    _dev_tensor(freq, torch.float32, (d // 2,), "freq")
-    sec = (ctypes.c_int32 * max(1, len(sections)))(*[int(m) for m in sections])
-    return n, hq, hk, d, sec
+        hk = k.shape[1] if k.dim() == 3 else 0
+        vk = _rows(k, dtype, dev, (n, hk, d), "k")
+    vq = _rows(q, dtype, dev, shape, "q")
+    na = len(sections)
+    return (SCN_TYPE[dtype], n, d, hq, hk, vq, vk, _vector(wq, torch.float32, dev, (d,), "wq"),
+            _vector(wk, torch.float32, dev, (d,), "wk"),
+            _vector(coords, torch.int32, dev, (n, na + 1), "coords"), na + 1,
+            _vector(freq, torch.float32, dev, (d // 2,), "freq"),
+            (ctypes.c_int32 * max(1, na))(*sections), dtype, dev)
 
 
 def norm_rotate_fwd(q: torch.Tensor, k: Optional[torch.Tensor], wq: Optional[torch.Tensor],
@@ -484,13 +524,13 @@ def norm_rotate_fwd(q: torch.Tensor, k: Optional[torch.Tensor], wq: Optional[tor
     None; coords int32 [n, 1 + axes]; freq float32 [D / 2]; sections the pairs
     of each axis.  Returns (qr, kr), in ``out`` where given (q and k themselves
     may be)."""
-    n, hq, hk, d, sec = _norm_args(q, k, wq, wk, coords, freq, sections)
-    qr = _out_rows(out[0], q, (n, hq, d), "out[0]")
-    kr = None if k is None else _out_rows(out[1], q, (n, hk, d), "out[1]")
-    _check(lib().scn_norm_rotate_fwd(
-        SCN_TYPE[q.dtype], n, d, hq, hk, _heads(q), _heads(k), _ptr(wq), _ptr(wk), float(eps),
-        _ptr(coords), len(sections) + 1, _ptr(freq), sec, _heads(qr), _heads(kr),
-        ctypes.c_void_p(_stream())), "scn_norm_rotate_fwd")
+    typ, n, d, hq, hk, vq, vk, pwq, pwk, pc, width, pf, sec, _, dev = _norm_args(
+        q, k, wq, wk, coords, freq, sections)
+    qr, oq = _out_rows(out[0], q, (n, hq, d), "out[0]")
+    kr, ok = (None, None) if k is None else _out_rows(out[1], q, (n, hk, d), "out[1]")
+    _check(lib().scn_norm_rotate_fwd(typ, n, d, hq, hk, _ref(vq), _ref(vk), pwq, pwk, eps, pc,
+                                     width, pf, sec, _ref(oq), _ref(ok), _raw_stream(dev)),
+           "scn_norm_rotate_fwd")
     return qr, kr
 
 
@@ -501,25 +541,30 @@ def norm_rotate_bwd(q: torch.Tensor, k: Optional[torch.Tensor], wq: Optional[tor
                     ws: Optional[torch.Tensor] = None):
     """Gradients of ``norm_rotate_fwd``: a dict with dq, dk (in ``out`` where
     given; dqr and dkr themselves may be) and the requested ones of dwq, dwk."""
-    n, hq, hk, d, sec = _norm_args(q, k, wq, wk, coords, freq, sections)
-    _head_rows(dqr, q, (n, hq, d), "dqr")
-    res = {"dq": _out_rows(out[0], q, (n, hq, d), "out[0]")}
+    typ, n, d, hq, hk, vq, vk, pwq, pwk, pc, width, pf, sec, dtype, dev = _norm_args(
+        q, k, wq, wk, coords, freq, sections)
+    gq = _rows(dqr, dtype, dev, (n, hq, d), "dqr")
+    res, gk, ok = {}, None, None
+    res["dq"], oq = _out_rows(out[0], q, (n, hq, d), "out[0]")
     if k is not None:
-        _head_rows(dkr, q, (n, hk, d), "dkr")
-        res["dk"] = _out_rows(out[1], q, (n, hk, d), "out[1]")
-    else:
-        dkr = None
+        gk = _rows(dkr, dtype, dev, (n, hk, d), "dkr")
+        res["dk"], ok = _out_rows(out[1], q, (n, hk, d), "out[1]")
+    pw = {}
     for name in ("dwq", "dwk"):
         if name in need and (name == "dwq" or k is not None):
             res[name] = torch.empty(d, dtype=torch.float32, device=q.device)
+            pw[name] = res[name].data_ptr()
     if ws is None:
-        ws = _bytes(lib().scn_norm_rotate_bwd_workspace_bytes(n, d, hq, hk), q.device)
+        ws = _bytes(lib().scn_norm_rotate_bwd_workspace_bytes(n, d, hq, hk) if pw else 0, q.device)
     _check(lib().scn_norm_rotate_bwd(
-        SCN_TYPE[q.dtype], n, d, hq, hk, _heads(q), _heads(k), _ptr(wq), _ptr(wk), float(eps),
-        _ptr(coords), len(sections) + 1, _ptr(freq), sec, _heads(dqr), _heads(dkr),
-        _heads(res["dq"]), _heads(res.get("dk")), _ptr(res.get("dwq")), _ptr(res.get("dwk")),
-        _ptr(ws), ws.numel(), ctypes.c_void_p(_stream())), "scn_norm_rotate_bwd")
+        typ, n, d, hq, hk, _ref(vq), _ref(vk), pwq, pwk, eps, pc, width, pf, sec, _ref(gq),
+        _ref(gk), _ref(oq), _ref(ok), pw.get("dwq"), pw.get("dwk"), ws.data_ptr(), ws.numel(),
+        _raw_stream(dev)), "scn_norm_rotate_bwd")
     return res
+
+
+def _ref(v):
+    return None if v is None else ctypes.byref(v)
 
 
 def _bound(w: Optional[int], name: str) -> int:
@@ -527,25 +572,30 @@ def _bound(w: Optional[int], name: str) -> int:
         return -1
     if w < 0:
         raise ValueError(f"{name} must be None (no bound) or at least 0, got {w}")
-    return int(w)
+    return w
 
 
-def _attn_args(q, k, v, ranges, left, right, sinks, scale):
-    _head_rows(q, None, (None, None, None), "q")
-    n, hq, d = (int(x) for x in q.shape)
-    _head_rows(k, q, (n, None, d), "k")
-    hk = int(k.shape[1])
-    _head_rows(v, q, (n, hk, d), "v")
+def _qkv(q, k, v):
+    shape, dtype, dev = _first(q, "q")
+    n, hq, d = shape
+    hk = k.shape[1] if isinstance(k, torch.Tensor) and k.dim() == 3 else 0
+    vq = _rows(q, dtype, dev, shape, "q")
+    vk = _rows(k, dtype, dev, (n, hk, d), "k")
+    vv = _rows(v, dtype, dev, (n, hk, d), "v")
     if hk < 1 or hq % hk:
         raise ValueError(f"{hq} query heads cannot share {hk} key heads evenly")
-    batch = int(ranges.shape[0]) - 1 if ranges.dim() == 1 else 0
+    return dtype, dev, n, hq, hk, d, vq, vk, vv
+
+
+def _attn_args(ranges, dev, left, right, sinks, scale, d):
+    batch = ranges.shape[0] - 1 if isinstance(ranges, torch.Tensor) and ranges.dim() == 1 else 0
     if batch < 1:
         raise ValueError("ranges must hold at least two bounds")
-    _dev_tensor(ranges, torch.int32, (batch + 1,), "ranges")
+    pr = _vector(ranges, torch.int32, dev, (batch + 1,), "ranges")
     if sinks < 0:
         raise ValueError(f"sinks must be at least 0, got {sinks}")
-    scale = d ** -0.5 if scale is None else float(scale)
-    return n, hq, hk, d, batch, scale, _bound(left, "left"), _bound(right, "right"), int(sinks)
+    return (batch, pr, d ** -0.5 if scale is None else scale, _bound(left, "left"),
+            _bound(right, "right"))
 
 
 def attn_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, ranges: torch.Tensor,
@@ -556,13 +606,13 @@ def attn_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, ranges: torch.Te
     ``site_ranges``.  Row i of a sample sees row j if j <= i + right and
     (j >= i - left or j < sinks); None is no bound, right=0 causal.  scale is
     D ** -0.5 unless given.  Returns (o [n, Hq, D], lse float32 [Hq, n])."""
-    n, hq, hk, d, batch, scale, l, r, sinks = _attn_args(q, k, v, ranges, left, right, sinks,
-                                                         scale)
-    o = _out_rows(out, q, (n, hq, d), "out")
+    dtype, dev, n, hq, hk, d, vq, vk, vv = _qkv(q, k, v)
+    batch, pr, scale, l, r = _attn_args(ranges, dev, left, right, sinks, scale, d)
+    o, vo = _out_rows(out, q, (n, hq, d), "out")
     lse = torch.empty((hq, n), dtype=torch.float32, device=q.device)
-    _check(lib().scn_attn_fwd(SCN_TYPE[q.dtype], n, batch, _ptr(ranges), d, hq, hk, _heads(q),
-                              _heads(k), _heads(v), scale, l, r, sinks, _heads(o), _ptr(lse),
-                              ctypes.c_void_p(_stream())), "scn_attn_fwd")
+    _check(lib().scn_attn_fwd(SCN_TYPE[dtype], n, batch, pr, d, hq, hk, _ref(vq), _ref(vk),
+                              _ref(vv), scale, l, r, sinks, _ref(vo), lse.data_ptr(),
+                              _raw_stream(dev)), "scn_attn_fwd")
     return o, lse
 
 
@@ -573,22 +623,21 @@ def attn_bwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Tensor,
              ws: Optional[torch.Tensor] = None):
     """Gradients of ``attn_fwd`` (``scn_attn_bwd``): a dict with dq, dk and dv,
     in ``out`` where given."""
-    n, hq, hk, d, batch, scale, l, r, sinks = _attn_args(q, k, v, ranges, left, right, sinks,
-                                                         scale)
-    _head_rows(o, q, (n, hq, d), "o")
-    _head_rows(do, q, (n, hq, d), "do")
-    _dev_tensor(lse, torch.float32, (hq, n), "lse")
-    res = {"dq": _out_rows(out[0], q, (n, hq, d), "out[0]"),
-           "dk": _out_rows(out[1], q, (n, hk, d), "out[1]"),
-           "dv": _out_rows(out[2], q, (n, hk, d), "out[2]")}
+    dtype, dev, n, hq, hk, d, vq, vk, vv = _qkv(q, k, v)
+    batch, pr, scale, l, r = _attn_args(ranges, dev, left, right, sinks, scale, d)
+    vo = _rows(o, dtype, dev, (n, hq, d), "o")
+    vg = _rows(do, dtype, dev, (n, hq, d), "do")
+    pl = _vector(lse, torch.float32, dev, (hq, n), "lse")
+    dq, wq = _out_rows(out[0], q, (n, hq, d), "out[0]")
+    dk, wk = _out_rows(out[1], q, (n, hk, d), "out[1]")
+    dv, wv = _out_rows(out[2], q, (n, hk, d), "out[2]")
     if ws is None:
         ws = _bytes(lib().scn_attn_bwd_workspace_bytes(n, batch, d, hq, hk, l, sinks), q.device)
     _check(lib().scn_attn_bwd(
-        SCN_TYPE[q.dtype], n, batch, _ptr(ranges), d, hq, hk, _heads(q), _heads(k), _heads(v),
-        _heads(o), _ptr(lse), _heads(do), scale, l, r, sinks, _heads(res["dq"]),
-        _heads(res["dk"]), _heads(res["dv"]), _ptr(ws), ws.numel(),
-        ctypes.c_void_p(_stream())), "scn_attn_bwd")
-    return res
+        SCN_TYPE[dtype], n, batch, pr, d, hq, hk, _ref(vq), _ref(vk), _ref(vv), _ref(vo), pl,
+        _ref(vg), scale, l, r, sinks, _ref(wq), _ref(wk), _ref(wv), ws.data_ptr(), ws.numel(),
+        _raw_stream(dev)), "scn_attn_bwd")
+    return {"dq": dq, "dk": dk, "dv": dv}
 
 
 def attn_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor,
@@ -600,28 +649,23 @@ def attn_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_cache: torch.
     Hk, D] (capacity > sinks; the rows past the sinks are a ring); length int32
     [streams], the tokens written before.  Writes the new keys and values to the
     caches and returns o [streams, Hq, D]; the caller advances length."""
-    _head_rows(q, None, (None, None, None), "q")
-    b, hq, d = (int(x) for x in q.shape)
-    _head_rows(k, q, (b, None, d), "k")
-    hk = int(k.shape[1])
-    _head_rows(v, q, (b, hk, d), "v")
-    if hk < 1 or hq % hk:
-        raise ValueError(f"{hq} query heads cannot share {hk} key heads evenly")
-    _head_rows(k_cache, q, (b, None, hk, d), "k_cache")
-    cap = int(k_cache.shape[1])
-    _head_rows(v_cache, q, (b, cap, hk, d), "v_cache")
-    _dev_tensor(length, torch.int32, (b,), "length")
+    dtype, dev, b, hq, hk, d, vq, vk, vv = _qkv(q, k, v)
+    cap = k_cache.shape[1] if isinstance(k_cache, torch.Tensor) and k_cache.dim() == 4 else 0
+    ck = _cache(k_cache, dtype, dev, (b, cap, hk, d), "k_cache")
+    cv = _cache(v_cache, dtype, dev, (b, cap, hk, d), "v_cache")
+    pl = _vector(length, torch.int32, dev, (b,), "length")
     if not 0 <= sinks < cap:
         raise ValueError(f"sinks must lie in [0, capacity = {cap}), got {sinks}")
     l = _bound(left, "left")
-    scale = d ** -0.5 if scale is None else float(scale)
-    o = _out_rows(out, q, (b, hq, d), "out")
+    o, vo = _out_rows(out, q, (b, hq, d), "out")
     if ws is None:
-        ws = _bytes(lib().scn_attn_step_workspace_bytes(b, cap, d, hq, hk, l, sinks), q.device)
+        n = lib().scn_attn_step_workspace_bytes(b, cap, d, hq, hk, l, sinks)
+        ws = _bytes(n, q.device) if n else None
     _check(lib().scn_attn_step(
-        SCN_TYPE[q.dtype], b, cap, d, hq, hk, _heads(q), _heads(k), _heads(v), _cache(k_cache),
-        _cache(v_cache), _ptr(length), scale, l, int(sinks), _heads(o), _ptr(ws), ws.numel(),
-        ctypes.c_void_p(_stream())), "scn_attn_step")
+        SCN_TYPE[dtype], b, cap, d, hq, hk, _ref(vq), _ref(vk), _ref(vv), _ref(ck), _ref(cv), pl,
+        d ** -0.5 if scale is None else scale, l, sinks, _ref(vo),
+        None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(),
+        _raw_stream(dev)), "scn_attn_step")
     return o
 
 
