@@ -396,7 +396,7 @@ scn_status scn_maxpool_bwd(const scn_rulebook* rb, const uint8_t* argmax, const 
 
 /* Rows of heads: channel c of head h of row t at ((T*)p)[t*row + h*head + c].
  * p is a device pointer, 16-byte aligned; row and head are strides in elements,
- * multiples of 16 bytes.  The parts of a matrix that holds queries, keys and
+ * multiples of 16 bytes, row in [0, 2^22].  The parts of a matrix that holds queries, keys and
  * values side by side are such views. */
 typedef struct scn_heads {
   void* p;

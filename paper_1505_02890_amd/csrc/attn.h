@@ -76,10 +76,11 @@ __device__ inline Span find_span(const int32_t* ranges, int batch, int64_t n, in
   }
   Span s;
   s.sample = __builtin_amdgcn_readfirstlane(lo);
-  s.base = range_at(ranges, s.sample, n);
-  const int64_t end = range_at(ranges, s.sample + 1, n);
-  s.m = (int)max((int64_t)0, end - s.base);
-  const int64_t local = tile - (s.base / ROWS + s.sample);
+  const int base = __builtin_amdgcn_readfirstlane((int)range_at(ranges, s.sample, n));
+  const int end = __builtin_amdgcn_readfirstlane((int)range_at(ranges, s.sample + 1, n));
+  s.base = base;
+  s.m = max(0, end - base);
+  const int64_t local = tile - ((int64_t)base / ROWS + s.sample);
   s.first = local < 0 || local * ROWS >= s.m ? s.m : (int)(local * ROWS);
   return s;
 }
@@ -133,11 +134,20 @@ __device__ inline v16f zero16() {
   return z;
 }
 
-// value of the other half's lane n
-__device__ inline float other_half(float v) {
+// maximum, NaN if either is (v_maximum3_f32 takes two at a time; fmaxf would quiet each
+// operand first)
+__device__ inline float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
+// sum and maximum of the lanes n of both halves, in both
+__device__ inline float both_sum(float v) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false,
                                                   false);
-  return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ inline float both_larger(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false,
+                                                  false);
+  return larger(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
 // A tile of ROWS rows by DP channels in LDS: NS planes of bf16, rows of DP, in pieces
@@ -156,26 +166,40 @@ struct Tile {
   static __device__ inline int at(int row, int piece) {
     return row * (DP * 2) + ((piece ^ twist(row)) << 4);
   }
-  // rows r0 + n, channels 16 s + 8 h + 0..7
-  static __device__ inline Frag<NS> rows(const char* t, int r0, int s, int lane) {
-    Frag<NS> f;
-    const int o = at(r0 + (lane & 31), 2 * s + (lane >> 5));
+  // A lane's places in the tile, kept in registers: r[s] of rows n, channels
+  // 16 s + 8 h + 0..7; c[d] and c[d] + 8 rows of the transposed reads.
+  struct Lane {
+    int r[DP / 16], c[DP / 32][2];
+    __device__ inline Lane(int lane) {
 #pragma unroll
-    for (int p = 0; p < NS; ++p) f.s[p] = *reinterpret_cast<const v4u*>(t + p * PLANE + o);
+      for (int s = 0; s < DP / 16; ++s) r[s] = at(lane & 31, 2 * s + (lane >> 5));
+      const int row = ((lane >> 5) << 2) + ((lane & 15) >> 2);
+#pragma unroll
+      for (int d = 0; d < DP / 32; ++d) {
+        const int ch = d * 32 + ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
+        c[d][0] = at(row, ch >> 3) + (ch & 7) * 2;
+        c[d][1] = at(row + 8, ch >> 3) + (ch & 7) * 2;
+      }
+    }
+  };
+  // rows r0 + n, channels 16 s + 8 h + 0..7 (r0 a multiple of 32)
+  static __device__ inline Frag<NS> rows(const char* t, const Lane& l, int r0, int s) {
+    Frag<NS> f;
+#pragma unroll
+    for (int p = 0; p < NS; ++p)
+      f.s[p] = *reinterpret_cast<const v4u*>(t + l.r[s] + r0 * (DP * 2) + p * PLANE);
     return f;
   }
-  // channels 32 db + n along the operand's rows; its reduction over the tile's rows
-  // r0 + 8 (j / 4) + 4 h + j % 4
-  static __device__ inline Frag<NS> cols(char* t, int r0, int db, int lane) {
+  // channels 32 d + n along the operand's rows; its reduction over the tile's rows
+  // r0 + 8 (j / 4) + 4 h + j % 4 (r0 a multiple of 16)
+  static __device__ inline Frag<NS> cols(char* t, const Lane& l, int r0, int d) {
     Frag<NS> f;
-    const int r = r0 + ((lane >> 5) << 2) + ((lane & 15) >> 2);
-    const int c = db * 32 + ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
-    const int o0 = at(r, c >> 3) + (c & 7) * 2, o1 = at(r + 8, c >> 3) + (c & 7) * 2;
     typedef __attribute__((address_space(3))) v4s lds4;
 #pragma unroll
     for (int p = 0; p < NS; ++p) {
-      const v4s a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(t + p * PLANE + o0));
-      const v4s b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(t + p * PLANE + o1));
+      char* const o = t + r0 * (DP * 2) + p * PLANE;
+      const v4s a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(o + l.c[d][0]));
+      const v4s b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(o + l.c[d][1]));
       const v2u x = __builtin_bit_cast(v2u, a), y = __builtin_bit_cast(v2u, b);
       f.s[p] = v4u{x[0], x[1], y[0], y[1]};
     }
@@ -184,8 +208,9 @@ struct Tile {
 };
 
 // A tile on its way from memory to LDS, through registers of THREADS threads.  Rows past
-// the last are the last one's again (their products are masked); channels past D are
-// zero.
+// those that there are read as zero (the buffer's bounds), and pieces past channel D are
+// the row's first again: what they put into the tile is multiplied with the other
+// operand's zeros, or becomes channels past D of a result.
 template <int NS, int DP, int ROWS, int THREADS>
 struct Stage {
   typedef typename Elem<NS>::T T;
@@ -194,21 +219,31 @@ struct Stage {
   static constexpr int N = (ROWS * PIECES + THREADS - 1) / THREADS;
   static constexpr bool EVEN = ROWS * PIECES % THREADS == 0;
   v4u r[N];
-  __device__ inline void load(const T* p, int64_t stride, int row0, int last, int D, int tid) {
+  // `off`: where the thread's pieces lie, bytes from the tile's first row (rows lie at
+  // most 2^24 bytes apart)
+  static __device__ inline void places(uint32_t (&off)[N], int64_t stride, int D, int tid) {
 #pragma unroll
     for (int u = 0; u < N; ++u) {
-      const int x = tid + u * THREADS, row = min(row0 + x / PIECES, last), c = x % PIECES * EPP;
-      r[u] = v4u{0, 0, 0, 0};
-      if ((EVEN || x < ROWS * PIECES) && c < D)
-        r[u] = *reinterpret_cast<const v4u*>(p + row * stride + c);
+      const int y = tid + u * THREADS, c = y % PIECES * EPP;
+      off[u] = ((uint32_t)(y / PIECES % ROWS) * (uint32_t)stride + (c < D ? c : 0)) * sizeof(T);
     }
+  }
+  // up to `rows` >= 1 rows from row j of p (p, j and rows uniform)
+  __device__ inline void load(const T* p, int64_t stride, const uint32_t (&off)[N], int j, int rows,
+                              int D) {
+    T* const q = const_cast<T*>(p) + (uint64_t)(uint32_t)j * (uint32_t)stride;
+    const uint32_t bytes = ((uint32_t)(min(rows, ROWS) - 1) * (uint32_t)stride + D) * sizeof(T);
+    const __amdgpu_buffer_rsrc_t b = __builtin_amdgcn_make_buffer_rsrc(q, 0, (int)bytes, 0x00020000);
+#pragma unroll
+    for (int u = 0; u < N; ++u)
+      r[u] = __builtin_amdgcn_raw_buffer_load_b128(b, (int)off[u], 0, 0);
   }
   __device__ inline void store(char* t, int tid) const {
     typedef Tile<NS, DP, ROWS> L;
 #pragma unroll
     for (int u = 0; u < N; ++u) {
-      const int x = tid + u * THREADS, row = x / PIECES, c = x % PIECES;
-      if (!EVEN && x >= ROWS * PIECES) continue;
+      const int y = tid + u * THREADS, row = y / PIECES, c = y % PIECES;
+      if (!EVEN && y >= ROWS * PIECES) continue;
       if constexpr (NS == 1) {
         *reinterpret_cast<v4u*>(t + L::at(row, c)) = r[u];
       } else {

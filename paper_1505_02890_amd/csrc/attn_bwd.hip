@@ -12,7 +12,6 @@ namespace scn {
 namespace {
 
 constexpr int RB = 128;        // rows of a block (32 a wave)
-constexpr int TB = 64;         // rows of the tiles that stream past them
 constexpr int NT = 256;
 constexpr int SC = 1024;       // queries of a sink share
 constexpr int SPLIT_SINKS = 256;
@@ -112,11 +111,11 @@ __device__ inline void dkv_row(const BwdArgs<NS>& a, const Span& sp, int hk, int
   }
 }
 
-template <int NS, int DP>
+// NB blocks of 32 keys to a tile
+template <int NS, int DP, int NB>
 __global__ void __launch_bounds__(NT, NS == 3 && DP > 32 ? 1 : 2) attn_dq_kernel(BwdArgs<NS> a) {
-  typedef Tile<NS, DP, TB> L;
-  typedef Elem<NS> E;
-  constexpr int NBUF = NS == 1 ? 2 : 1;
+  constexpr int KT = 32 * NB;
+  typedef Tile<NS, DP, KT> L;
   extern __shared__ char smem[];
   const int tid = threadIdx.x, lane = tid & 63, n32 = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -139,12 +138,16 @@ __global__ void __launch_bounds__(NT, NS == 3 && DP > 32 ? 1 : 2) attn_dq_kernel
       Q[s] = load_frag<NS>(q, s, a.D, lane);
       G[s] = load_frag<NS>(g, s, a.D, lane);
       const int c = 16 * s + 8 * half;
-      if (c < a.D)
+      if (c < a.D) {
+        float x[8], y[8];
+        load8<NS>(g + c, x);
+        load8<NS>(o + c, y);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) delta = fmaf(E::get(g[c + j]), E::get(o[c + j]), delta);
+        for (int j = 0; j < 8; ++j) delta = fmaf(x[j], y[j], delta);
+      }
     }
   }
-  delta += other_half(delta);
+  delta = both_sum(delta);
   const int64_t at = h * a.n + sp.base + i;
   const float lse2 = a.lse[at] * LOG2E;
   if (mine && half == 0) a.delta[at] = delta;
@@ -152,68 +155,100 @@ __global__ void __launch_bounds__(NT, NS == 3 && DP > 32 ? 1 : 2) attn_dq_kernel
 #pragma unroll
   for (int d = 0; d < DP / 32; ++d) dQ[d] = zero16();
 
+  // the keys, as in the forward
   const int lo = a.w.lo(sp.first), hi = a.w.hi(min(sp.first + RB, sp.m) - 1, sp.m);
-  const int ns = min(a.w.sinks, lo), nst = (ns + TB - 1) / TB;
-  const int ntile = nst + (hi - lo + TB) / TB;
+  const int ns = min(a.w.sinks, lo), nst = (ns + KT - 1) / KT, nt = nst + (hi - lo + KT) / KT;
+  const int wl = lo < a.w.sinks ? lo : a.w.lo(i0), wh = a.w.hi(i1, sp.m);
+  const int al = a.w.lo(i0 + 31), ah = a.w.hi(i0, sp.m);
   const auto* const kp = a.k.p + sp.base * a.k.row + (h / a.group) * a.k.head;
   const auto* const vp = a.v.p + sp.base * a.v.row + (h / a.group) * a.v.head;
-  Stage<NS, DP, TB, NT> sk, sv;
+  typedef Stage<NS, DP, KT, NT> St;
+  St sk, sv;
+  uint32_t ko[St::N], vo[St::N];
+  St::places(ko, a.k.row, a.D, tid);
+  St::places(vo, a.v.row, a.D, tid);
+  const typename L::Lane pl(lane);
+  auto first_key = [&](int t) { return t < nst ? t * KT : lo + (t - nst) * KT; };
   auto fetch = [&](int t) {
-    const int j0 = t < nst ? t * TB : lo + (t - nst) * TB, last = t < nst ? ns - 1 : hi;
-    sk.load(kp, a.k.row, j0, last, a.D, tid);
-    sv.load(vp, a.v.row, j0, last, a.D, tid);
+    const int j = first_key(t), rows = (t < nst ? ns : hi + 1) - j;
+    sk.load(kp, a.k.row, ko, j, rows, a.D);
+    sv.load(vp, a.v.row, vo, j, rows, a.D);
   };
-  fetch(0);
-  sk.store(smem, tid);
-  sv.store(smem + L::BYTES, tid);
-  __syncthreads();
-  for (int t = 0; t < ntile; ++t) {
-    if (t + 1 < ntile) fetch(t + 1);
-    char* const kt = smem + (NBUF == 2 ? (t & 1) * 2 * L::BYTES : 0);
-    char* const vt = kt + L::BYTES;
+  auto put = [&](int t) {
+    sk.store(smem + (t & 1) * 2 * L::BYTES, tid);
+    sv.store(smem + (t & 1) * 2 * L::BYTES + L::BYTES, tid);
+  };
+  auto take = [&](int t) {
+    const int j0 = first_key(t);
     const bool sink = t < nst;
-    const int j0 = sink ? t * TB : lo + (t - nst) * TB, last = sink ? ns - 1 : hi;
-    const bool any = i0 <= i1 && j0 <= a.w.hi(i1, sp.m) &&
-                     (sink || j0 + TB > a.w.lo(i0) || j0 < a.w.sinks);
-    if (any) {
-      const bool all = j0 + TB - 1 <= last &&
-                       (sink || (j0 + TB - 1 <= i0 + a.w.right && j0 >= a.w.lo(i0 + 31)));
+    char* const kt = smem + (t & 1) * 2 * L::BYTES;
+    char* const vt = kt + L::BYTES;
+    v16f S[NB], P[NB];
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        v16f S = zero16(), P = zero16();
+    for (int b = 0; b < NB; ++b) {
+      S[b] = zero16();
+      P[b] = zero16();
 #pragma unroll
-        for (int s = 0; s < DP / 16; ++s) {
-          S = mma<NS>(L::rows(kt, 32 * b, s, lane), Q[s], S);
-          P = mma<NS>(L::rows(vt, 32 * b, s, lane), G[s], P);
-        }
+      for (int s = 0; s < DP / 16; ++s) S[b] = mma<NS>(L::rows(kt, pl, 32 * b, s), Q[s], S[b]);
+#pragma unroll
+      for (int s = 0; s < DP / 16; ++s) P[b] = mma<NS>(L::rows(vt, pl, 32 * b, s), G[s], P[b]);
+    }
+    if (sink ? j0 + 32 * NB > ns : j0 < al || j0 + 32 * NB - 1 > ah) {
+      const int l = (sink ? 0 : a.w.lo(i)) - j0 - 4 * half;
+      const int u = (sink ? ns - 1 : a.w.hi(i, sp.m)) - j0 - 4 * half;
+      const int z = (sink ? 0 : a.w.sinks - j0) - 4 * half;
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          float p = __builtin_amdgcn_exp2f(fmaf(S[r], c2, -lse2));
-          if (!all) {
-            const int j = j0 + 32 * b + 8 * (r / 4) + 4 * half + r % 4;
-            if (!(j <= last && (sink || a.w.sees(i, j)))) p = 0.f;
-          }
-          S[r] = p * (P[r] - delta);
+          const int e = 32 * b + 8 * (r / 4) + r % 4;
+          S[b][r] = ((e <= u) & ((e >= l) | (e < z))) ? S[b][r] : -INFINITY;
         }
+    }
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          float x[8];
+    for (int b = 0; b < NB; ++b) {
 #pragma unroll
-          for (int j = 0; j < 8; ++j) x[j] = S[8 * s + j];
-          const Frag<NS> X = to_frag<NS>(x);
+      for (int r = 0; r < 16; ++r)
+        S[b][r] = __builtin_amdgcn_exp2f(fmaf(S[b][r], c2, -lse2)) * (P[b][r] - delta);
 #pragma unroll
-          for (int d = 0; d < DP / 32; ++d)
-            dQ[d] = mma<NS>(L::cols(kt, 32 * b + 16 * s, d, lane), X, dQ[d]);
-        }
+      for (int s = 0; s < 2; ++s) {
+        float x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = S[b][8 * s + j];
+        const Frag<NS> X = to_frag<NS>(x);
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d)
+          dQ[d] = mma<NS>(L::cols(kt, pl, 32 * b + 16 * s, d), X, dQ[d]);
       }
     }
-    if (t + 1 < ntile) {
-      if (NBUF == 1) __syncthreads();
-      char* const nx = smem + (NBUF == 2 ? ((t & 1) ^ 1) * 2 * L::BYTES : 0);
-      sk.store(nx, tid);
-      sv.store(nx + L::BYTES, tid);
+  };
+  auto pass = [&](int t) {
+    if (t + 1 < nt) put(t + 1);
+    if (t + 2 < nt) fetch(t + 2);
+  };
+  auto place = [&](int x) { return nst + max(0, x) / KT; };
+  const int e0 = i0 <= i1 ? nst : 0;
+  const int s1 = i0 <= i1 ? place(wl - lo) : nt, e1 = i0 <= i1 ? place(wh - lo) + 1 : nt;
+  fetch(0);
+  put(0);
+  if (nt > 1) fetch(1);
+  __syncthreads();
+  int t = 0;
+  for (int seg = 0; seg < 2; ++seg) {
+    const int s = seg ? s1 : 0, e = seg ? e1 : e0;
+    for (; t < s; ++t) {
+      pass(t);
       __syncthreads();
     }
+    for (; t < e; ++t) {
+      pass(t);
+      take(t);
+      __syncthreads();
+    }
+  }
+  for (; t < nt; ++t) {
+    pass(t);
+    __syncthreads();
   }
   bool fine = true;
 #pragma unroll
@@ -234,8 +269,9 @@ __global__ void __launch_bounds__(NT, NS == 3 && DP > 32 ? 1 : 2) attn_dq_kernel
 
 // What a wave with 32 keys does with 32 queries of a tile: dV += P^T dO, dK += dS^T Q
 // (transposed).  see(i, j) masks the pairs of query i0 + row and key j if `mask`.
-template <int NS, int DP, class See>
-__device__ inline void key_block(char* qt, char* gt, const float* lse2, const float* delta, int r0,
+template <int NS, int DP, int TB, class See>
+__device__ inline void key_block(char* qt, char* gt, const typename Tile<NS, DP, TB>::Lane& pl,
+                                 const float* lse2, const float* delta, int r0,
                                  const Frag<NS> (&K)[DP / 16], const Frag<NS> (&V)[DP / 16],
                                  float c2, bool mask, const See& see, v16f (&dK)[DP / 32],
                                  v16f (&dV)[DP / 32]) {
@@ -244,8 +280,13 @@ __device__ inline void key_block(char* qt, char* gt, const float* lse2, const fl
   v16f S = zero16(), P = zero16();
 #pragma unroll
   for (int s = 0; s < DP / 16; ++s) {
-    S = mma<NS>(L::rows(qt, r0, s, lane), K[s], S);
-    P = mma<NS>(L::rows(gt, r0, s, lane), V[s], P);
+    S = mma<NS>(L::rows(qt, pl, r0, s), K[s], S);
+    P = mma<NS>(L::rows(gt, pl, r0, s), V[s], P);
+  }
+  if (mask) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+      S[r] = see(r0 + 8 * (r / 4) + 4 * half + r % 4) ? S[r] : -INFINITY;
   }
 #pragma unroll
   for (int g = 0; g < 4; ++g) {
@@ -254,10 +295,8 @@ __device__ inline void key_block(char* qt, char* gt, const float* lse2, const fl
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int r = 4 * g + j;
-      float p = __builtin_amdgcn_exp2f(fmaf(S[r], c2, -l[j]));
-      if (mask && !see(r0 + 8 * g + 4 * half + j)) p = 0.f;
-      S[r] = p;
-      P[r] = p * (P[r] - e[j]);
+      S[r] = __builtin_amdgcn_exp2f(fmaf(S[r], c2, -l[j]));
+      P[r] = S[r] * (P[r] - e[j]);
     }
   }
 #pragma unroll
@@ -271,23 +310,29 @@ __device__ inline void key_block(char* qt, char* gt, const float* lse2, const fl
     const Frag<NS> X = to_frag<NS>(x), Y = to_frag<NS>(y);
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d) {
-      dV[d] = mma<NS>(L::cols(gt, r0 + 16 * s, d, lane), X, dV[d]);
-      dK[d] = mma<NS>(L::cols(qt, r0 + 16 * s, d, lane), Y, dK[d]);
+      dV[d] = mma<NS>(L::cols(gt, pl, r0 + 16 * s, d), X, dV[d]);
+      dK[d] = mma<NS>(L::cols(qt, pl, r0 + 16 * s, d), Y, dK[d]);
     }
   }
 }
 
 // The tiles of queries that stream past a block's keys, over its query heads
-template <int NS, int DP, int THREADS>
+template <int NS, int DP, int TB, int THREADS>
 struct QueryTiles {
   typedef Tile<NS, DP, TB> L;
   static constexpr int BUF = 2 * L::BYTES + 2 * TB * 4;
-  Stage<NS, DP, TB, THREADS> q, g;
+  typedef Stage<NS, DP, TB, THREADS> St;
+  St q, g;
+  uint32_t qo[St::N], go[St::N];
   float lse2, delta;
+  __device__ inline void init(const BwdArgs<NS>& a, int tid) {
+    St::places(qo, a.q.row, a.D, tid);
+    St::places(go, a.d_o.row, a.D, tid);
+  }
   __device__ inline void fetch(const BwdArgs<NS>& a, const Span& sp, int h, int i0, int last,
                                int tid) {
-    q.load(a.q.p + sp.base * a.q.row + h * a.q.head, a.q.row, i0, last, a.D, tid);
-    g.load(a.d_o.p + sp.base * a.d_o.row + h * a.d_o.head, a.d_o.row, i0, last, a.D, tid);
+    q.load(a.q.p + sp.base * a.q.row + h * a.q.head, a.q.row, qo, i0, last + 1 - i0, a.D);
+    g.load(a.d_o.p + sp.base * a.d_o.row + h * a.d_o.head, a.d_o.row, go, i0, last + 1 - i0, a.D);
     if (tid < TB) {
       const int64_t at = h * a.n + sp.base + min(i0 + tid, last);
       lse2 = a.lse[at] * LOG2E;
@@ -310,7 +355,8 @@ struct QueryTiles {
 // block (chunk, sink tile of 32, key head), two waves with 32 queries of each tile.
 template <int NS, int DP>
 __global__ void __launch_bounds__(128, 1) attn_sink_kernel(BwdArgs<NS> a, int nst) {
-  typedef QueryTiles<NS, DP, 128> QT;
+  constexpr int TB = 64;
+  typedef QueryTiles<NS, DP, TB, 128> QT;
   typedef typename QT::L L;
   extern __shared__ char smem[];
   const int tid = threadIdx.x, lane = tid & 63, n32 = lane & 31, half = lane >> 5;
@@ -334,6 +380,8 @@ __global__ void __launch_bounds__(128, 1) attn_sink_kernel(BwdArgs<NS> a, int ns
 #pragma unroll
   for (int d = 0; d < DP / 32; ++d) dK[d] = dV[d] = zero16();
   QT st;
+  st.init(a, tid);
+  const typename L::Lane pl(lane);
   const int per = (end - first + TB) / TB, ntile = per * a.group;
   st.fetch(a, sp, hk * a.group, first, end, tid);
   for (int t = 0; t < ntile; ++t) {
@@ -343,8 +391,8 @@ __global__ void __launch_bounds__(128, 1) attn_sink_kernel(BwdArgs<NS> a, int ns
     if (t + 1 < ntile)
       st.fetch(a, sp, hk * a.group + (t + 1) / per, first + (t + 1) % per * TB, end, tid);
     const float* const f = reinterpret_cast<const float*>(smem + 2 * L::BYTES);
-    auto see = [&](int r) { return i0 + r <= end && j < i0 + r - a.w.left; };
-    key_block<NS, DP>(smem, smem + L::BYTES, f, f + TB, 32 * wave, K, V, c2, true, see, dK, dV);
+    auto see = [&](int r) { return (i0 + r <= end) & (j < i0 + r - a.w.left); };
+    key_block<NS, DP, TB>(smem, smem + L::BYTES, pl, f, f + TB, 32 * wave, K, V, c2, true, see, dK, dV);
     __syncthreads();
   }
   // the second wave's sums through LDS, then out
@@ -373,11 +421,10 @@ __global__ void __launch_bounds__(128, 1) attn_sink_kernel(BwdArgs<NS> a, int ns
     }
 }
 
-template <int NS, int DP>
+template <int NS, int DP, int TB>
 __global__ void __launch_bounds__(NT, NS == 3 || DP > 64 ? 1 : 2) attn_dkv_kernel(BwdArgs<NS> a) {
-  typedef QueryTiles<NS, DP, NT> QT;
+  typedef QueryTiles<NS, DP, TB, NT> QT;
   typedef typename QT::L L;
-  constexpr int NBUF = NS == 1 ? 2 : 1;
   extern __shared__ char smem[];
   const int tid = threadIdx.x, lane = tid & 63, n32 = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -406,32 +453,49 @@ __global__ void __launch_bounds__(NT, NS == 3 || DP > 64 ? 1 : 2) attn_dkv_kerne
                                    : min(sp.m - 1, min(sp.first + RB, sp.m) - 1 + w.left);
   const int per = (end - first + TB) / TB, ntile = per * a.group;
   QT st;
+  st.init(a, tid);
+  const typename L::Lane pl(lane);
   auto fetch = [&](int t) {
     st.fetch(a, sp, hk * a.group + t / per, first + t % per * TB, end, tid);
   };
+  auto put = [&](int t) { st.store(smem + (t & 1) * QT::BUF, tid); };
+  auto pass = [&](int t) {
+    if (t + 1 < ntile) put(t + 1);
+    if (t + 2 < ntile) fetch(t + 2);
+  };
+  // The wave takes the tiles [s, e) of each query head: the queries that see one of its
+  // keys.
+  const int ql = max(0, j0 - w.right) - first;
+  const int qh = (j0 < sinks ? sp.m - 1 : min(sp.m - 1, j1 + w.left)) - first;
+  const int s = j0 <= j1 ? max(0, ql) / TB : per, e = j0 <= j1 ? min(per, qh / TB + 1) : per;
   fetch(0);
-  st.store(smem, tid);
+  put(0);
+  if (ntile > 1) fetch(1);
   __syncthreads();
-  for (int t = 0; t < ntile; ++t) {
-    if (t + 1 < ntile) fetch(t + 1);
-    char* const b = smem + (NBUF == 2 ? (t & 1) * QT::BUF : 0);
-    const float* const f = reinterpret_cast<const float*>(b + 2 * L::BYTES);
-#pragma unroll
-    for (int u = 0; u < TB / 32; ++u) {
-      const int i0 = first + t % per * TB + 32 * u, i1 = i0 + 31;
-      const bool any = j0 <= j1 && i0 <= end && j0 <= i1 + w.right &&
-                       (j1 >= i0 - w.left || j0 < sinks);
-      const bool all = i1 <= end && j0 + 31 <= i0 + w.right && j0 >= i1 - w.left;
-      auto see = [&](int r) {
-        const int i = i0 - 32 * u + r;
-        return i <= end && w.sees(i, j);
-      };
-      if (any)
-        key_block<NS, DP>(b, b + L::BYTES, f, f + TB, 32 * u, K, V, c2, !all, see, dK, dV);
+  for (int t = 0; t < ntile;) {
+    const int t0 = t;
+    for (; t < t0 + s; ++t) {
+      pass(t);
+      __syncthreads();
     }
-    if (t + 1 < ntile) {
-      if (NBUF == 1) __syncthreads();
-      st.store(smem + (NBUF == 2 ? ((t & 1) ^ 1) * QT::BUF : 0), tid);
+    for (; t < t0 + e; ++t) {
+      pass(t);
+      char* const b = smem + (t & 1) * QT::BUF;
+      const float* const f = reinterpret_cast<const float*>(b + 2 * L::BYTES);
+#pragma unroll
+      for (int u = 0; u < TB / 32; ++u) {
+        const int i0 = first + (t - t0) * TB + 32 * u, i1 = i0 + 31;
+        const bool all = i1 <= end && j0 + 31 <= i0 + w.right && j0 >= i1 - w.left;
+        auto see = [&](int r) {
+          const int i = i0 - 32 * u + r;
+          return (i <= end) & (j <= i + w.right) & ((j >= i - w.left) | (j < sinks));
+        };
+        key_block<NS, DP, TB>(b, b + L::BYTES, pl, f, f + TB, 32 * u, K, V, c2, !all, see, dK, dV);
+      }
+      __syncthreads();
+    }
+    for (; t < t0 + per; ++t) {
+      pass(t);
       __syncthreads();
     }
   }
@@ -496,24 +560,26 @@ scn_status launch(const BwdArgs<NS>& a, hipStream_t st) {
     return SCN_ERR_OVERFLOW;
   }
   {
-    constexpr size_t smem = (NS == 1 ? 4 : 2) * Tile<NS, DP, TB>::BYTES;
+    constexpr int NB = NS == 1 && DP <= 64 ? 2 : 1;
+    constexpr size_t smem = 4 * Tile<NS, DP, 32 * NB>::BYTES;
     static LdsLimit limit;
-    auto fn = attn_dq_kernel<NS, DP>;
+    auto fn = attn_dq_kernel<NS, DP, NB>;
     if (scn_status rc = allow_lds(reinterpret_cast<const void*>(fn), limit, smem)) return rc;
     hipLaunchKernelGGL(fn, dim3((unsigned)(tiles * a.Hq)), dim3(NT), smem, st, a);
     SCN_LAUNCH_CHECK();
   }
   if (a.share) {
-    constexpr size_t smem = std::max<size_t>(QueryTiles<NS, DP, 128>::BUF, DP * 2 * 32 * 4);
+    constexpr size_t smem = std::max<size_t>(QueryTiles<NS, DP, 64, 128>::BUF, DP * 2 * 32 * 4);
     static LdsLimit limit;
     auto fn = attn_sink_kernel<NS, DP>;
     if (scn_status rc = allow_lds(reinterpret_cast<const void*>(fn), limit, smem)) return rc;
     hipLaunchKernelGGL(fn, dim3((unsigned)shares), dim3(128), smem, st, a, nst);
     SCN_LAUNCH_CHECK();
   }
-  constexpr size_t smem = (NS == 1 ? 2 : 1) * QueryTiles<NS, DP, NT>::BUF;
+  constexpr int TB = NS == 1 ? 64 : 32;  // (split tiles are three times as large)
+  constexpr size_t smem = 2 * QueryTiles<NS, DP, TB, NT>::BUF;
   static LdsLimit limit;
-  auto fn = attn_dkv_kernel<NS, DP>;
+  auto fn = attn_dkv_kernel<NS, DP, TB>;
   if (scn_status rc = allow_lds(reinterpret_cast<const void*>(fn), limit, smem)) return rc;
   hipLaunchKernelGGL(fn, dim3((unsigned)(tiles * a.Hk)), dim3(NT), smem, st, a);
   SCN_LAUNCH_CHECK();

@@ -7,13 +7,12 @@
 // (its keys along the registers), so the maximum and the sum stay in the lane but for
 // one exchange with the other half, and P^T goes on into O^T += V^T P^T as it is.
 #include <cmath>
+#include <type_traits>
 
 #include "attn.h"
 
 namespace scn {
 namespace {
-
-constexpr int QB = 128, KB = 64, NT = 256;
 
 template <int NS>
 struct FwdArgs {
@@ -67,18 +66,32 @@ __device__ inline void fwd_row(const FwdArgs<NS>& a, const Span& sp, int h, int 
   if (a.lse && lane == 0) a.lse[h * a.n + sp.base + i] = top + logf(sum);
 }
 
-template <int NS, int DP>
-__global__ void __launch_bounds__(NT, NS == 3 && DP > 64 ? 1 : 2) attn_fwd_kernel(FwdArgs<NS> a) {
-  typedef Tile<NS, DP, KB> L;
-  constexpr int NBUF = NS == 1 ? 2 : 1;  // split tiles are three times as large
+// QW waves of 32 queries by KW groups that share out the keys of a tile, 32 NB each
+template <int NS, int DP, int QW_, int KW_, int NB_>
+struct Shape {
+  static constexpr int QW = QW_, KW = KW_, NB = NB_, QB = 32 * QW, NT = 64 * QW * KW;
+  static constexpr int KT = 32 * NB * KW;
+  typedef Tile<NS, DP, KT> L;
+  static constexpr int BUF = 2 * L::BYTES;       // keys and values
+  static constexpr int JOIN = DP / 32 * 16 + 2;  // floats a lane hands over
+  static constexpr size_t SMEM = std::max<size_t>(2 * BUF, (size_t)QW * (KW - 1) * JOIN * 256);
+};
+
+template <int NS, int DP, int QW, int KW, int NB>
+__global__ void __launch_bounds__(64 * QW * KW, NS == 3 && DP > 64 ? 1 : 2)
+    attn_fwd_kernel(FwdArgs<NS> a) {
+  typedef Shape<NS, DP, QW, KW, NB> X;
+  typedef typename X::L L;
+  constexpr int QB = X::QB, KT = X::KT, NT = X::NT;
   extern __shared__ char smem[];
   const int tid = threadIdx.x, lane = tid & 63, n32 = lane & 31, half = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), kw = wave / QW;
   const int h = blockIdx.x % a.Hq;
   const Span sp = find_span<QB>(a.ranges, a.batch, a.n, blockIdx.x / a.Hq);
   if (sp.first >= sp.m) return;
-  const int i0 = sp.first + wave * 32, i1 = min(i0 + 31, sp.m - 1);  // the wave's queries
-  const int i = min(i0 + n32, sp.m - 1);                             // the lane's
+  // the wave's queries (i1 < i0 past the sample's rows) and the lane's
+  const int i0 = sp.first + wave % QW * 32, i1 = min(i0 + 31, sp.m - 1);
+  const int i = min(i0 + n32, sp.m - 1);
   const float c2 = a.scale * LOG2E;
 
   Frag<NS> Q[DP / 16];
@@ -90,98 +103,194 @@ __global__ void __launch_bounds__(NT, NS == 3 && DP > 64 ? 1 : 2) attn_fwd_kerne
   v16f O[DP / 32];
 #pragma unroll
   for (int d = 0; d < DP / 32; ++d) O[d] = zero16();
-  float top = -INFINITY, sum = 0.f;  // sum: of this half's keys
+  // The maximum of the scores (log 2) and the sum, of this half's keys.  The maximum
+  // moves only when a score passes it by 2^8 (`limit`, unscaled): until then the terms
+  // stay below 2^8 and the sums far from fp32's range.
+  float top = -INFINITY, base = 0.f, limit = -INFINITY, sum = 0.f;
 
-  // the block's keys: the sinks [0, ns), then the window [lo, hi]
+  // The block's keys: the sinks [0, ns), then the window [lo, hi], in tiles of KT; and
+  // what some query of the wave and all of them see of the window
   const int lo = a.w.lo(sp.first), hi = a.w.hi(min(sp.first + QB, sp.m) - 1, sp.m);
-  const int ns = min(a.w.sinks, lo), nst = (ns + KB - 1) / KB;
-  const int ntile = nst + (hi - lo + KB) / KB;
+  const int ns = min(a.w.sinks, lo), nst = (ns + KT - 1) / KT, nt = nst + (hi - lo + KT) / KT;
+  const int wl = lo < a.w.sinks ? lo : a.w.lo(i0), wh = a.w.hi(i1, sp.m);
+  const int al = a.w.lo(i0 + 31), ah = a.w.hi(i0, sp.m);
   const auto* const kp = a.k.p + sp.base * a.k.row + (h / a.group) * a.k.head;
   const auto* const vp = a.v.p + sp.base * a.v.row + (h / a.group) * a.v.head;
-  Stage<NS, DP, KB, NT> sk, sv;
+  typedef Stage<NS, DP, KT, NT> St;
+  St sk, sv;
+  uint32_t ko[St::N], vo[St::N];
+  St::places(ko, a.k.row, a.D, tid);
+  St::places(vo, a.v.row, a.D, tid);
+  const typename L::Lane at(lane);
+  auto first_key = [&](int t) { return t < nst ? t * KT : lo + (t - nst) * KT; };
   auto fetch = [&](int t) {
-    const int j0 = t < nst ? t * KB : lo + (t - nst) * KB, last = t < nst ? ns - 1 : hi;
-    sk.load(kp, a.k.row, j0, last, a.D, tid);
-    sv.load(vp, a.v.row, j0, last, a.D, tid);
+    const int j = first_key(t), rows = (t < nst ? ns : hi + 1) - j;
+    sk.load(kp, a.k.row, ko, j, rows, a.D);
+    sv.load(vp, a.v.row, vo, j, rows, a.D);
   };
-  fetch(0);
-  sk.store(smem, tid);
-  sv.store(smem + L::BYTES, tid);
-  __syncthreads();
-  for (int t = 0; t < ntile; ++t) {
-    if (t + 1 < ntile) fetch(t + 1);
-    char* const kt = smem + (NBUF == 2 ? (t & 1) * 2 * L::BYTES : 0);
-    char* const vt = kt + L::BYTES;
+  auto put = [&](int t) {
+    sk.store(smem + (t & 1) * X::BUF, tid);
+    sv.store(smem + (t & 1) * X::BUF + L::BYTES, tid);
+  };
+  // the wave's keys of tile t
+  auto take = [&](int t) {
+    constexpr int M = NB;
+    const int j0 = first_key(t) + kw * 32 * NB;
     const bool sink = t < nst;
-    const int j0 = sink ? t * KB : lo + (t - nst) * KB, last = sink ? ns - 1 : hi;
-    // (a wave past the sample's rows has i1 < i0: nothing)
-    const bool any = i0 <= i1 && j0 <= a.w.hi(i1, sp.m) &&
-                     (sink || j0 + KB > a.w.lo(i0) || j0 < a.w.sinks);
-    if (any) {
-      const bool all = j0 + KB - 1 <= last &&
-                       (sink || (j0 + KB - 1 <= i0 + a.w.right && j0 >= a.w.lo(i0 + 31)));
-      v16f S[2];
+    char* const kt = smem + (t & 1) * X::BUF + kw * 32 * NB * DP * 2;
+    char* const vt = kt + L::BYTES;
+    constexpr bool EARLY = NS == 1 || DP == 32;  // values read before they are needed
+    Frag<NS> V[M][2][DP / 32];
+    v16f S[M];
+    {
+      Frag<NS> K[M][DP / 16];
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
+      for (int b = 0; b < M; ++b)
+#pragma unroll
+        for (int s = 0; s < DP / 16; ++s) K[b][s] = L::rows(kt, at, 32 * b, s);
+      if constexpr (EARLY) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+          for (int d = 0; d < DP / 32; ++d) V[0][s][d] = L::cols(vt, at, 16 * s, d);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int b = 0; b < M; ++b) {
         S[b] = zero16();
 #pragma unroll
-        for (int s = 0; s < DP / 16; ++s) S[b] = mma<NS>(L::rows(kt, 32 * b, s, lane), Q[s], S[b]);
+        for (int s = 0; s < DP / 16; ++s) S[b] = mma<NS>(K[b][s], Q[s], S[b]);
       }
-      if (!all) {
+    }
+    if (sink ? j0 + 32 * M > ns : j0 < al || j0 + 32 * M - 1 > ah) {
+      const int l = (sink ? 0 : a.w.lo(i)) - j0 - 4 * half;
+      const int u = (sink ? ns - 1 : a.w.hi(i, sp.m)) - j0 - 4 * half;
+      const int z = a.w.sinks - j0 - 4 * half;
+      if (sink || j0 >= a.w.sinks) {
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+        for (int b = 0; b < M; ++b)
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
-            const int j = j0 + 32 * b + 8 * (r / 4) + 4 * half + r % 4;
-            if (!(j <= last && (sink || a.w.sees(i, j)))) S[b][r] = -INFINITY;
+            const int e = 32 * b + 8 * (r / 4) + r % 4;
+            S[b][r] = ((e >= l) & (e <= u)) ? S[b][r] : -INFINITY;
+          }
+      } else {
+#pragma unroll
+        for (int b = 0; b < M; ++b)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int e = 32 * b + 8 * (r / 4) + r % 4;
+            S[b][r] = ((e <= u) & ((e >= l) | (e < z))) ? S[b][r] : -INFINITY;
           }
       }
-      float mx = S[0][0];
+    }
+    float mx[M];
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
+    for (int b = 0; b < M; ++b) {
+      mx[b] = larger(S[b][0], S[b][1]);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, S[b][r]);
-      mx = fmaxf(mx, other_half(mx)) * c2;
-      // The maximum moves only when a score passes it by 2^8: until then the terms
-      // stay below 2^8 and the sums far from fp32's range.
-      if (__ballot(mx > top + 8.f)) {
-        const float now = fmaxf(top, mx);
-        const float f = now == top ? 1.f : exp2f(top - now);
-        top = now;
-        sum *= f;
+      for (int r = 2; r < 16; ++r) mx[b] = larger(mx[b], S[b][r]);
+    }
+    const float m = both_larger(M == 2 ? larger(mx[0], mx[M - 1]) : mx[0]);
+    if (__ballot(m > limit)) {
+      const float now = fmaxf(top, m * c2);
+      const float f = now == top ? 1.f : __builtin_amdgcn_exp2f(top - now);
+      top = now;
+      base = now == -INFINITY ? 0.f : now;
+      limit = (now + 8.f) / c2;
+      sum *= f;
 #pragma unroll
-        for (int d = 0; d < DP / 32; ++d)
+      for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) O[d][r] *= f;
-      }
-      const float base = top == -INFINITY ? 0.f : top;
+        for (int r = 0; r < 16; ++r) O[d][r] *= f;
+    }
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
+    for (int b = 0; b < M; ++b) {
+      if constexpr (EARLY && M == 2)
+        if (b == 1) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          S[b][r] = __builtin_amdgcn_exp2f(fmaf(S[b][r], c2, -base));
-          sum += S[b][r];
+          for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int d = 0; d < DP / 32; ++d) V[1][s][d] = L::cols(vt, at, 32 + 16 * s, d);
         }
 #pragma unroll
-      for (int s = 0; s < 4; ++s) {
+      for (int r = 0; r < 16; ++r) {
+        S[b][r] = __builtin_amdgcn_exp2f(fmaf(S[b][r], c2, -base));
+        sum += S[b][r];
+      }
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
         float p[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) p[j] = S[s / 2][8 * (s & 1) + j];
+        for (int j = 0; j < 8; ++j) p[j] = S[b][8 * s + j];
         const Frag<NS> P = to_frag<NS>(p);
 #pragma unroll
         for (int d = 0; d < DP / 32; ++d)
-          O[d] = mma<NS>(L::cols(vt, 16 * s, d, lane), P, O[d]);
+          O[d] = mma<NS>(EARLY ? V[b][s][d] : L::cols(vt, at, 32 * b + 16 * s, d), P, O[d]);
       }
     }
-    if (t + 1 < ntile) {
-      if (NBUF == 1) __syncthreads();
-      char* const nx = smem + (NBUF == 2 ? ((t & 1) ^ 1) * 2 * L::BYTES : 0);
-      sk.store(nx, tid);
-      sv.store(nx + L::BYTES, tid);
+  };
+  // While a tile is taken, the next one goes from registers to the other buffer and the
+  // one after that is loaded.
+  auto pass = [&](int t) {
+    if (t + 1 < nt) put(t + 1);
+    if (t + 2 < nt) fetch(t + 2);
+  };
+  // The wave takes the tiles [0, e0) of sinks and [s1, e1) of its window, and passes the
+  // others on.  (A branch round `take` would have the sums copied at its end.)
+  auto place = [&](int x) { return nst + max(0, x - kw * 32 * NB) / KT; };
+  const int some = i0 <= i1 && wh - lo >= kw * 32 * NB;  // if it sees any of its window's keys
+  const int e0 = i0 <= i1 ? nst : 0;
+  const int s1 = some ? place(wl - lo) : nt, e1 = some ? place(wh - lo) + 1 : nt;
+  fetch(0);
+  put(0);
+  if (nt > 1) fetch(1);
+  __syncthreads();
+  int t = 0;
+  for (int seg = 0; seg < 2; ++seg) {
+    const int s = seg ? s1 : 0, e = seg ? e1 : e0;
+    for (; t < s; ++t) {
+      pass(t);
+      __syncthreads();
+    }
+    for (; t < e; ++t) {
+      pass(t);
+      take(t);
       __syncthreads();
     }
   }
-  sum += other_half(sum);
+  for (; t < nt; ++t) {
+    pass(t);
+    __syncthreads();
+  }
+  sum = both_sum(sum);
+  if constexpr (KW > 1) {
+    // the groups' shares of the keys, joined in order
+    float* const x = reinterpret_cast<float*>(smem) + lane;
+    if (kw > 0) {
+      float* const o = x + (wave - QW) * X::JOIN * 64;
+#pragma unroll
+      for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[(d * 16 + r) * 64] = O[d][r];
+      o[(X::JOIN - 2) * 64] = top;
+      o[(X::JOIN - 1) * 64] = sum;
+    }
+    __syncthreads();
+    if (kw > 0) return;
+    for (int g = 1; g < KW; ++g) {
+      const float* const o = x + ((g - 1) * QW + wave) * X::JOIN * 64;
+      const float top2 = o[(X::JOIN - 2) * 64], now = fmaxf(top, top2);
+      const float base = now == -INFINITY ? 0.f : now;
+      const float f = __builtin_amdgcn_exp2f(top - base), f2 = __builtin_amdgcn_exp2f(top2 - base);
+      top = now;
+      sum = sum * f + o[(X::JOIN - 1) * 64] * f2;
+#pragma unroll
+      for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) O[d][r] = O[d][r] * f + o[(d * 16 + r) * 64] * f2;
+    }
+  }
   const float inv = 1.f / sum;
   bool fine = fabsf(top) < INFINITY && sum < INFINITY;
 #pragma unroll
@@ -203,20 +312,34 @@ __global__ void __launch_bounds__(NT, NS == 3 && DP > 64 ? 1 : 2) attn_fwd_kerne
   }
 }
 
-template <int NS, int DP>
+template <int NS, int DP, int QW, int KW, int NB>
 scn_status launch(const FwdArgs<NS>& a, hipStream_t st) {
-  constexpr size_t smem = (NS == 1 ? 4 : 2) * Tile<NS, DP, KB>::BYTES;
+  typedef Shape<NS, DP, QW, KW, NB> X;
   static LdsLimit limit;
-  auto fn = attn_fwd_kernel<NS, DP>;
-  if (scn_status rc = allow_lds(reinterpret_cast<const void*>(fn), limit, smem)) return rc;
-  const int64_t blocks = (a.n / QB + a.batch) * a.Hq;
+  auto fn = attn_fwd_kernel<NS, DP, QW, KW, NB>;
+  if (scn_status rc = allow_lds(reinterpret_cast<const void*>(fn), limit, X::SMEM)) return rc;
+  const int64_t blocks = (a.n / X::QB + a.batch) * a.Hq;
   if (blocks > INT32_MAX) {
     set_error("scn_attn_fwd: more than 2^31 blocks of rows and heads");
     return SCN_ERR_OVERFLOW;
   }
-  hipLaunchKernelGGL(fn, dim3((unsigned)blocks), dim3(NT), smem, st, a);
+  hipLaunchKernelGGL(fn, dim3((unsigned)blocks), dim3(X::NT), X::SMEM, st, a);
   SCN_LAUNCH_CHECK();
   return SCN_OK;
+}
+
+template <int NS, int DP>
+scn_status launch(const FwdArgs<NS>& a, hipStream_t st) {
+  const int64_t blocks = (a.n / 128 + a.batch) * a.Hq;
+  if constexpr (NS == 1 && DP <= 64) {
+    if (blocks < 512) return launch<NS, DP, 2, 2, 2>(a, st);
+    if constexpr (DP <= 32) return launch<NS, DP, 2, 1, 1>(a, st);
+    return launch<NS, DP, 4, 1, 2>(a, st);
+  } else {
+    if constexpr (NS == 1 || DP <= 64)
+      if (blocks < 512 || (NS == 3 && DP == 64)) return launch<NS, DP, 4, 2, 1>(a, st);
+    return launch<NS, DP, 4, 1, 1>(a, st);
+  }
 }
 
 template <int NS>

@@ -23,6 +23,10 @@ scn_status check_heads(const char* who, const char* name, const scn_heads* h, in
     set_error("%s: %s must be 16-byte aligned with strides of whole 16 bytes", who, name);
     return SCN_ERR_INVALID;
   }
+  if (h->row < 0 || h->row > (1 << 22)) {
+    set_error("%s: %s has rows more than 2^22 elements apart, or in falling order", who, name);
+    return SCN_ERR_UNSUPPORTED;
+  }
   return SCN_OK;
 }
 
