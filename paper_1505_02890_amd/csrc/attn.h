@@ -45,9 +45,9 @@ struct Heads {
   int64_t row, head;
 };
 
-// The rows of one tile of a sample.  Tiles of ROWS rows are numbered over all samples
-// with tile_start(b) = ranges[b] / ROWS + b, which leaves room for each sample's
-// tiles whatever the lengths, so a grid of n / ROWS + B blocks covers them and no
+// The rows of one tile of a sample.  Tiles of `rows` rows are numbered over all samples
+// with tile_start(b) = ranges[b] / rows + b, which leaves room for each sample's
+// tiles whatever the lengths, so a grid of n / rows + B blocks covers them and no
 // length has to be known on the host (blocks past a sample's rows leave at once).
 // Bounds are clamped to [0, n], so that a bad range reads no row outside the arrays.
 struct Span {
@@ -62,13 +62,12 @@ __device__ inline int64_t range_at(const int32_t* ranges, int b, int64_t n) {
 }
 // Every lane of the wave takes part.  The sample is the last b with
 // tile_start(b) <= tile, found 64 ways at a time.
-template <int ROWS>
-__device__ inline Span find_span(const int32_t* ranges, int batch, int64_t n, int tile) {
+__device__ inline Span find_span(const int32_t* ranges, int batch, int64_t n, int tile, int rows) {
   const int lane = threadIdx.x & 63;
   int lo = 0, len = batch;
   while (len > 1) {
     const int stride = (len + 63) >> 6, b = lo + lane * stride;
-    const bool below = lane * stride < len && range_at(ranges, b, n) / ROWS + b <= tile;
+    const bool below = lane * stride < len && (int)range_at(ranges, b, n) / rows + b <= tile;
     const int c = __popcll(__ballot(below));
     const int step = max(c - 1, 0) * stride;
     lo += step;
@@ -80,8 +79,8 @@ __device__ inline Span find_span(const int32_t* ranges, int batch, int64_t n, in
   const int end = __builtin_amdgcn_readfirstlane((int)range_at(ranges, s.sample + 1, n));
   s.base = base;
   s.m = max(0, end - base);
-  const int64_t local = tile - ((int64_t)base / ROWS + s.sample);
-  s.first = local < 0 || local * ROWS >= s.m ? s.m : (int)(local * ROWS);
+  const int64_t local = tile - (base / rows + s.sample);
+  s.first = local < 0 || local * rows >= s.m ? s.m : (int)(local * rows);
   return s;
 }
 

@@ -11,9 +11,6 @@
 namespace scn {
 namespace {
 
-constexpr int RB = 128;        // rows of a block (32 a wave)
-constexpr int NT = 256;
-constexpr int SC = 1024;       // queries of a sink share
 constexpr int SPLIT_SINKS = 256;
 
 template <int NS>
@@ -27,6 +24,7 @@ struct BwdArgs {
   const float* lse;  // [Hq][n]
   float* delta;      // [Hq][n]
   float* share;      // the sinks' shares [chunk][Hk][sinks][2][D], or null
+  int sc;            // queries of a share
   float scale;
   Window w;
 };
@@ -111,18 +109,28 @@ __device__ inline void dkv_row(const BwdArgs<NS>& a, const Span& sp, int hk, int
   }
 }
 
-// NB blocks of 32 keys to a tile
-template <int NS, int DP, int NB>
-__global__ void __launch_bounds__(NT, NS == 3 && DP > 32 ? 1 : 2) attn_dq_kernel(BwdArgs<NS> a) {
-  constexpr int KT = 32 * NB;
+// QW waves of 32 queries by KW groups that share out the keys of a tile, 32 each
+template <int NS, int DP, int QW, int KW>
+struct QueryShape {
+  static constexpr int QB = 32 * QW, NT = 64 * QW * KW, KT = 32 * KW;
   typedef Tile<NS, DP, KT> L;
+  static constexpr size_t SMEM =
+      std::max<size_t>(4 * L::BYTES, (size_t)QW * (KW - 1) * (DP / 32 * 16) * 256);
+};
+
+template <int NS, int DP, int QW, int KW>
+__global__ void __launch_bounds__(64 * QW * KW, NS == 3 && DP > 32 ? 1 : 2)
+    attn_dq_kernel(BwdArgs<NS> a) {
+  typedef QueryShape<NS, DP, QW, KW> X;
+  typedef typename X::L L;
+  constexpr int KT = X::KT, NT = X::NT, QB = X::QB;
   extern __shared__ char smem[];
   const int tid = threadIdx.x, lane = tid & 63, n32 = lane & 31, half = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), kw = KW == 1 ? 0 : wave / QW;
   const int h = blockIdx.x % a.Hq;
-  const Span sp = find_span<RB>(a.ranges, a.batch, a.n, blockIdx.x / a.Hq);
+  const Span sp = find_span(a.ranges, a.batch, a.n, blockIdx.x / a.Hq, QB);
   if (sp.first >= sp.m) return;
-  const int i0 = sp.first + wave * 32, i1 = min(i0 + 31, sp.m - 1);
+  const int i0 = sp.first + (wave - kw * QW) * 32, i1 = min(i0 + 31, sp.m - 1);
   const int i = min(i0 + n32, sp.m - 1);
   const bool mine = i0 + n32 < sp.m;
   const float c2 = a.scale * LOG2E;
@@ -150,13 +158,13 @@ __global__ void __launch_bounds__(NT, NS == 3 && DP > 32 ? 1 : 2) attn_dq_kernel
   delta = both_sum(delta);
   const int64_t at = h * a.n + sp.base + i;
   const float lse2 = a.lse[at] * LOG2E;
-  if (mine && half == 0) a.delta[at] = delta;
+  if (mine && half == 0 && kw == 0) a.delta[at] = delta;
   v16f dQ[DP / 32];
 #pragma unroll
   for (int d = 0; d < DP / 32; ++d) dQ[d] = zero16();
 
   // the keys, as in the forward
-  const int lo = a.w.lo(sp.first), hi = a.w.hi(min(sp.first + RB, sp.m) - 1, sp.m);
+  const int lo = a.w.lo(sp.first), hi = a.w.hi(min(sp.first + QB, sp.m) - 1, sp.m);
   const int ns = min(a.w.sinks, lo), nst = (ns + KT - 1) / KT, nt = nst + (hi - lo + KT) / KT;
   const int wl = lo < a.w.sinks ? lo : a.w.lo(i0), wh = a.w.hi(i1, sp.m);
   const int al = a.w.lo(i0 + 31), ah = a.w.hi(i0, sp.m);
@@ -179,56 +187,46 @@ __global__ void __launch_bounds__(NT, NS == 3 && DP > 32 ? 1 : 2) attn_dq_kernel
     sv.store(smem + (t & 1) * 2 * L::BYTES + L::BYTES, tid);
   };
   auto take = [&](int t) {
-    const int j0 = first_key(t);
+    const int j0 = first_key(t) + kw * 32;
     const bool sink = t < nst;
-    char* const kt = smem + (t & 1) * 2 * L::BYTES;
+    char* const kt = smem + (t & 1) * 2 * L::BYTES + kw * 32 * DP * 2;
     char* const vt = kt + L::BYTES;
-    v16f S[NB], P[NB];
+    v16f S = zero16(), P = zero16();
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      S[b] = zero16();
-      P[b] = zero16();
+    for (int s = 0; s < DP / 16; ++s) S = mma<NS>(L::rows(kt, pl, 0, s), Q[s], S);
 #pragma unroll
-      for (int s = 0; s < DP / 16; ++s) S[b] = mma<NS>(L::rows(kt, pl, 32 * b, s), Q[s], S[b]);
-#pragma unroll
-      for (int s = 0; s < DP / 16; ++s) P[b] = mma<NS>(L::rows(vt, pl, 32 * b, s), G[s], P[b]);
-    }
-    if (sink ? j0 + 32 * NB > ns : j0 < al || j0 + 32 * NB - 1 > ah) {
+    for (int s = 0; s < DP / 16; ++s) P = mma<NS>(L::rows(vt, pl, 0, s), G[s], P);
+    if (sink ? j0 + 32 > ns : j0 < al || j0 + 31 > ah) {
       const int l = (sink ? 0 : a.w.lo(i)) - j0 - 4 * half;
       const int u = (sink ? ns - 1 : a.w.hi(i, sp.m)) - j0 - 4 * half;
       const int z = (sink ? 0 : a.w.sinks - j0) - 4 * half;
 #pragma unroll
-      for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int e = 32 * b + 8 * (r / 4) + r % 4;
-          S[b][r] = ((e <= u) & ((e >= l) | (e < z))) ? S[b][r] : -INFINITY;
-        }
+      for (int r = 0; r < 16; ++r) {
+        const int e = 8 * (r / 4) + r % 4;
+        S[r] = ((e <= u) & ((e >= l) | (e < z))) ? S[r] : -INFINITY;
+      }
     }
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
+    for (int r = 0; r < 16; ++r)
+      S[r] = __builtin_amdgcn_exp2f(fmaf(S[r], c2, -lse2)) * (P[r] - delta);
 #pragma unroll
-      for (int r = 0; r < 16; ++r)
-        S[b][r] = __builtin_amdgcn_exp2f(fmaf(S[b][r], c2, -lse2)) * (P[b][r] - delta);
+    for (int s = 0; s < 2; ++s) {
+      float x[8];
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        float x[8];
+      for (int j = 0; j < 8; ++j) x[j] = S[8 * s + j];
+      const Frag<NS> X = to_frag<NS>(x);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = S[b][8 * s + j];
-        const Frag<NS> X = to_frag<NS>(x);
-#pragma unroll
-        for (int d = 0; d < DP / 32; ++d)
-          dQ[d] = mma<NS>(L::cols(kt, pl, 32 * b + 16 * s, d), X, dQ[d]);
-      }
+      for (int d = 0; d < DP / 32; ++d) dQ[d] = mma<NS>(L::cols(kt, pl, 16 * s, d), X, dQ[d]);
     }
   };
   auto pass = [&](int t) {
     if (t + 1 < nt) put(t + 1);
     if (t + 2 < nt) fetch(t + 2);
   };
-  auto place = [&](int x) { return nst + max(0, x) / KT; };
+  auto place = [&](int x) { return nst + max(0, x - kw * 32) / KT; };
+  const int some = i0 <= i1 && wh - lo >= kw * 32;
   const int e0 = i0 <= i1 ? nst : 0;
-  const int s1 = i0 <= i1 ? place(wl - lo) : nt, e1 = i0 <= i1 ? place(wh - lo) + 1 : nt;
+  const int s1 = some ? place(wl - lo) : nt, e1 = some ? place(wh - lo) + 1 : nt;
   fetch(0);
   put(0);
   if (nt > 1) fetch(1);
@@ -249,6 +247,23 @@ __global__ void __launch_bounds__(NT, NS == 3 && DP > 32 ? 1 : 2) attn_dq_kernel
   for (; t < nt; ++t) {
     pass(t);
     __syncthreads();
+  }
+  if constexpr (KW > 1) {
+    float* const x = reinterpret_cast<float*>(smem) + lane;
+    if (kw > 0)
+#pragma unroll
+      for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          x[((wave - QW) * (DP / 32) * 16 + d * 16 + r) * 64] = dQ[d][r];
+    __syncthreads();
+    if (kw > 0) return;
+    for (int g = 0; g < KW - 1; ++g)
+#pragma unroll
+      for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          dQ[d][r] += x[((g * QW + wave) * (DP / 32) * 16 + d * 16 + r) * 64];
   }
   bool fine = true;
 #pragma unroll
@@ -351,7 +366,7 @@ struct QueryTiles {
 };
 
 // Sinks are seen by every later query, so a block that owned them would run far longer
-// than the others.  Their pairs past the window go here, in shares of SC queries:
+// than the others.  Their pairs past the window go here, in shares of sc queries:
 // block (chunk, sink tile of 32, key head), two waves with 32 queries of each tile.
 template <int NS, int DP>
 __global__ void __launch_bounds__(128, 1) attn_sink_kernel(BwdArgs<NS> a, int nst) {
@@ -363,9 +378,9 @@ __global__ void __launch_bounds__(128, 1) attn_sink_kernel(BwdArgs<NS> a, int ns
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int hk = blockIdx.x % a.Hk, j0 = blockIdx.x / a.Hk % nst * 32;
   const int chunk = blockIdx.x / a.Hk / nst;
-  const Span sp = find_span<SC>(a.ranges, a.batch, a.n, chunk);
+  const Span sp = find_span(a.ranges, a.batch, a.n, chunk, a.sc);
   const int ns = min(a.w.sinks, sp.m);
-  const int end = min(sp.first + SC, sp.m) - 1;         // the share's queries
+  const int end = min(sp.first + a.sc, sp.m) - 1;       // the share's queries
   const int first = max(sp.first, j0 + a.w.left + 1);   // ... past the window of j0
   if (sp.first >= sp.m || j0 >= ns || first > end) return;
   const int j = min(j0 + n32, ns - 1);
@@ -421,17 +436,58 @@ __global__ void __launch_bounds__(128, 1) attn_sink_kernel(BwdArgs<NS> a, int ns
     }
 }
 
-template <int NS, int DP, int TB>
-__global__ void __launch_bounds__(NT, NS == 3 || DP > 64 ? 1 : 2) attn_dkv_kernel(BwdArgs<NS> a) {
+// A sink's shares, added up in order into the first of them: block (sample, head, sink),
+// an element a thread.
+template <int NS>
+__global__ void __launch_bounds__(256) attn_share_kernel(BwdArgs<NS> a) {
+  const int j = blockIdx.x % a.w.sinks, hk = blockIdx.x / a.w.sinks % a.Hk;
+  const int b = blockIdx.x / a.w.sinks / a.Hk;
+  const int base = (int)range_at(a.ranges, b, a.n);
+  const int m = (int)range_at(a.ranges, b + 1, a.n) - base;
+  const int far = (j & ~31) + a.w.left + 1;  // the first query past the window
+  if ((int)threadIdx.x >= 2 * a.D || j >= m || far >= m) return;
+  const int64_t step = (int64_t)a.Hk * a.w.sinks * 2 * a.D;
+  float* const p = a.share + (int64_t)(base / a.sc + b + far / a.sc) * step +
+                   ((int64_t)hk * a.w.sinks + j) * 2 * a.D + threadIdx.x;
+  const int n = (m + a.sc - 1) / a.sc - far / a.sc;
+  float s = 0.f;
+  int c = 0;
+  for (; c + 8 <= n; c += 8) {
+    float x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = p[(c + e) * step];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s += x[e];
+  }
+  for (; c < n; ++c) s += p[c * step];
+  *p = s;
+}
+
+// KW waves of 32 keys by QW groups that share out the queries of a tile, 32 U each.  The
+// groups' sums join in LDS at the end.
+template <int NS, int DP, int KW, int QW, int U>
+struct KeyShape {
+  static constexpr int KB = 32 * KW, NT = 64 * KW * QW, TB = 32 * U * QW;
   typedef QueryTiles<NS, DP, TB, NT> QT;
+  static constexpr int JOIN = DP / 32 * 32;  // floats a lane hands over
+  static constexpr size_t SMEM =
+      std::max<size_t>(2 * QT::BUF, (size_t)KW * (QW - 1) * JOIN * 256);
+};
+
+template <int NS, int DP, int KW, int QW, int U>
+__global__ void __launch_bounds__(64 * KW * QW, NS == 3 || DP > 64 ? 1 : 2)
+    attn_dkv_kernel(BwdArgs<NS> a) {
+  typedef KeyShape<NS, DP, KW, QW, U> X;
+  constexpr int KB = X::KB, TB = X::TB;
+  typedef typename X::QT QT;
   typedef typename QT::L L;
   extern __shared__ char smem[];
   const int tid = threadIdx.x, lane = tid & 63, n32 = lane & 31, half = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), qw = QW == 1 ? 0 : wave / KW;
   const int hk = blockIdx.x % a.Hk;
-  const Span sp = find_span<RB>(a.ranges, a.batch, a.n, blockIdx.x / a.Hk);
+  const Span sp = find_span(a.ranges, a.batch, a.n, blockIdx.x / a.Hk, KB);
   if (sp.first >= sp.m) return;
-  const int j0 = sp.first + wave * 32, j1 = min(j0 + 31, sp.m - 1);  // the wave's keys
+  const int j0 = sp.first + (wave - qw * KW) * 32, j1 = min(j0 + 31, sp.m - 1);  // the wave's keys
   const int j = min(j0 + n32, sp.m - 1);
   const float c2 = a.scale * LOG2E;
   // sinks whose far queries other blocks have taken are ordinary keys here
@@ -450,7 +506,7 @@ __global__ void __launch_bounds__(NT, NS == 3 || DP > 64 ? 1 : 2) attn_dkv_kerne
 
   const int first = max(0, sp.first - w.right);
   const int end = sp.first < sinks ? sp.m - 1
-                                   : min(sp.m - 1, min(sp.first + RB, sp.m) - 1 + w.left);
+                                   : min(sp.m - 1, min(sp.first + KB, sp.m) - 1 + w.left);
   const int per = (end - first + TB) / TB, ntile = per * a.group;
   QT st;
   st.init(a, tid);
@@ -465,9 +521,11 @@ __global__ void __launch_bounds__(NT, NS == 3 || DP > 64 ? 1 : 2) attn_dkv_kerne
   };
   // The wave takes the tiles [s, e) of each query head: the queries that see one of its
   // keys.
-  const int ql = max(0, j0 - w.right) - first;
-  const int qh = (j0 < sinks ? sp.m - 1 : min(sp.m - 1, j1 + w.left)) - first;
-  const int s = j0 <= j1 ? max(0, ql) / TB : per, e = j0 <= j1 ? min(per, qh / TB + 1) : per;
+  const int q0 = qw * 32 * U;  // the wave's queries of a tile
+  const int ql = max(0, j0 - w.right) - first - q0;
+  const int qh = (j0 < sinks ? sp.m - 1 : min(sp.m - 1, j1 + w.left)) - first - q0;
+  const bool some = j0 <= j1 && qh >= 0;
+  const int s = some ? min(per, max(0, ql) / TB) : per, e = some ? min(per, qh / TB + 1) : per;
   fetch(0);
   put(0);
   if (ntile > 1) fetch(1);
@@ -483,14 +541,15 @@ __global__ void __launch_bounds__(NT, NS == 3 || DP > 64 ? 1 : 2) attn_dkv_kerne
       char* const b = smem + (t & 1) * QT::BUF;
       const float* const f = reinterpret_cast<const float*>(b + 2 * L::BYTES);
 #pragma unroll
-      for (int u = 0; u < TB / 32; ++u) {
-        const int i0 = first + (t - t0) * TB + 32 * u, i1 = i0 + 31;
+      for (int u = 0; u < U; ++u) {
+        const int i0 = first + (t - t0) * TB + q0 + 32 * u, i1 = i0 + 31;
         const bool all = i1 <= end && j0 + 31 <= i0 + w.right && j0 >= i1 - w.left;
         auto see = [&](int r) {
-          const int i = i0 - 32 * u + r;
+          const int i = i0 - q0 - 32 * u + r;
           return (i <= end) & (j <= i + w.right) & ((j >= i - w.left) | (j < sinks));
         };
-        key_block<NS, DP, TB>(b, b + L::BYTES, pl, f, f + TB, 32 * u, K, V, c2, !all, see, dK, dV);
+        key_block<NS, DP, TB>(b, b + L::BYTES, pl, f, f + TB, q0 + 32 * u, K, V, c2, !all, see, dK,
+                              dV);
       }
       __syncthreads();
     }
@@ -499,28 +558,50 @@ __global__ void __launch_bounds__(NT, NS == 3 || DP > 64 ? 1 : 2) attn_dkv_kerne
       __syncthreads();
     }
   }
-  const bool mine = j0 + n32 < sp.m;
-  const int far = (j & ~31) + a.w.left + 1;  // first query past the window of the sink tile
-  if (a.share && mine && j < a.w.sinks && far < sp.m) {
-    // the shares of these queries, in order
-    const int64_t chunk0 = sp.base / SC + sp.sample;
-    for (int c = far / SC; c < (sp.m + SC - 1) / SC; ++c) {
-      const float* const p = a.share + (((chunk0 + c) * a.Hk + hk) * a.w.sinks + j) * 2 * a.D;
+  if constexpr (QW > 1) {
+    float* const x = reinterpret_cast<float*>(smem) + lane;
+    if (qw > 0) {
+      float* const o = x + (wave - KW) * X::JOIN * 64;
 #pragma unroll
       for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const int ch = 32 * d + 8 * g + 4 * half;
-          if (ch >= a.D) continue;
-          const v4f x = *reinterpret_cast<const v4f*>(p + ch);
-          const v4f y = *reinterpret_cast<const v4f*>(p + a.D + ch);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            dK[d][4 * g + e] += x[e];
-            dV[d][4 * g + e] += y[e];
-          }
+        for (int r = 0; r < 16; ++r) {
+          o[(d * 16 + r) * 64] = dK[d][r];
+          o[((DP / 32 + d) * 16 + r) * 64] = dV[d][r];
         }
     }
+    __syncthreads();
+    if (qw > 0) return;
+    for (int g = 1; g < QW; ++g) {
+      const float* const o = x + ((g - 1) * KW + wave) * X::JOIN * 64;
+#pragma unroll
+      for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          dK[d][r] += o[(d * 16 + r) * 64];
+          dV[d][r] += o[((DP / 32 + d) * 16 + r) * 64];
+        }
+    }
+  }
+  const bool mine = j0 + n32 < sp.m;
+  const int far = (j & ~31) + a.w.left + 1;  // first query past the window of the sink tile
+  if (a.share && mine && j < a.w.sinks && far < sp.m) {
+    const int64_t c = sp.base / a.sc + sp.sample + far / a.sc;  // where their sum lies
+    const float* const p = a.share + ((c * a.Hk + hk) * a.w.sinks + j) * 2 * a.D;
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const int ch = 32 * d + 8 * g + 4 * half;
+        if (ch >= a.D) continue;
+        const v4f x = *reinterpret_cast<const v4f*>(p + ch);
+        const v4f y = *reinterpret_cast<const v4f*>(p + a.D + ch);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          dK[d][4 * g + e] += x[e];
+          dV[d][4 * g + e] += y[e];
+        }
+      }
   }
   bool fine = true;
 #pragma unroll
@@ -548,42 +629,104 @@ __global__ void __launch_bounds__(NT, NS == 3 || DP > 64 ? 1 : 2) attn_dkv_kerne
 bool split_sinks(int64_t n, int64_t left, int64_t sinks) {
   return left >= 0 && left < n && sinks > 0 && sinks <= SPLIT_SINKS;
 }
-int64_t sink_chunks(int64_t n, int batch) { return n / SC + batch; }
+// Shares of at least 256 queries (some tiles' work for a block), and not more than about
+// 256 of them to add up.
+int share_rows(int64_t n) {
+  int sc = 256;
+  while (n / sc > 256) sc *= 2;
+  return sc;
+}
+int64_t sink_chunks(int64_t n, int batch) { return n / share_rows(n) + batch; }
 
-template <int NS, int DP>
-scn_status launch(const BwdArgs<NS>& a, hipStream_t st) {
-  const int64_t tiles = a.n / RB + a.batch;
-  const int nst = (a.w.sinks + 31) / 32;
-  const int64_t shares = a.share ? sink_chunks(a.n, a.batch) * a.Hk * nst : 0;
-  if (std::max(tiles * a.Hq, shares) > INT32_MAX) {
+template <int NS, int DP, int KW, int QW, int U>
+scn_status launch_dkv(const BwdArgs<NS>& a, hipStream_t st) {
+  typedef KeyShape<NS, DP, KW, QW, U> X;
+  static LdsLimit limit;
+  auto fn = attn_dkv_kernel<NS, DP, KW, QW, U>;
+  if (scn_status rc = allow_lds(reinterpret_cast<const void*>(fn), limit, X::SMEM)) return rc;
+  const int64_t blocks = (a.n / X::KB + a.batch) * a.Hk;
+  if (blocks > INT32_MAX) {
     set_error("scn_attn_bwd: more than 2^31 blocks of rows and heads");
     return SCN_ERR_OVERFLOW;
   }
-  {
-    constexpr int NB = NS == 1 && DP <= 64 ? 2 : 1;
-    constexpr size_t smem = 4 * Tile<NS, DP, 32 * NB>::BYTES;
-    static LdsLimit limit;
-    auto fn = attn_dq_kernel<NS, DP, NB>;
-    if (scn_status rc = allow_lds(reinterpret_cast<const void*>(fn), limit, smem)) return rc;
-    hipLaunchKernelGGL(fn, dim3((unsigned)(tiles * a.Hq)), dim3(NT), smem, st, a);
-    SCN_LAUNCH_CHECK();
-  }
-  if (a.share) {
-    constexpr size_t smem = std::max<size_t>(QueryTiles<NS, DP, 64, 128>::BUF, DP * 2 * 32 * 4);
-    static LdsLimit limit;
-    auto fn = attn_sink_kernel<NS, DP>;
-    if (scn_status rc = allow_lds(reinterpret_cast<const void*>(fn), limit, smem)) return rc;
-    hipLaunchKernelGGL(fn, dim3((unsigned)shares), dim3(128), smem, st, a, nst);
-    SCN_LAUNCH_CHECK();
-  }
-  constexpr int TB = NS == 1 ? 64 : 32;  // (split tiles are three times as large)
-  constexpr size_t smem = 2 * QueryTiles<NS, DP, TB, NT>::BUF;
-  static LdsLimit limit;
-  auto fn = attn_dkv_kernel<NS, DP, TB>;
-  if (scn_status rc = allow_lds(reinterpret_cast<const void*>(fn), limit, smem)) return rc;
-  hipLaunchKernelGGL(fn, dim3((unsigned)(tiles * a.Hk)), dim3(NT), smem, st, a);
+  hipLaunchKernelGGL(fn, dim3((unsigned)blocks), dim3(X::NT), X::SMEM, st, a);
   SCN_LAUNCH_CHECK();
   return SCN_OK;
+}
+
+template <int NS, int DP, int QW, int KW>
+scn_status launch_dq(const BwdArgs<NS>& a, hipStream_t st) {
+  typedef QueryShape<NS, DP, QW, KW> X;
+  static LdsLimit limit;
+  auto fn = attn_dq_kernel<NS, DP, QW, KW>;
+  if (scn_status rc = allow_lds(reinterpret_cast<const void*>(fn), limit, X::SMEM)) return rc;
+  const int64_t blocks = (a.n / X::QB + a.batch) * a.Hq;
+  if (blocks > INT32_MAX) {
+    set_error("scn_attn_bwd: more than 2^31 blocks of rows and heads");
+    return SCN_ERR_OVERFLOW;
+  }
+  hipLaunchKernelGGL(fn, dim3((unsigned)blocks), dim3(X::NT), X::SMEM, st, a);
+  SCN_LAUNCH_CHECK();
+  return SCN_OK;
+}
+
+template <int NS, int DP>
+scn_status launch_sinks(const BwdArgs<NS>& a, hipStream_t st) {
+  const int nst = (a.w.sinks + 31) / 32;
+  const int64_t blocks = sink_chunks(a.n, a.batch) * a.Hk * nst;
+  if (std::max(blocks, (int64_t)a.w.sinks * a.Hk * a.batch) > INT32_MAX) {
+    set_error("scn_attn_bwd: more than 2^31 blocks of sinks and heads");
+    return SCN_ERR_OVERFLOW;
+  }
+  constexpr size_t smem = std::max<size_t>(QueryTiles<NS, DP, 64, 128>::BUF, DP * 2 * 32 * 4);
+  static LdsLimit limit;
+  auto fn = attn_sink_kernel<NS, DP>;
+  if (scn_status rc = allow_lds(reinterpret_cast<const void*>(fn), limit, smem)) return rc;
+  hipLaunchKernelGGL(fn, dim3((unsigned)blocks), dim3(128), smem, st, a, nst);
+  SCN_LAUNCH_CHECK();
+  hipLaunchKernelGGL(attn_share_kernel<NS>, dim3((unsigned)(a.w.sinks * a.Hk * a.batch)), dim3(256),
+                     0, st, a);
+  SCN_LAUNCH_CHECK();
+  return SCN_OK;
+}
+
+// The shapes, by measurement (us; queries' pass, keys' pass):
+//  - Two waves by two groups serve most: four waves side by side and no groups are 2 to
+//    4% better in the keys' pass once there are over a thousand blocks of 128 keys
+//    (60,007 rows of 4 heads, 64 channels: 188 against 207), and with more than 64
+//    channels, where two groups' tiles and sums crowd the registers (30,000 rows of 2 key
+//    heads, 128 channels: 223 against 272).
+//  - Few blocks, counted against the query heads that each has to take in turn: a wave's
+//    32 keys by four groups (2000 rows of 4 heads: 54 to 27; 32,001 rows, 4 heads on one:
+//    310 to 190).
+//  - fp32, 64 channels: four waves by two groups in the queries' pass (20,000 rows of 4
+//    heads: 381 to 300).
+template <int NS, int DP>
+scn_status launch(const BwdArgs<NS>& a, hipStream_t st) {
+  const int64_t tiles = a.n / 128 + a.batch;
+  scn_status rc;
+  if constexpr (NS == 3 && DP > 64) {
+    rc = launch_dq<NS, DP, 4, 1>(a, st);
+  } else if constexpr (NS == 3 && DP == 64) {
+    rc = launch_dq<NS, DP, 4, 2>(a, st);
+  } else {
+    constexpr int QW = DP > 64 ? 4 : 2, KW = DP > 64 ? 1 : 2;
+    rc = tiles * a.Hq >= 512 ? launch_dq<NS, DP, QW, KW>(a, st) : launch_dq<NS, DP, 2, 2>(a, st);
+  }
+  if (rc) return rc;
+  if (a.share && (rc = launch_sinks<NS, DP>(a, st))) return rc;
+  const int64_t blocks = tiles * a.Hk;
+  if constexpr (NS == 3) {
+    if constexpr (DP <= 64)
+      return launch_dkv<NS, DP, 2, 2, 1>(a, st);
+    else
+      return launch_dkv<NS, DP, 4, 1, 1>(a, st);
+  } else {
+    if constexpr (DP <= 64)
+      if (blocks < 128 * a.group) return launch_dkv<NS, DP, 1, 4, 1>(a, st);
+    if (blocks < (DP <= 64 ? 1024 : 384)) return launch_dkv<NS, DP, 2, 2, 1>(a, st);
+    return launch_dkv<NS, DP, 4, 1, 2>(a, st);
+  }
 }
 
 template <int NS>
@@ -647,13 +790,13 @@ scn_status scn_attn_bwd(int32_t type, int64_t n, int32_t batch, const int32_t* r
     return run<1>(BwdArgs<1>{n, batch, D, Hq, Hk, Hq / Hk, ranges, view<const T>(q),
                              view<const T>(k), view<const T>(v), view<const T>(o),
                              view<const T>(d_o), view<T>(dq), view<T>(dk), view<T>(dv), lse, delta,
-                             share, scale, w}, st);
+                             share, share_rows(n), scale, w}, st);
   }
   typedef float T;
   return run<3>(BwdArgs<3>{n, batch, D, Hq, Hk, Hq / Hk, ranges, view<const T>(q),
                            view<const T>(k), view<const T>(v), view<const T>(o),
                            view<const T>(d_o), view<T>(dq), view<T>(dk), view<T>(dv), lse, delta,
-                           share, scale, w}, st);
+                           share, share_rows(n), scale, w}, st);
 }
 
 }  // extern "C"

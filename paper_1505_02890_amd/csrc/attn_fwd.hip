@@ -85,12 +85,12 @@ __global__ void __launch_bounds__(64 * QW * KW, NS == 3 && DP > 64 ? 1 : 2)
   constexpr int QB = X::QB, KT = X::KT, NT = X::NT;
   extern __shared__ char smem[];
   const int tid = threadIdx.x, lane = tid & 63, n32 = lane & 31, half = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), kw = wave / QW;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), kw = KW == 1 ? 0 : wave / QW;
   const int h = blockIdx.x % a.Hq;
-  const Span sp = find_span<QB>(a.ranges, a.batch, a.n, blockIdx.x / a.Hq);
+  const Span sp = find_span(a.ranges, a.batch, a.n, blockIdx.x / a.Hq, QB);
   if (sp.first >= sp.m) return;
   // the wave's queries (i1 < i0 past the sample's rows) and the lane's
-  const int i0 = sp.first + wave % QW * 32, i1 = min(i0 + 31, sp.m - 1);
+  const int i0 = sp.first + (wave - kw * QW) * 32, i1 = min(i0 + 31, sp.m - 1);
   const int i = min(i0 + n32, sp.m - 1);
   const float c2 = a.scale * LOG2E;
 
