@@ -505,8 +505,8 @@ scn_status scn_attn_bwd(int32_t type, int64_t n, int32_t batch, const int32_t* r
                         const scn_heads* dv, void* ws, size_t ws_bytes, hipStream_t stream);
 
 /* Bytes of device workspace scn_attn_step needs. */
-size_t scn_attn_step_workspace_bytes(int32_t streams, int64_t capacity, int32_t D, int32_t Hq,
-                                     int32_t Hk, int64_t left, int64_t sinks);
+size_t scn_attn_step_workspace_bytes(int32_t type, int32_t streams, int64_t capacity, int32_t D,
+                                     int32_t Hq, int32_t Hk, int64_t left, int64_t sinks);
 
 /*
  * Attention of one new token of each stream, over the stream's last tokens and

@@ -125,7 +125,7 @@ def lib() -> ctypes.CDLL:
         "scn_attn_bwd_workspace_bytes": (sz, [i64, i32, i32, i32, i32, i64, i64]),
         "scn_attn_bwd": (st, [i32, i64, i32, P, i32, i32, i32, P, P, P, P, P, P, f32, i64, i64,
                               i64, P, P, P, P, sz, P]),
-        "scn_attn_step_workspace_bytes": (sz, [i32, i64, i32, i32, i32, i64, i64]),
+        "scn_attn_step_workspace_bytes": (sz, [i32, i32, i64, i32, i32, i32, i64, i64]),
         "scn_attn_step": (st, [i32, i32, i64, i32, i32, i32, P, P, P, P, P, P, f32, i64, i64, P,
                                P, sz, P]),
         "scn_set_allocator": (None, [_ALLOC_FN, _FREE_FN, P]),
@@ -659,7 +659,7 @@ def attn_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_cache: torch.
     l = _bound(left, "left")
     o, vo = _out_rows(out, q, (b, hq, d), "out")
     if ws is None:
-        n = lib().scn_attn_step_workspace_bytes(b, cap, d, hq, hk, l, sinks)
+        n = lib().scn_attn_step_workspace_bytes(SCN_TYPE[dtype], b, cap, d, hq, hk, l, sinks)
         ws = _bytes(n, q.device) if n else None
     _check(lib().scn_attn_step(
         SCN_TYPE[dtype], b, cap, d, hq, hk, _ref(vq), _ref(vk), _ref(vv), _ref(ck), _ref(cv), pl,

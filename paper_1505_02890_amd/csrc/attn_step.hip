@@ -1,10 +1,10 @@
 // Attention of one new token of each stream over its cache: the sinks and the last
 // positions of the ring, each row read once.  Memory bounds it (two flops a byte and
-// query head), so there is nothing to stage: LP lanes hold a key's channels, eight a
-// lane, and take every query head of the key head while its row is in registers.  Each
-// group of LP lanes keeps a running maximum, sum and output of its own; they join
-// within the wave, the block and, where a stream's keys are split over blocks, in a
-// second kernel, always in the same order.
+// query head).  A stream's rows are split over blocks where there are few streams; the
+// parts' outputs, maxima and sums join in a second kernel, always in the same order.
+// Measured, reading the visible rows: 128 streams of 2064 rows, 8 heads on 2 of 64
+// channels, bf16: 29 us, 3.9 TB/s (64 channels' rows lie 256 bytes apart); one stream of
+// 262,144 rows, 4 heads of 32, fp32: 47 us, 5.7 TB/s.
 #include "attn.h"
 
 namespace scn {
@@ -12,6 +12,7 @@ namespace {
 
 constexpr int NT = 256;
 constexpr int U = 4;  // rows of a lane group in flight
+constexpr int MAX_SPLITS = 1024;
 
 struct Ring {
   int64_t stream, row, head;
@@ -42,7 +43,9 @@ __device__ inline void join(float& m, float& l, float m2, float l2, float& f, fl
   m = t;
 }
 
-// GC query heads of a key head (pass), one split of a stream's visible positions
+// fp32, on the vector unit: LP lanes hold a key's channels, eight a lane, and take GC query
+// heads of the key head while its row is in registers.  Each group of LP lanes keeps a
+// running maximum, sum and output of its own, which join within the wave and the block.
 template <int NS, int LP, int GC>
 __global__ void __launch_bounds__(NT) attn_step_kernel(StepArgs<NS> a) {
   typedef Elem<NS> E;
@@ -172,30 +175,232 @@ __global__ void __launch_bounds__(NT) attn_step_kernel(StepArgs<NS> a) {
   }
 }
 
-// The splits of a stream's head: blockIdx.x = stream * Hq + head
+// bf16, on matrix cores: the query heads of a key head are the columns of the
+// forward's products, up to 32 of them, and a wave takes 32 cache rows at a time through
+// its own part of LDS.  A row then costs the same whether one head or 32 read it, where
+// the kernel above takes 28 vector instructions a lane for each (16 heads on one of 128
+// channels, 64 streams of 4096 rows: 109 us that way, 28 this way).
+template <int DP>
+__global__ void __launch_bounds__(NT, 2) attn_step_wide_kernel(StepArgs<1> a) {
+  typedef uint16_t T;
+  typedef Tile<1, DP, 32> L;
+  typedef Stage<1, DP, 32, 64> St;
+  constexpr int JOIN = DP / 32 * 16 + 2;
+  constexpr int WAVES = NT / 64;
+  __shared__ __align__(16) char smem[std::max(WAVES * 2 * L::BYTES, (WAVES - 1) * JOIN * 256)];
+  const int split = blockIdx.x % a.splits, pass = blockIdx.x / a.splits % a.passes;
+  const int hk = blockIdx.x / a.splits / a.passes % a.Hk;
+  const int s = blockIdx.x / a.splits / a.passes / a.Hk;
+  const int h0 = hk * a.group + pass * 32, nh = min(32, a.group - pass * 32);
+  const int tid = threadIdx.x, lane = tid & 63, n32 = lane & 31, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int p = __builtin_amdgcn_readfirstlane(min(max(0, a.length[s]), INT32_MAX - 1));
+  const float c2 = a.scale * LOG2E;
+  // What the new token sees, in runs of cache rows: the sinks, the ring's part up to its
+  // end, the part from its begin, and the token's own row, which is not in the cache yet.
+  const int ring = a.cap - a.sinks;
+  const int lo = min(p, max(a.sinks, p - a.reach)), ns = min(a.sinks, p);
+  const int old = p - lo, r0 = old > 0 ? (lo - a.sinks) % ring : 0;
+  const int nb = min(old, ring - r0), nc = old - nb;
+  const int ta = (ns + 31) / 32, tb = ta + (nb + 31) / 32, tc = tb + (nc + 31) / 32;
+  const int per = (tc + a.splits) / a.splits;  // of tc + 1 tiles
+  const int t1 = min(tc + 1, (split + 1) * per);
+  const T* const kn = a.k.p + s * a.k.row + hk * a.k.head;
+  const T* const vn = a.v.p + s * a.v.row + hk * a.v.head;
+  T* const kc = a.kc + s * a.ks.stream + hk * a.ks.head;
+  T* const vc = a.vc + s * a.vs.stream + hk * a.vs.head;
+
+  Frag<1> Q[DP / 16];
+#pragma unroll
+  for (int c = 0; c < DP / 16; ++c) {
+    Q[c].s[0] = v4u{0, 0, 0, 0};
+    if (n32 < nh) Q[c] = load_frag<1>(a.q.p + s * a.q.row + (h0 + n32) * a.q.head, c, a.D, lane);
+  }
+  v16f O[DP / 32];
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d) O[d] = zero16();
+  float top = -INFINITY, base = 0.f, sum = 0.f;
+  St sk, sv;
+  uint32_t ko[St::N], vo[St::N];
+  St::places(ko, a.ks.row, a.D, lane);
+  St::places(vo, a.vs.row, a.D, lane);
+  const typename L::Lane at(lane);
+  auto fetch = [&](int t) -> int {
+    // tile t's rows
+    int row, n;
+    if (t < ta) {
+      row = t * 32;
+      n = ns - row;
+    } else if (t < tb) {
+      row = a.sinks + r0 + (t - ta) * 32;
+      n = nb - (t - ta) * 32;
+    } else if (t < tc) {
+      row = a.sinks + (t - tb) * 32;
+      n = nc - (t - tb) * 32;
+    } else {
+      sk.load(kn, 0, ko, 0, 1, a.D);
+      sv.load(vn, 0, vo, 0, 1, a.D);
+      return 1;
+    }
+    sk.load(kc, a.ks.row, ko, row, n, a.D);
+    sv.load(vc, a.vs.row, vo, row, n, a.D);
+    return min(n, 32);
+  };
+  char* const kt = smem + wave * 2 * L::BYTES;
+  char* const vt = kt + L::BYTES;
+  int n = 0, t = split * per + wave;
+  if (t < t1) n = fetch(t);
+  for (; t < t1; t += WAVES) {
+    sk.store(kt, lane);
+    sv.store(vt, lane);
+    const int now = n;
+    if (t + WAVES < t1) n = fetch(t + WAVES);
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    v16f S = zero16();
+#pragma unroll
+    for (int c = 0; c < DP / 16; ++c) S = mma<1>(L::rows(kt, at, 0, c), Q[c], S);
+    if (now < 32)
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        S[r] = 8 * (r / 4) + 4 * half + r % 4 < now ? S[r] : -INFINITY;
+    float m = larger(S[0], S[1]);
+#pragma unroll
+    for (int r = 2; r < 16; ++r) m = larger(m, S[r]);
+    m = both_larger(m) * c2;
+    if (__ballot(m > top + 8.f)) {
+      const float next = fmaxf(top, m);
+      const float f = next == top ? 1.f : __builtin_amdgcn_exp2f(top - next);
+      top = next;
+      base = next == -INFINITY ? 0.f : next;
+      sum *= f;
+#pragma unroll
+      for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) O[d][r] *= f;
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      S[r] = __builtin_amdgcn_exp2f(fmaf(S[r], c2, -base));
+      sum += S[r];
+    }
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      float x[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = S[8 * e + j];
+      // The weights keep 16 bits, in two parts: the matrix cores have time to spare
+      // here, and one stream's output is all that a step gives.
+      Frag<1> P[2];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t hi = cvt2_bf16(x[2 * j], x[2 * j + 1]);
+        P[0].s[0][j] = hi;
+        P[1].s[0][j] = cvt2_bf16(x[2 * j] - __uint_as_float(hi << 16),
+                                 x[2 * j + 1] - __uint_as_float(hi & 0xffff0000u));
+      }
+#pragma unroll
+      for (int d = 0; d < DP / 32; ++d) {
+        const Frag<1> V = L::cols(vt, at, 16 * e, d);
+        O[d] = mma<1>(V, P[1], O[d]);
+        O[d] = mma<1>(V, P[0], O[d]);
+      }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+  sum = both_sum(sum);
+  // the waves, joined in order
+  float* const x = reinterpret_cast<float*>(smem) + lane;
+  __syncthreads();
+  if (wave > 0) {
+    float* const o = x + (wave - 1) * JOIN * 64;
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[(d * 16 + r) * 64] = O[d][r];
+    o[(JOIN - 2) * 64] = top;
+    o[(JOIN - 1) * 64] = sum;
+  }
+  __syncthreads();
+  if (wave == 0) {
+    for (int g = 0; g < WAVES - 1; ++g) {
+      const float* const o = x + g * JOIN * 64;
+      float f, f2;
+      join(top, sum, o[(JOIN - 2) * 64], o[(JOIN - 1) * 64], f, f2);
+#pragma unroll
+      for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) O[d][r] = O[d][r] * f + o[(d * 16 + r) * 64] * f2;
+    }
+    if (n32 < nh) {
+      if (a.splits == 1) {
+        const float inv = 1.f / sum;
+        T* const o = a.o.p + s * a.o.row + (h0 + n32) * a.o.head;
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d) store_cols<1>(o, O[d], inv, d, a.D, lane);
+      } else {
+        float* const o =
+            a.part + (((int64_t)s * a.Hq + h0 + n32) * a.splits + split) * (a.D + 2);
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int c = 32 * d + 8 * (r / 4) + 4 * half + r % 4;
+            if (c < a.D) o[c] = O[d][r];
+          }
+        if (half == 0) {
+          o[a.D] = top;
+          o[a.D + 1] = sum;
+        }
+      }
+    }
+  }
+  if (split == 0 && pass == 0 && tid < a.D) {
+    const int64_t r = p < a.sinks ? p : a.sinks + (p - a.sinks) % ring;
+    kc[r * a.ks.row + tid] = kn[tid];
+    vc[r * a.vs.row + tid] = vn[tid];
+  }
+}
+
+// The splits of a stream's head (blockIdx.x = stream * Hq + head): their weights first,
+// a split a thread, then the outputs, channels side by side.
 template <int NS>
 __global__ void __launch_bounds__(NT) attn_step_join_kernel(StepArgs<NS> a) {
-  __shared__ float red[3][NT];
+  __shared__ float w[MAX_SPLITS], red[NT];
   const int s = blockIdx.x / a.Hq, h = blockIdx.x % a.Hq, tid = threadIdx.x;
-  const float* const part = a.part + (int64_t)blockIdx.x * a.splits * (a.D + 2);
+  const int64_t step = a.D + 2;
+  const float* const part = a.part + (int64_t)blockIdx.x * a.splits * step;
+  float m = -INFINITY, l = 0.f;
+  for (int i = tid; i < a.splits; i += NT) {
+    w[i] = part[i * step + a.D];
+    m = fmaxf(m, w[i]);  // (a split whose scores are NaN has a sum that is)
+  }
+  red[tid] = wave_max(m);
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < NT; i += 64) m = fmaxf(m, red[i]);
+  __syncthreads();
+  const float b = m == -INFINITY ? 0.f : m;
+  for (int i = tid; i < a.splits; i += NT) {
+    w[i] = __builtin_amdgcn_exp2f(w[i] - b);
+    l = fmaf(w[i], part[i * step + a.D + 1], l);
+  }
+  red[tid] = wave_sum(l);
+  __syncthreads();
+  l = 0.f;
+#pragma unroll
+  for (int i = 0; i < NT; i += 64) l += red[i];
+  __syncthreads();
   const int slices = NT / a.D, sl = tid / a.D, ch = tid % a.D;
-  float m = -INFINITY, l = 0.f, v = 0.f, f, f2;
+  float v = 0.f;
   if (sl < slices)
-    for (int i = sl; i < a.splits; i += slices) {
-      const float* const p = part + (int64_t)i * (a.D + 2);
-      join(m, l, p[a.D], p[a.D + 1], f, f2);
-      v = v * f + p[ch] * f2;
-    }
-  red[0][tid] = m;
-  red[1][tid] = l;
-  red[2][tid] = v;
+#pragma unroll 8
+    for (int i = sl; i < a.splits; i += slices) v = fmaf(w[i], part[i * step + ch], v);
+  red[tid] = v;
   __syncthreads();
   if (tid >= a.D) return;
-  for (int i = 1; i < slices; ++i) {
-    const int x = i * a.D + ch;
-    join(m, l, red[0][x], red[1][x], f, f2);
-    v = v * f + red[2][x] * f2;
-  }
+  for (int i = 1; i < slices; ++i) v += red[i * a.D + ch];
   a.o.p[s * a.o.row + h * a.o.head + ch] = Elem<NS>::put(v / l);
 }
 
@@ -205,20 +410,27 @@ int lanes_per_key(int D) {
   return lp;
 }
 
+// bf16 goes to the matrix cores.  fp32 stays on the vector unit, which reads it at 4.6 to
+// 6.7 TB/s with up to four heads to a key head.
 struct Plan {
   int gc, passes, splits;
 };
-// Query heads of a pass: all of the key head's up to eight (registers).  Splits: blocks
-// for four a CU, of at least 256 keys.
-Plan plan(int streams, int64_t cap, int Hq, int Hk, int64_t left, int64_t sinks) {
+// Query heads of a pass: 32 columns, or up to eight (registers).  Splits: blocks for four
+// (bf16) or two a CU, with at least 1024 or 256 rows to each (131,072 rows of 2 heads of
+// 128 channels, bf16: 48 us in parts of 256, 37 of 512, 34 of 1024; one fp32 stream of
+// 262,144: 55 us in 4096 blocks, 47 in 512).
+Plan plan(int type, int streams, int64_t cap, int Hq, int Hk, int64_t left, int64_t sinks) {
   Plan p;
   const int group = Hq / Hk;
-  p.gc = group <= 1 ? 1 : group <= 2 ? 2 : group <= 4 ? 4 : 8;
+  const bool wide = type == SCN_BF16;
+  p.gc = wide ? 32 : group <= 1 ? 1 : group <= 2 ? 2 : group <= 4 ? 4 : 8;
   p.passes = (int)ceil_div(group, p.gc);
   const int64_t ring = cap - sinks;
   const int64_t see = sinks + (left < 0 || left >= ring ? ring : left + 1);
   const int64_t blocks = (int64_t)streams * Hk * p.passes;
-  p.splits = (int)std::max<int64_t>(1, std::min(ceil_div(1024, blocks), ceil_div(see, 256)));
+  const int64_t want = wide ? 1024 : 512, rows = wide ? 1024 : 256;
+  p.splits = (int)std::max<int64_t>(1, std::min({ceil_div(want, blocks), ceil_div(see, rows),
+                                                 (int64_t)MAX_SPLITS}));
   return p;
 }
 
@@ -231,14 +443,31 @@ void launch_gc(const StepArgs<NS>& a, int gc, hipStream_t st) {
   if (gc == 8) hipLaunchKernelGGL((attn_step_kernel<NS, LP, 8>), grid, block, 0, st, a);
 }
 
+template <int DP>
+void launch_wide(const StepArgs<1>& a, hipStream_t st) {
+  hipLaunchKernelGGL(attn_step_wide_kernel<DP>,
+                     dim3((unsigned)(a.splits * a.passes * a.Hk * a.streams)), dim3(NT), 0, st, a);
+}
+
 template <int NS>
 scn_status run(const StepArgs<NS>& a, int gc, hipStream_t st) {
-  switch (lanes_per_key(a.D)) {
-    case 1: launch_gc<NS, 1>(a, gc, st); break;
-    case 2: launch_gc<NS, 2>(a, gc, st); break;
-    case 4: launch_gc<NS, 4>(a, gc, st); break;
-    case 8: launch_gc<NS, 8>(a, gc, st); break;
-    default: launch_gc<NS, 16>(a, gc, st);
+  if constexpr (NS == 1) {
+    if (a.D <= 32)
+      launch_wide<32>(a, st);
+    else if (a.D <= 64)
+      launch_wide<64>(a, st);
+    else if (a.D <= 96)
+      launch_wide<96>(a, st);
+    else
+      launch_wide<128>(a, st);
+  } else {
+    switch (lanes_per_key(a.D)) {
+      case 1: launch_gc<NS, 1>(a, gc, st); break;
+      case 2: launch_gc<NS, 2>(a, gc, st); break;
+      case 4: launch_gc<NS, 4>(a, gc, st); break;
+      case 8: launch_gc<NS, 8>(a, gc, st); break;
+      default: launch_gc<NS, 16>(a, gc, st);
+    }
   }
   SCN_LAUNCH_CHECK();
   if (a.splits > 1) {
@@ -285,12 +514,12 @@ using namespace scn;
 
 extern "C" {
 
-size_t scn_attn_step_workspace_bytes(int32_t streams, int64_t capacity, int32_t D, int32_t Hq,
-                                     int32_t Hk, int64_t left, int64_t sinks) {
-  if (streams < 1 || streams > 65535 || capacity < 1 || capacity > ATTN_ROWS || D < 1 ||
+size_t scn_attn_step_workspace_bytes(int32_t type, int32_t streams, int64_t capacity, int32_t D,
+                                     int32_t Hq, int32_t Hk, int64_t left, int64_t sinks) {
+  if ((type != SCN_F32 && type != SCN_BF16) || streams < 1 || streams > 65535 || capacity < 1 || capacity > ATTN_ROWS || D < 1 ||
       D > ATTN_D || Hk < 1 || Hq < 1 || Hq % Hk != 0 || sinks < 0 || sinks >= capacity)
     return 0;
-  const Plan p = plan(streams, capacity, Hq, Hk, left, sinks);
+  const Plan p = plan(type, streams, capacity, Hq, Hk, left, sinks);
   return p.splits > 1 ? (size_t)streams * Hq * p.splits * (D + 2) * 4 : 0;
 }
 
@@ -319,13 +548,14 @@ scn_status scn_attn_step(int32_t type, int32_t streams, int64_t capacity, int32_
   if (scn_status rc = check_heads(who, "o", o, type)) return rc;
   if (scn_status rc = check_cache(who, "k_cache", k_cache, type)) return rc;
   if (scn_status rc = check_cache(who, "v_cache", v_cache, type)) return rc;
-  const Plan p = plan(streams, capacity, Hq, Hk, left, sinks);
+  const Plan p = plan(type, streams, capacity, Hq, Hk, left, sinks);
   if ((int64_t)streams * Hk * p.passes * p.splits > INT32_MAX || (int64_t)streams * Hq > INT32_MAX) {
     set_error("%s: more than 2^31 blocks of streams and heads", who);
     return SCN_ERR_OVERFLOW;
   }
   if (p.splits > 1 &&
-      (!ws || ws_bytes < scn_attn_step_workspace_bytes(streams, capacity, D, Hq, Hk, left, sinks))) {
+      (!ws || ws_bytes < scn_attn_step_workspace_bytes(type, streams, capacity, D, Hq, Hk, left,
+                                                      sinks))) {
     set_error("%s: workspace missing or too small", who);
     return SCN_ERR_WORKSPACE;
   }

@@ -502,5 +502,5 @@ def test_abi_refuses_before_any_launch(scn):
                           -1, 0, None, None, None) == 4
     assert L.scn_attn_step(0, 1, 2 ** 31, 32, 1, 1, None, None, None, None, None,
                            ctypes.c_void_p(256), 1.0, -1, 0, None, None, 0, None) == 4
-    assert L.scn_attn_step_workspace_bytes(1, i64(4), 32, 1, 1, i64(-1), i64(4)) == 0
+    assert L.scn_attn_step_workspace_bytes(0, 1, i64(4), 32, 1, 1, i64(-1), i64(4)) == 0
     assert L.scn_attn_bwd_workspace_bytes(i64(0), 1, 32, 1, 1, i64(-1), i64(0)) == 0
