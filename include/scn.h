@@ -434,9 +434,9 @@ scn_status scn_site_ranges(const int32_t* coords, int64_t n, int32_t width, int3
  *  type      SCN_F32 or SCN_BF16, of q, k and the results.
  *  n, D, Hq, Hk   rows, channels of a head (a multiple of 8, at most 128),
  *            heads of q and of k (Hk may be 0: k, wk and kr are then not read).
- *  wq, wk    device float[D], or NULL for ones.
+ *  wq, wk    device float[D], 16-byte aligned, or NULL for ones.
  *  coords    device int32[n][width], column 0 (the sample) unused.
- *  freq      device float[D/2], radians per lattice step.
+ *  freq      device float[D/2], 16-byte aligned, radians per lattice step.
  *  sections  host int32[width - 1], each >= 0, of sum <= D/2.
  *  qr, kr    written; may be q and k themselves.
  * Errors: SCN_ERR_INVALID, SCN_ERR_UNSUPPORTED (D), SCN_ERR_OVERFLOW (n above

@@ -13,12 +13,15 @@
 // bf16 planes whose six products stand for one (NS = 3, split.h).
 #pragma once
 
+#include <type_traits>
+
 #include "scn_internal.h"
 #include "split.h"
 
 namespace scn {
 
 typedef short v4s __attribute__((ext_vector_type(4)));
+typedef int v4i __attribute__((ext_vector_type(4)));
 typedef uint32_t v2u __attribute__((ext_vector_type(2)));
 
 template <int NS>
@@ -321,24 +324,37 @@ __device__ inline void load8(const typename Elem<NS>::T* p, float (&v)[8]) {
     }
   }
 }
+// (past: not to be kept in the caches)
 template <int NS>
-__device__ inline void store8(typename Elem<NS>::T* p, const float (&v)[8]) {
+__device__ inline void store8(typename Elem<NS>::T* p, const float (&v)[8], bool past) {
+  auto put = [&](auto x, auto* q) {
+    if (past)
+      __builtin_nontemporal_store(x, q);
+    else
+      *q = x;
+  };
   if constexpr (NS == 1) {
     v4u a;
 #pragma unroll
     for (int j = 0; j < 4; ++j) a[j] = cvt2_bf16(v[2 * j], v[2 * j + 1]);
-    *reinterpret_cast<v4u*>(p) = a;
+    put(a, reinterpret_cast<v4u*>(p));
   } else {
-    *reinterpret_cast<v4f*>(p) = v4f{v[0], v[1], v[2], v[3]};
-    *reinterpret_cast<v4f*>(p + 4) = v4f{v[4], v[5], v[6], v[7]};
+    put(v4f{v[0], v[1], v[2], v[3]}, reinterpret_cast<v4f*>(p));
+    put(v4f{v[4], v[5], v[6], v[7]}, reinterpret_cast<v4f*>(p + 4));
   }
 }
 
-// sum over aligned groups of LP lanes
+// sum over aligned groups of LP <= 16 lanes, in all of them
 template <int LP>
 __device__ inline float group_sum(float v) {
-#pragma unroll
-  for (int d = 1; d < LP; d <<= 1) v += __shfl_xor(v, d);
+  auto add = [&](auto perm) {
+    v += __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(v), decltype(perm)::value, 0xf,
+                                                  0xf, true));
+  };
+  if constexpr (LP >= 2) add(std::integral_constant<int, 0xb1>());   // lanes 1, 0, 3, 2
+  if constexpr (LP >= 4) add(std::integral_constant<int, 0x4e>());   // 2, 3, 0, 1
+  if constexpr (LP >= 8) add(std::integral_constant<int, 0x141>());  // mirrored in eights
+  if constexpr (LP >= 16) add(std::integral_constant<int, 0x140>()); // in sixteens
   return v;
 }
 

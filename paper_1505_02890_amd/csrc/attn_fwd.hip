@@ -7,7 +7,6 @@
 // (its keys along the registers), so the maximum and the sum stay in the lane but for
 // one exchange with the other half, and P^T goes on into O^T += V^T P^T as it is.
 #include <cmath>
-#include <type_traits>
 
 #include "attn.h"
 
