@@ -12,6 +12,7 @@ namespace scn {
 namespace {
 
 constexpr int SPLIT_SINKS = 256;
+constexpr int FEW_KEYS = 64;
 
 template <int NS>
 struct BwdArgs {
@@ -158,10 +159,21 @@ __global__ void __launch_bounds__(64 * QW * KW, NS == 3 && DP > 32 ? 1 : 2)
   delta = both_sum(delta);
   const int64_t at = h * a.n + sp.base + i;
   const float lse2 = a.lse[at] * LOG2E;
-  if (mine && half == 0 && kw == 0) a.delta[at] = delta;
-  v16f dQ[DP / 32];
+  // <do, o> has the rounding of o to bf16, the same for all keys of a row, where the sum of
+  // dS is 0 by definition.  (Left in, dq and dk are off by 1.7 to 3 times their own
+  // rounding where a row sees few keys, 1.5 to 1.7 times elsewhere; without, 1.4 to 1.5,
+  // from dS in bf16.)  Up to 64 channels the sum of dS is kept (`over`), taken off dQ as
+  // over P K at the end, and delta set right for the keys' pass: 140 to 174 us at 60,007
+  // rows of 4 heads, 64 channels, 1025 keys each.  Wider heads lack the registers (478 to
+  // 615 us for the gradients of 30,000 rows of 4 heads, 128 channels): see below.
+  constexpr bool EXACT = NS == 1 && DP <= 64;
+  float over = 0.f;
+  v16f dQ[DP / 32], PK[EXACT ? DP / 32 : 1];
 #pragma unroll
   for (int d = 0; d < DP / 32; ++d) dQ[d] = zero16();
+  if constexpr (EXACT)
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d) PK[d] = zero16();
 
   // the keys, as in the forward
   const int lo = a.w.lo(sp.first), hi = a.w.hi(min(sp.first + QB, sp.m) - 1, sp.m);
@@ -186,12 +198,12 @@ __global__ void __launch_bounds__(64 * QW * KW, NS == 3 && DP > 32 ? 1 : 2)
     sk.store(smem + (t & 1) * 2 * L::BYTES, tid);
     sv.store(smem + (t & 1) * 2 * L::BYTES + L::BYTES, tid);
   };
-  auto take = [&](int t) {
+  // S and dP of the wave's keys of tile t, at kt
+  auto scores = [&](int t, char* kt, v16f& S, v16f& P) {
     const int j0 = first_key(t) + kw * 32;
     const bool sink = t < nst;
-    char* const kt = smem + (t & 1) * 2 * L::BYTES + kw * 32 * DP * 2;
     char* const vt = kt + L::BYTES;
-    v16f S = zero16(), P = zero16();
+    S = P = zero16();
 #pragma unroll
     for (int s = 0; s < DP / 16; ++s) S = mma<NS>(L::rows(kt, pl, 0, s), Q[s], S);
 #pragma unroll
@@ -206,17 +218,40 @@ __global__ void __launch_bounds__(64 * QW * KW, NS == 3 && DP > 32 ? 1 : 2)
         S[r] = ((e <= u) & ((e >= l) | (e < z))) ? S[r] : -INFINITY;
       }
     }
+  };
+  auto tile = [&](int t) { return smem + (t & 1) * 2 * L::BYTES + kw * 32 * DP * 2; };
+  auto take = [&](int t) {
+    char* const kt = tile(t);
+    v16f S, P;
+    Frag<NS> KC[2][DP / 32];  // read early where the registers allow two waves only anyway
+    if constexpr (EXACT) {
 #pragma unroll
-    for (int r = 0; r < 16; ++r)
-      S[r] = __builtin_amdgcn_exp2f(fmaf(S[r], c2, -lse2)) * (P[r] - delta);
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d) KC[s][d] = L::cols(kt, pl, 16 * s, d);
+    }
+    scores(t, kt, S, P);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      S[r] = __builtin_amdgcn_exp2f(fmaf(S[r], c2, -lse2));
+      P[r] = S[r] * (P[r] - delta);
+      if constexpr (EXACT) over += P[r];
+    }
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-      float x[8];
+      float x[8], y[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] = S[8 * s + j];
-      const Frag<NS> X = to_frag<NS>(x);
+      for (int j = 0; j < 8; ++j) {
+        x[j] = S[8 * s + j];
+        y[j] = P[8 * s + j];
+      }
+      const Frag<NS> X = to_frag<NS>(x), Y = to_frag<NS>(y);
 #pragma unroll
-      for (int d = 0; d < DP / 32; ++d) dQ[d] = mma<NS>(L::cols(kt, pl, 16 * s, d), X, dQ[d]);
+      for (int d = 0; d < DP / 32; ++d) {
+        const Frag<NS> K = EXACT ? KC[s][d] : L::cols(kt, pl, 16 * s, d);
+        dQ[d] = mma<NS>(K, Y, dQ[d]);
+        if constexpr (EXACT) PK[d] = mma<NS>(K, X, PK[d]);
+      }
     }
   };
   auto pass = [&](int t) {
@@ -227,27 +262,72 @@ __global__ void __launch_bounds__(64 * QW * KW, NS == 3 && DP > 32 ? 1 : 2)
   const int some = i0 <= i1 && wh - lo >= kw * 32;
   const int e0 = i0 <= i1 ? nst : 0;
   const int s1 = some ? place(wl - lo) : nt, e1 = some ? place(wh - lo) + 1 : nt;
-  fetch(0);
-  put(0);
-  if (nt > 1) fetch(1);
-  __syncthreads();
-  int t = 0;
-  for (int seg = 0; seg < 2; ++seg) {
-    const int s = seg ? s1 : 0, e = seg ? e1 : e0;
-    for (; t < s; ++t) {
-      pass(t);
-      __syncthreads();
-    }
-    for (; t < e; ++t) {
-      pass(t);
-      take(t);
-      __syncthreads();
-    }
-  }
-  for (; t < nt; ++t) {
-    pass(t);
+  auto sweep = [&](auto what) {
+    fetch(0);
+    put(0);
+    if (nt > 1) fetch(1);
     __syncthreads();
+    int t = 0;
+    for (int seg = 0; seg < 2; ++seg) {
+      const int s = seg ? s1 : 0, e = seg ? e1 : e0;
+      for (; t < s; ++t) {
+        pass(t);
+        __syncthreads();
+      }
+      for (; t < e; ++t) {
+        pass(t);
+        what(t);
+        __syncthreads();
+      }
+    }
+    for (; t < nt; ++t) {
+      pass(t);
+      __syncthreads();
+    }
+  };
+  // the sum over the row's groups of keys, in order
+  auto joined = [&](float v) {
+    v = both_sum(v);
+    if constexpr (KW > 1) {
+      float* const x = reinterpret_cast<float*>(smem) + lane;
+      x[wave * 64] = v;
+      __syncthreads();
+      v = 0.f;
+      for (int g = 0; g < KW; ++g) v += x[(g * QW + wave - kw * QW) * 64];
+      __syncthreads();
+    }
+    return v;
+  };
+  // Wide heads: blocks whose first or last row sees few keys (and so the fewest) take the
+  // sum of P dP over that of P for delta, in a sweep of its own.
+  auto keys = [&](int i) { return a.w.hi(i, sp.m) - a.w.lo(i) + 1 + min(a.w.sinks, a.w.lo(i)); };
+  if (NS == 1 && !EXACT && min(keys(sp.first), keys(min(sp.first + QB, sp.m) - 1)) < FEW_KEYS) {
+    float e = 0.f, z = 0.f;
+    sweep([&](int t) {
+      v16f S, P;
+      scores(t, tile(t), S, P);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float p = __builtin_amdgcn_exp2f(fmaf(S[r], c2, -lse2));
+        e = fmaf(p, p == 0.f ? 0.f : P[r], e);  // dP of a masked key may be infinite
+        z += p;
+      }
+    });
+    e = joined(e);
+    z = joined(z);
+    if (fabsf(e / z) < INFINITY) delta = e / z;
   }
+  sweep(take);
+  if constexpr (EXACT) {
+    over = joined(over);
+    over = fabsf(over) < INFINITY ? over : 0.f;
+    delta += over;
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) dQ[d][r] = fmaf(-over, PK[d][r], dQ[d][r]);
+  }
+  if (mine && half == 0 && kw == 0) a.delta[at] = delta;
   if constexpr (KW > 1) {
     float* const x = reinterpret_cast<float*>(smem) + lane;
     if (kw > 0)
@@ -283,8 +363,9 @@ __global__ void __launch_bounds__(64 * QW * KW, NS == 3 && DP > 32 ? 1 : 2)
 }
 
 // What a wave with 32 keys does with 32 queries of a tile: dV += P^T dO, dK += dS^T Q
-// (transposed).  see(i, j) masks the pairs of query i0 + row and key j if `mask`.
-template <int NS, int DP, int TB, class See>
+// (transposed).  see(i, j) masks the pairs of query i0 + row and key j if `mask`.  EARLY
+// reads each pair of products' operands ahead of them, for some 60 registers more.
+template <int NS, int DP, int TB, bool EARLY, class See>
 __device__ inline void key_block(char* qt, char* gt, const typename Tile<NS, DP, TB>::Lane& pl,
                                  const float* lse2, const float* delta, int r0,
                                  const Frag<NS> (&K)[DP / 16], const Frag<NS> (&V)[DP / 16],
@@ -292,11 +373,37 @@ __device__ inline void key_block(char* qt, char* gt, const typename Tile<NS, DP,
                                  v16f (&dV)[DP / 32]) {
   typedef Tile<NS, DP, TB> L;
   const int lane = threadIdx.x & 63, half = lane >> 5;
+  Frag<NS> QR[DP / 16], GR[DP / 16], QC[2][DP / 32], GC[2][DP / 32];
+  v4f ls[4], de[4];
+  auto sums = [&](int g) {
+    ls[g] = *reinterpret_cast<const v4f*>(lse2 + r0 + 8 * g + 4 * half);
+    de[g] = *reinterpret_cast<const v4f*>(delta + r0 + 8 * g + 4 * half);
+  };
+  if constexpr (EARLY) {
+#pragma unroll
+    for (int s = 0; s < DP / 16; ++s) {
+      QR[s] = L::rows(qt, pl, r0, s);
+      GR[s] = L::rows(gt, pl, r0, s);
+    }
+#pragma unroll
+    for (int g = 0; g < 4; ++g) sums(g);
+    __builtin_amdgcn_sched_barrier(0);
+  }
   v16f S = zero16(), P = zero16();
 #pragma unroll
   for (int s = 0; s < DP / 16; ++s) {
-    S = mma<NS>(L::rows(qt, pl, r0, s), K[s], S);
-    P = mma<NS>(L::rows(gt, pl, r0, s), V[s], P);
+    S = mma<NS>(EARLY ? QR[s] : L::rows(qt, pl, r0, s), K[s], S);
+    P = mma<NS>(EARLY ? GR[s] : L::rows(gt, pl, r0, s), V[s], P);
+  }
+  if constexpr (EARLY) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int d = 0; d < DP / 32; ++d) {
+        GC[s][d] = L::cols(gt, pl, r0 + 16 * s, d);
+        QC[s][d] = L::cols(qt, pl, r0 + 16 * s, d);
+      }
+    __builtin_amdgcn_sched_barrier(0);
   }
   if (mask) {
 #pragma unroll
@@ -305,13 +412,12 @@ __device__ inline void key_block(char* qt, char* gt, const typename Tile<NS, DP,
   }
 #pragma unroll
   for (int g = 0; g < 4; ++g) {
-    const v4f l = *reinterpret_cast<const v4f*>(lse2 + r0 + 8 * g + 4 * half);
-    const v4f e = *reinterpret_cast<const v4f*>(delta + r0 + 8 * g + 4 * half);
+    if constexpr (!EARLY) sums(g);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int r = 4 * g + j;
-      S[r] = __builtin_amdgcn_exp2f(fmaf(S[r], c2, -l[j]));
-      P[r] = S[r] * (P[r] - e[j]);
+      S[r] = __builtin_amdgcn_exp2f(fmaf(S[r], c2, -ls[g][j]));
+      P[r] = S[r] * (P[r] - de[g][j]);
     }
   }
 #pragma unroll
@@ -325,8 +431,8 @@ __device__ inline void key_block(char* qt, char* gt, const typename Tile<NS, DP,
     const Frag<NS> X = to_frag<NS>(x), Y = to_frag<NS>(y);
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d) {
-      dV[d] = mma<NS>(L::cols(gt, pl, r0 + 16 * s, d), X, dV[d]);
-      dK[d] = mma<NS>(L::cols(qt, pl, r0 + 16 * s, d), Y, dK[d]);
+      dV[d] = mma<NS>(EARLY ? GC[s][d] : L::cols(gt, pl, r0 + 16 * s, d), X, dV[d]);
+      dK[d] = mma<NS>(EARLY ? QC[s][d] : L::cols(qt, pl, r0 + 16 * s, d), Y, dK[d]);
     }
   }
 }
@@ -407,7 +513,8 @@ __global__ void __launch_bounds__(128, 1) attn_sink_kernel(BwdArgs<NS> a, int ns
       st.fetch(a, sp, hk * a.group + (t + 1) / per, first + (t + 1) % per * TB, end, tid);
     const float* const f = reinterpret_cast<const float*>(smem + 2 * L::BYTES);
     auto see = [&](int r) { return (i0 + r <= end) & (j < i0 + r - a.w.left); };
-    key_block<NS, DP, TB>(smem, smem + L::BYTES, pl, f, f + TB, 32 * wave, K, V, c2, true, see, dK, dV);
+    key_block<NS, DP, TB, false>(smem, smem + L::BYTES, pl, f, f + TB, 32 * wave, K, V, c2, true, see,
+                                 dK, dV);
     __syncthreads();
   }
   // the second wave's sums through LDS, then out
@@ -479,6 +586,9 @@ __global__ void __launch_bounds__(64 * KW * QW, NS == 3 || DP > 64 ? 1 : 2)
     attn_dkv_kernel(BwdArgs<NS> a) {
   typedef KeyShape<NS, DP, KW, QW, U> X;
   constexpr int KB = X::KB, TB = X::TB;
+  // 183 to 174 us at 60,007 rows of 4 heads; narrower heads lose 1%, the others lack the
+  // registers, as do four groups
+  constexpr bool EARLY = NS == 1 && DP == 64 && QW < 4;
   typedef typename X::QT QT;
   typedef typename QT::L L;
   extern __shared__ char smem[];
@@ -548,8 +658,8 @@ __global__ void __launch_bounds__(64 * KW * QW, NS == 3 || DP > 64 ? 1 : 2)
           const int i = i0 - q0 - 32 * u + r;
           return (i <= end) & (j <= i + w.right) & ((j >= i - w.left) | (j < sinks));
         };
-        key_block<NS, DP, TB>(b, b + L::BYTES, pl, f, f + TB, q0 + 32 * u, K, V, c2, !all, see, dK,
-                              dV);
+        key_block<NS, DP, TB, EARLY>(b, b + L::BYTES, pl, f, f + TB, q0 + 32 * u, K, V, c2, !all,
+                                     see, dK, dV);
       }
       __syncthreads();
     }
