@@ -6,6 +6,15 @@
 // Queries' pass, as the forward: S^T = K Q^T and dP^T = V dO^T with a query per lane,
 // dQ^T += K^T dS^T.  Keys' pass: S = Q K^T and dP = dO V^T with a key per lane,
 // dV^T += dO^T P and dK^T += Q^T dS.
+// A third kernel takes the queries that see the sinks from past their window, in
+// shares that a fourth adds up in order.  P and dS are rounded to bf16 for their products
+// (in three parts for fp32), all sums are in fp32.
+//
+// The vector unit and the waits between a tile's steps bound both passes.  60,007 rows, 4
+// heads of 64 channels, bf16, windows of 1025 rows and a sink: queries' pass 174 us,
+// keys' pass 174, sinks 16 and 5.  34,567 rows, 4 heads on 2 of 32 channels, fp32, 256
+// rows back and two sinks: 66, 90, 24 and 5 us.  More keys a barrier (64 for 32), four
+// waves side by side, or three waves a SIMD by spilling measure the same or worse.
 #include "attn.h"
 
 namespace scn {
@@ -801,11 +810,13 @@ scn_status launch_sinks(const BwdArgs<NS>& a, hipStream_t st) {
 }
 
 // The shapes, by measurement (us; queries' pass, keys' pass):
-//  - Two waves by two groups serve most: four waves side by side and no groups are 2 to
-//    4% better in the keys' pass once there are over a thousand blocks of 128 keys
-//    (60,007 rows of 4 heads, 64 channels: 188 against 207), and with more than 64
+//  - Two waves by two groups serve most: four waves side by side and no groups are better
+//    in the keys' pass once there are over a thousand blocks of 128 keys (60,007 rows of 4
+//    heads, 64 channels: 188 against 207 before the reads ahead), and with more than 64
 //    channels, where two groups' tiles and sums crowd the registers (30,000 rows of 2 key
-//    heads, 128 channels: 223 against 272).
+//    heads, 128 channels: 223 against 272).  The queries' pass of wide heads does so from
+//    512 blocks of 128 queries on (both passes: 486 against 502 at 30,000 rows of 4 heads,
+//    165 against 145 at 2000).
 //  - Few blocks, counted against the query heads that each has to take in turn: a wave's
 //    32 keys by four groups (2000 rows of 4 heads: 54 to 27; 32,001 rows, 4 heads on one:
 //    310 to 190).
@@ -821,7 +832,7 @@ scn_status launch(const BwdArgs<NS>& a, hipStream_t st) {
     rc = launch_dq<NS, DP, 4, 2>(a, st);
   } else {
     constexpr int QW = DP > 64 ? 4 : 2, KW = DP > 64 ? 1 : 2;
-    rc = tiles * a.Hq >= 512 ? launch_dq<NS, DP, QW, KW>(a, st) : launch_dq<NS, DP, 2, 2>(a, st);
+    rc = tiles * a.Hq < 512 ? launch_dq<NS, DP, 2, 2>(a, st) : launch_dq<NS, DP, QW, KW>(a, st);
   }
   if (rc) return rc;
   if (a.share && (rc = launch_sinks<NS, DP>(a, st))) return rc;

@@ -1,11 +1,21 @@
 // Attention within samples, forward: one pass over the keys that a tile of queries
 // sees, with the running maximum and sum of the softmax.
 //
-// A block holds QB = 128 consecutive queries of one sample and head, 32 a wave, and
-// takes their keys in tiles of 64 from LDS: first the sinks below the window, then the
-// window from its first key.  Per tile and wave S^T = K Q^T has a query in each lane
-// (its keys along the registers), so the maximum and the sum stay in the lane but for
-// one exchange with the other half, and P^T goes on into O^T += V^T P^T as it is.
+// A block holds 32 QW consecutive queries of one sample and head, 32 a wave, and takes
+// their keys in tiles through two LDS buffers, one tile ahead in registers: first the
+// sinks below the window, then the window from its first key.  Per 32 keys and wave
+// S^T = K Q^T has a query in each lane (its keys along the registers), so the maximum and
+// the sum stay in the lane but for one exchange with the other half, and P^T goes on into
+// O^T += V^T P^T as it is.  bf16: P is rounded to bf16 for that product, which leaves o at
+// most 1.4 times as far off as its own rounding; the sum has the unrounded terms.  fp32:
+// each operand in three bf16 parts, six products.
+//
+// The vector unit bounds it: 32 x 32 scores of 64 channels cost some 74 vector
+// instructions, 400 cycles, beside 256 on the matrix cores.  All pairs of 16,384 rows, 4
+// heads of 64 channels, bf16: 330 us, 834 TFLOP/s; the vector unit issues in 67% of the
+// cycles, the matrix cores are busy in 44%, and neither a third wave, wave priorities nor
+// another order of the instructions gain.  Windows of 1025 rows (60,007 rows, 4 heads):
+// 110 us, 570 TFLOP/s, the rest being masked ends, the sinks' tile and blocks starting.
 #include <cmath>
 
 #include "attn.h"
@@ -327,6 +337,16 @@ scn_status launch(const FwdArgs<NS>& a, hipStream_t st) {
   return SCN_OK;
 }
 
+// The shapes (waves of queries, groups of keys, blocks of 32 keys), by measurement (us):
+//  - Few blocks of 128 queries leave compute units idle: groups share out the keys (4 x
+//    4000 rows, 4 heads of 64, bf16: 19 against 22; 16,384 rows, 2 heads of 128: 297
+//    against 361).  Many do better without (60,007 rows, 4 heads of 64: 110 against 149;
+//    32,001 rows, 2 heads of 128: 79 against 94; fp32, 34,567 rows, 4 heads of 32: 51
+//    against 72), but for fp32 heads of 64, whose operands leave a SIMD one wave (20,000
+//    rows of 4 heads: 224 against 302).
+//  - bf16 up to 64 channels has the registers for 64 keys at a time (32,001 rows of 4
+//    heads: 76 against 83).  Narrower heads do better in small blocks, two waves and 32
+//    keys (160,003 rows of 8 heads of 32, windows of 257 rows: 144 against 169).
 template <int NS, int DP>
 scn_status launch(const FwdArgs<NS>& a, hipStream_t st) {
   const int64_t blocks = (a.n / 128 + a.batch) * a.Hq;
