@@ -15,7 +15,8 @@
 // heads of 64 channels, bf16: 330 us, 834 TFLOP/s; the vector unit issues in 67% of the
 // cycles, the matrix cores are busy in 44%, and neither a third wave, wave priorities nor
 // another order of the instructions gain.  Windows of 1025 rows (60,007 rows, 4 heads):
-// 110 us, 570 TFLOP/s, the rest being masked ends, the sinks' tile and blocks starting.
+// 110 us, 570 TFLOP/s, vector unit 44%, the rest being masked ends, the sinks' tile and
+// blocks starting.
 #include <cmath>
 
 #include "attn.h"
