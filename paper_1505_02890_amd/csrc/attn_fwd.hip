@@ -87,8 +87,11 @@ struct Shape {
   static constexpr size_t SMEM = std::max<size_t>(2 * BUF, (size_t)QW * (KW - 1) * JOIN * 256);
 };
 
+// Two waves a SIMD leave each 256 registers, which all but fp32 heads of more than 96
+// channels do with.  (With 512 the compiler put fp32 sums of 96 channels into accumulation
+// registers, copied them out at the loop's head, and read the last product's too early there.)
 template <int NS, int DP, int QW, int KW, int NB>
-__global__ void __launch_bounds__(64 * QW * KW, NS == 3 && DP > 64 ? 1 : 2)
+__global__ void __launch_bounds__(64 * QW * KW, NS == 3 && DP > 96 ? 1 : 2)
     attn_fwd_kernel(FwdArgs<NS> a) {
   typedef Shape<NS, DP, QW, KW, NB> X;
   typedef typename X::L L;
