@@ -385,6 +385,12 @@ __device__ inline float row_dot(const typename Elem<NS>::T* a, const typename El
   return s;
 }
 
+// A sum of weights is at least 1, and below 2^8 times the keys, but for the rounding of
+// the maximum: the weights are exp2(s c - m) with m rounded and s c not, so all of a row's
+// are off by the same factor, which leaves o and lse as they are.  From scores of 2^31 on
+// that factor passes 2^64, and weights end at 0 or infinity; sums outside these bounds say
+// so (what is lost within them is below 2^-86 of the sum).
+constexpr float SUM_LEAST = 0x1p-40f, SUM_MOST = 0x1p60f;
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f;
 constexpr int ATTN_D = 128;                     // most channels of a head

@@ -305,7 +305,7 @@ __global__ void __launch_bounds__(64 * QW * KW, NS == 3 && DP > 96 ? 1 : 2)
     }
   }
   const float inv = 1.f / sum;
-  bool fine = fabsf(top) < INFINITY && sum < INFINITY;
+  bool fine = fabsf(top) < INFINITY && sum > SUM_LEAST && sum < SUM_MOST;
 #pragma unroll
   for (int d = 0; d < DP / 32; ++d) fine &= finite16(O[d]);
   const bool mine = i0 + n32 < sp.m;
@@ -315,7 +315,8 @@ __global__ void __launch_bounds__(64 * QW * KW, NS == 3 && DP > 96 ? 1 : 2)
     for (int d = 0; d < DP / 32; ++d) store_cols<NS>(o, O[d], inv, d, a.D, lane);
     if (a.lse && half == 0) a.lse[h * a.n + sp.base + i] = (top + log2f(sum)) * LN2;
   }
-  // A term that is infinite or NaN spoils sums it does not enter (0 times it is NaN)
+  // A term that is infinite or NaN spoils sums it does not enter (0 times it is NaN), and
+  // scores past 2^31 lose theirs
   const uint64_t bad = __ballot(mine && !fine);
   uint32_t rows = (uint32_t)bad | (uint32_t)(bad >> 32);
   while (rows) {

@@ -1,0 +1,125 @@
+"""Attention of values far from 1: scores past 2^31, values near the type's largest,
+fp32 operands whose split has no low parts, and infinities that a row sees."""
+from __future__ import annotations
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import attention_reference as ref  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
+E = ref.E
+
+
+@pytest.fixture(scope="module")
+def scn():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_1505_02890_amd as m
+    m.lib()
+    return m
+
+
+def f64(t):
+    torch.cuda.synchronize()
+    return t.detach().double().cpu().numpy()
+
+
+def bounds(lens):
+    return torch.tensor(np.concatenate([[0], np.cumsum(lens)]), dtype=torch.int32, device="cuda")
+
+
+def check(name, got, want, tol):
+    got = f64(got) if isinstance(got, torch.Tensor) else got
+    bad = ~((np.abs(got - want) <= tol) | (got == want) | (np.isnan(got) & np.isnan(want)))
+    if bad.any():
+        i = tuple(np.argwhere(bad)[0])
+        raise AssertionError(f"{name}: {bad.sum()}/{bad.size} outside their bound, the first at "
+                             f"{i}: {got[i]!r} against {want[i]!r}, bound {tol[i]:.3g}")
+
+
+# --------------------------------------------------------------------------
+# large scores
+# --------------------------------------------------------------------------
+# Entries are whole numbers times powers of two, so every score is exact in fp32 and a row's
+# largest ones are equal or 2^e / 4 and more apart: the weights are 1 / (how many are
+# largest) and 0, whatever e is.  Bounds are those of attention_reference with the weights'
+# own error es left at 16 roundings (of the exponential, the sum, its logarithm and
+# their differences), and of <do, o> 2^-15 as where a row sees one key.  The gradients form
+# the weights from log sums in fp32: each is within 3 roundings of it (its own, its
+# product's and the difference's) of its value, which past 8192 would be more than 2^-9.
+# From there on the gradients must not depend on it.
+
+def whole(n, heads, D, seed, exponent, dtype):
+    rng = np.random.default_rng(seed)
+    x = rng.integers(-3, 4, (n, heads, D)) * 2.0 ** exponent
+    return torch.tensor(x, dtype=torch.float32).to(TYPES[dtype]).cuda()
+
+
+def one_hot(q, k, v, lens, see, scale, bf16, do):
+    n, H, D = q.shape
+    K = k.shape[1]
+    u = ref.unit(bf16)
+    val = {"o": np.zeros((n, H, D)), "lse": np.zeros((H, n)), "dq": np.zeros((n, H, D)),
+           "dk": np.zeros((n, K, D)), "dv": np.zeros((n, K, D))}
+    tol = {x: np.zeros_like(a) for x, a in val.items()}
+    at = 0
+    for m in lens:
+        r = slice(at, at + m)
+        at += m
+        es, sums = 16 * E, (np.sqrt(m) + 64) * E
+        for h in range(H):
+            g = h // (H // K)
+            Q, KK, V, G = q[r, h], k[r, g], v[r, g], do[r, h]
+            s = np.where(see(m), scale * (Q @ KK.T), -np.inf)
+            top = s.max(1, keepdims=True)
+            w = np.exp(s - top)
+            z = w.sum(1, keepdims=True)
+            p = w / z
+            o = p @ V
+            val["o"][r, h] = o
+            tol["o"][r, h] = ((u if bf16 else 0) + es + sums) * (p @ np.abs(V)) + u * np.abs(o)
+            val["lse"][h, r] = (top + np.log(z))[:, 0]
+            tol["lse"][h, r] = (4 * E * np.abs(top) + es)[:, 0]
+            dp = G @ V.T
+            ds = p * (dp - (p * dp).sum(1, keepdims=True))
+            mag = np.abs(G) @ np.abs(V).T
+            eg = es + np.where(np.abs(top) > 8192, 0, 3 * E * (np.abs(top) + np.log(z)))
+            eds = eg * np.abs(ds) + p * 2.0 ** -15 * (mag + (p * mag).sum(1, keepdims=True))
+            eds = eds + (u if bf16 else 0) * (np.abs(ds) + eds)
+            ep = p * (eg + sums + (u if bf16 else 0))
+            val["dq"][r, h] = scale * (ds @ KK)
+            tol["dq"][r, h] = scale * (eds + sums * np.abs(ds)) @ np.abs(KK)
+            val["dk"][r, g] += scale * (ds.T @ Q)
+            tol["dk"][r, g] += scale * (eds + sums * np.abs(ds)).T @ np.abs(Q)
+            val["dv"][r, g] += p.T @ G
+            tol["dv"][r, g] += ep.T @ np.abs(G)
+    for x in ("dq", "dk", "dv"):
+        tol[x] += u * (np.abs(val[x]) + tol[x])
+    return val, tol
+
+
+EXPONENTS = [0, 8, 13, 20, 31, 40, 90]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("exponent", EXPONENTS)
+@pytest.mark.parametrize("D,lens,left,right,sinks", [
+    (32, [130, 1, 70], None, None, 0), (64, [300, 41], 60, 3, 2), (128, [200], None, 0, 0)])
+def test_scores_past_the_exponent(scn, dtype, exponent, D, lens, left, right, sinks):
+    n, H, K, scale = sum(lens), 4, 2, 0.25
+    q = whole(n, H, D, 1, exponent - exponent // 2, dtype)
+    k = whole(n, K, D, 2, exponent // 2, dtype)
+    g = torch.Generator().manual_seed(3)
+    v, do = (torch.randn(n, h, D, generator=g).to(TYPES[dtype]).cuda() for h in (K, H))
+    how = dict(left=left, right=right, sinks=sinks, scale=scale)
+    o, lse = scn.attn_fwd(q, k, v, bounds(lens), **how)
+    want, tol = one_hot(f64(q), f64(k), f64(v), lens,
+                        lambda m: ref.visible(m, left, right, sinks), scale, dtype == "bf16",
+                        f64(do))
+    check("o", o, want["o"], tol["o"])
+    check("lse", lse, want["lse"], tol["lse"])
