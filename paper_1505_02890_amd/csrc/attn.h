@@ -385,6 +385,27 @@ __device__ inline float row_dot(const typename Elem<NS>::T* a, const typename El
   return s;
 }
 
+// The softmax of one row that a wave forms again: the largest score and the sum of the
+// weights, a share of the keys per lane.  (A score of NaN makes the sum NaN, and so the
+// weights.)
+struct RowSum {
+  float top = -INFINITY, sum = 0.f;
+  __device__ inline void add(float s) {
+    if (s > top) {
+      sum *= expf(top - s);
+      top = s;
+    }
+    sum += s == -INFINITY ? 0.f : expf(s - top);
+  }
+  // all lanes' shares, in all of them
+  __device__ inline void join() {
+    const float t = wave_max(top);
+    sum = wave_sum(top == -INFINITY ? sum : sum * expf(top - t));
+    top = t;
+  }
+  __device__ inline float weight(float s) const { return expf(s - top) / sum; }
+};
+
 // A sum of weights is at least 1, and below 2^8 times the keys, but for the rounding of
 // the maximum: the weights are exp2(s c - m) with m rounded and s c not, so all of a row's
 // are off by the same factor, which leaves o and lse as they are.  From scores of 2^31 on

@@ -37,8 +37,10 @@ struct FwdArgs {
   Window w;
 };
 
-// One row once more in fp32, over the keys that it sees and no others: two passes over
-// its keys, a key per lane for the scores, channels along the lanes for the sum.
+// One row once more in fp32, over the keys that it sees and no others: the maximum and
+// the sum first, a key per lane, then the values by weights that are divided already
+// (terms before the division may pass fp32's range where the result does not), channels
+// along the lanes.
 template <int NS>
 __device__ inline void fwd_row(const FwdArgs<NS>& a, const Span& sp, int h, int i) {
   typedef Elem<NS> E;
@@ -48,32 +50,25 @@ __device__ inline void fwd_row(const FwdArgs<NS>& a, const Span& sp, int h, int 
   const auto* const v = a.v.p + sp.base * a.v.row + (h / a.group) * a.v.head;
   const int lo = a.w.lo(i), hi = a.w.hi(i, sp.m), ns = min(a.w.sinks, lo);
   const int cnt = ns + hi - lo + 1;  // the keys: [0, ns), then [lo, hi]
-  auto score = [&](int x) -> float {
-    const int j = x < ns ? x : lo + x - ns;
-    return row_dot<NS>(q, k + j * a.k.row, a.D) * a.scale;
-  };
-  float top = -INFINITY, sum = 0.f, o0 = 0.f, o1 = 0.f;
-  bool nan = false;
+  auto key = [&](int x) { return x < ns ? x : lo + x - ns; };
+  auto score = [&](int x) { return row_dot<NS>(q, k + key(x) * a.k.row, a.D) * a.scale; };
+  RowSum r;
+  for (int x = lane; x < cnt; x += 64) r.add(score(x));
+  r.join();
+  float o0 = 0.f, o1 = 0.f;
   for (int x0 = 0; x0 < cnt; x0 += 64) {
-    const float s = x0 + lane < cnt ? score(x0 + lane) : -INFINITY;
-    nan |= s != s;
-    top = fmaxf(top, wave_max(s));
-  }
-  if (__ballot(nan)) top = NAN;
-  for (int x0 = 0; x0 < cnt; x0 += 64) {
-    const float p = x0 + lane < cnt ? expf(score(x0 + lane) - top) : 0.f;
-    sum += wave_sum(p);
+    const float p = x0 + lane < cnt ? r.weight(score(x0 + lane)) : 0.f;
     for (int y = 0; y < min(64, cnt - x0); ++y) {
-      const int x = x0 + y, j = x < ns ? x : lo + x - ns;
+      const auto* const vj = v + key(x0 + y) * a.v.row;
       const float py = __shfl(p, y);
-      if (lane < a.D) o0 = fmaf(py, E::get(v[j * a.v.row + lane]), o0);
-      if (64 + lane < a.D) o1 = fmaf(py, E::get(v[j * a.v.row + 64 + lane]), o1);
+      if (lane < a.D) o0 = fmaf(py, E::get(vj[lane]), o0);
+      if (64 + lane < a.D) o1 = fmaf(py, E::get(vj[64 + lane]), o1);
     }
   }
   auto* const o = a.o.p + (sp.base + i) * a.o.row + h * a.o.head;
-  if (lane < a.D) o[lane] = E::put(o0 / sum);
-  if (64 + lane < a.D) o[64 + lane] = E::put(o1 / sum);
-  if (a.lse && lane == 0) a.lse[h * a.n + sp.base + i] = top + logf(sum);
+  if (lane < a.D) o[lane] = E::put(o0);
+  if (64 + lane < a.D) o[64 + lane] = E::put(o1);
+  if (a.lse && lane == 0) a.lse[h * a.n + sp.base + i] = r.top + logf(r.sum);
 }
 
 // QW waves of 32 queries by KW groups that share out the keys of a tile, 32 NB each

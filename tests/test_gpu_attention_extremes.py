@@ -35,7 +35,9 @@ def bounds(lens):
 
 def check(name, got, want, tol):
     got = f64(got) if isinstance(got, torch.Tensor) else got
-    bad = ~((np.abs(got - want) <= tol) | (got == want) | (np.isnan(got) & np.isnan(want)))
+    with np.errstate(invalid="ignore"):  # inf - inf
+        near = np.abs(got - want) <= tol
+    bad = ~(near | (got == want) | (np.isnan(got) & np.isnan(want)))
     if bad.any():
         i = tuple(np.argwhere(bad)[0])
         raise AssertionError(f"{name}: {bad.sum()}/{bad.size} outside their bound, the first at "
@@ -123,3 +125,81 @@ def test_scores_past_the_exponent(scn, dtype, exponent, D, lens, left, right, si
                         f64(do))
     check("o", o, want["o"], tol["o"])
     check("lse", lse, want["lse"], tol["lse"])
+
+
+# --------------------------------------------------------------------------
+# values near the type's largest: weights are at most 1, but their terms before the
+# division by their sum need not be
+# --------------------------------------------------------------------------
+
+def large_values(n, heads, D, seed, dtype):
+    g = torch.Generator().manual_seed(seed)
+    x = (0.8 + 0.1 * torch.rand(n, heads, D, generator=g)) * torch.finfo(TYPES[dtype]).max
+    x[:, :, 1::2] *= -1
+    return x.to(TYPES[dtype]).cuda()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [32, 64, 128])
+def test_values_near_the_largest(scn, dtype, D):
+    lens, H, K = [200, 1, 33], 2, 1
+    n = sum(lens)
+    g = torch.Generator().manual_seed(5)
+    q, k = (torch.randn(n, h, D, generator=g).to(TYPES[dtype]).cuda() for h in (H, K))
+    v = large_values(n, K, D, 6, dtype)
+    o, lse = scn.attn_fwd(q, k, v, bounds(lens), right=0)
+    want = ref.attention(f64(q), f64(k), f64(v), lens, None, 0, 0, D ** -0.5, dtype == "bf16")
+    check("o", o, *want["o"])
+    check("lse", lse, *want["lse"])
+
+
+# --------------------------------------------------------------------------
+# infinities and NaN that a row sees
+# --------------------------------------------------------------------------
+
+def one_row(q, K, V, scale, bf16):
+    """o [H, D] of one query row on K, V [m, H, D], and its bound: channels that an infinite
+    value enters are infinite, rows with a score of +inf or NaN are NaN, and scores of -inf
+    have no weight."""
+    with np.errstate(invalid="ignore", over="ignore"):
+        s = scale * np.einsum("hd,mhd->hm", q, K)
+        top = s.max(1, keepdims=True)
+        w = np.exp(s - top)
+        w /= w.sum(1, keepdims=True)
+        live = (w != 0)[..., None]
+        Vt = V.transpose(1, 0, 2)
+        terms = np.where(live, w[..., None] * Vt, 0)
+        o = terms.sum(1)
+        fin = np.where(np.isfinite(terms), terms, 0)
+        smag = scale * np.einsum("hd,mhd->hm", np.abs(q), np.where(np.isfinite(K), np.abs(K), 0))
+        es = 2 * (q.shape[1] + 2) * E * smag.max(1) + (
+            2 * np.where(np.isfinite(s), np.abs(s), 0).max(1) + 8) * 4 * E
+    u = ref.unit(bf16)
+    m = K.shape[0]
+    tol = ((2 * es)[:, None] + 2 * (np.sqrt(m) + 64) * E + (u if bf16 else 0)) * np.abs(
+        fin).sum(1) + 1.01 * u * np.abs(np.where(np.isfinite(o), o, 0)) + 1e-30
+    return o, tol
+
+
+INF = float("inf")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [24, 64, 80, 128])
+@pytest.mark.parametrize("what", ["inf", "both", "key"])
+def test_rows_see_infinities(scn, dtype, D, what):
+    n, at = 150, 70
+    t = TYPES[dtype]
+    g = torch.Generator().manual_seed(12)
+    q, k, v = (torch.randn(n, 2, D, generator=g).to(t).cuda() for _ in range(3))
+    if what == "key":
+        k[at, :, 0] = -INF
+    else:
+        v[at, :, 3] = INF
+        if what == "both":
+            v[at // 2, 0, 3] = -INF
+    o, _ = scn.attn_fwd(q, k, v, bounds([n]), right=0)
+    Q, KK, V, got = f64(q), f64(k), f64(v), f64(o)
+    for i in (0, at // 2, at - 1, at, at + 1, n - 1):
+        want, tol = one_row(Q[i], KK[:i + 1], V[:i + 1], D ** -0.5, dtype == "bf16")
+        check(f"o[{i}]", got[i], want, tol)
