@@ -43,6 +43,47 @@ __device__ inline void join(float& m, float& l, float m2, float l2, float& f, fl
   m = t;
 }
 
+// One stream's head once more in fp32, term by term, by one wave: the maximum and the sum
+// first, a key per lane, then the values by their weights, channels along the lanes.  For
+// results that came out infinite or NaN (an infinite value that the token sees, but also
+// one that a weight's low part, or a zero that fills a tile, was multiplied with), and for
+// bf16 scores whose weights all ended at 0 or infinity (attn.h: SUM_LEAST).
+template <int NS>
+__device__ inline void step_row(const StepArgs<NS>& a, int s, int h) {
+  typedef Elem<NS> E;
+  const int lane = threadIdx.x & 63, hk = h / a.group;
+  const int p = min(max(0, a.length[s]), INT32_MAX - 1);
+  const int lo = min(p + 1, max(a.sinks, p - a.reach)), ns = min(a.sinks, p + 1);
+  const int cnt = ns + p - lo + 1, ring = a.cap - a.sinks;
+  const int r0 = lo < a.sinks ? 0 : (lo - a.sinks) % ring;
+  const auto* const q = a.q.p + s * a.q.row + h * a.q.head;
+  // the x-th key's row: the token's own (the last) as it came, the others in the cache
+  auto row = [&](int x, const Ring& r, const typename E::T* cache,
+                 const Heads<const typename E::T>& now) {
+    const int y = r0 + x - ns;
+    const int64_t t = x < ns ? x : a.sinks + (y < ring ? y : y - ring);
+    return x == cnt - 1 ? now.p + s * now.row + hk * now.head
+                        : cache + s * r.stream + hk * r.head + t * r.row;
+  };
+  auto score = [&](int x) { return row_dot<NS>(q, row(x, a.ks, a.kc, a.k), a.D) * a.scale; };
+  RowSum r;
+  for (int x = lane; x < cnt; x += 64) r.add(score(x));
+  r.join();
+  float o0 = 0.f, o1 = 0.f;
+  for (int x0 = 0; x0 < cnt; x0 += 64) {
+    const float w = x0 + lane < cnt ? r.weight(score(x0 + lane)) : 0.f;
+    for (int y = 0; y < min(64, cnt - x0); ++y) {
+      const auto* const v = row(x0 + y, a.vs, a.vc, a.v);
+      const float wy = __shfl(w, y);
+      if (lane < a.D) o0 = fmaf(wy, E::get(v[lane]), o0);
+      if (64 + lane < a.D) o1 = fmaf(wy, E::get(v[64 + lane]), o1);
+    }
+  }
+  auto* const o = a.o.p + s * a.o.row + h * a.o.head;
+  if (lane < a.D) o[lane] = E::put(o0);
+  if (64 + lane < a.D) o[64 + lane] = E::put(o1);
+}
+
 // fp32, on the vector unit: LP lanes hold a key's channels, eight a lane, and take GC query
 // heads of the key head while its row is in registers.  Each group of LP lanes keeps a
 // running maximum, sum and output of its own, which join within the wave and the block.
@@ -53,6 +94,7 @@ __global__ void __launch_bounds__(NT) attn_step_kernel(StepArgs<NS> a) {
   constexpr int KW = 64 / LP;         // keys of a wave at once
   constexpr int KB = KW * (NT / 64);  // ... of the block
   __shared__ float red[NT / 64][GC][LP * 8 + 2];
+  __shared__ bool bad[GC];
   const int split = blockIdx.x % a.splits, pass = blockIdx.x / a.splits % a.passes;
   const int hk = blockIdx.x / a.splits / a.passes % a.Hk;
   const int s = blockIdx.x / a.splits / a.passes / a.Hk;
@@ -146,6 +188,7 @@ __global__ void __launch_bounds__(NT) attn_step_kernel(StepArgs<NS> a) {
       red[wave][g][LP * 8 + 1] = l[g];
     }
   }
+  if (tid < GC) bad[tid] = false;
   __syncthreads();
   for (int i = tid; i < nh * a.D; i += NT) {
     const int g = i / a.D, ch = i % a.D;
@@ -156,7 +199,9 @@ __global__ void __launch_bounds__(NT) attn_step_kernel(StepArgs<NS> a) {
       v = v * f + red[w][g][ch] * f2;
     }
     if (a.splits == 1) {
-      a.o.p[s * a.o.row + (h0 + g) * a.o.head + ch] = E::put(v / ll);
+      v /= ll;
+      red[0][g][ch] = v;
+      if (!(fabsf(v) < INFINITY)) bad[g] = true;
     } else {
       float* const out = a.part + (((int64_t)s * a.Hq + h0 + g) * a.splits + split) * (a.D + 2);
       out[ch] = v;
@@ -165,6 +210,15 @@ __global__ void __launch_bounds__(NT) attn_step_kernel(StepArgs<NS> a) {
         out[a.D + 1] = ll;
       }
     }
+  }
+  if (a.splits == 1) {
+    __syncthreads();
+    for (int i = tid; i < nh * a.D; i += NT) {
+      const int g = i / a.D, ch = i % a.D;
+      if (!bad[g]) a.o.p[s * a.o.row + (h0 + g) * a.o.head + ch] = E::put(red[0][g][ch]);
+    }
+    for (int g = wave; g < nh; g += NT / 64)
+      if (bad[g]) step_row<NS>(a, s, h0 + g);
   }
   // The new rows go to the cache.  No block reads that row: what it held is a
   // capacity's ring before the new token, past the reach.
@@ -324,6 +378,7 @@ __global__ void __launch_bounds__(NT, 2) attn_step_wide_kernel(StepArgs<1> a) {
   }
   __syncthreads();
   if (wave == 0) {
+    bool fine = true;
     for (int g = 0; g < WAVES - 1; ++g) {
       const float* const o = x + g * JOIN * 64;
       float f, f2;
@@ -337,8 +392,12 @@ __global__ void __launch_bounds__(NT, 2) attn_step_wide_kernel(StepArgs<1> a) {
       if (a.splits == 1) {
         const float inv = 1.f / sum;
         T* const o = a.o.p + s * a.o.row + (h0 + n32) * a.o.head;
+        fine = fabsf(top) < INFINITY && sum > SUM_LEAST && sum < SUM_MOST;
 #pragma unroll
-        for (int d = 0; d < DP / 32; ++d) store_cols<1>(o, O[d], inv, d, a.D, lane);
+        for (int d = 0; d < DP / 32; ++d) {
+          fine &= finite16(O[d]);
+          store_cols<1>(o, O[d], inv, d, a.D, lane);
+        }
       } else {
         float* const o =
             a.part + (((int64_t)s * a.Hq + h0 + n32) * a.splits + split) * (a.D + 2);
@@ -355,6 +414,9 @@ __global__ void __launch_bounds__(NT, 2) attn_step_wide_kernel(StepArgs<1> a) {
         }
       }
     }
+    const uint64_t bad = __ballot(!fine);
+    uint32_t heads = (uint32_t)bad | (uint32_t)(bad >> 32);
+    for (; heads; heads &= heads - 1) step_row<1>(a, s, h0 + __builtin_ctz(heads));
   }
   if (split == 0 && pass == 0 && tid < a.D) {
     const int64_t r = p < a.sinks ? p : a.sinks + (p - a.sinks) % ring;
@@ -399,9 +461,17 @@ __global__ void __launch_bounds__(NT) attn_step_join_kernel(StepArgs<NS> a) {
     for (int i = sl; i < a.splits; i += slices) v = fmaf(w[i], part[i * step + ch], v);
   red[tid] = v;
   __syncthreads();
-  if (tid >= a.D) return;
-  for (int i = 1; i < slices; ++i) v += red[i * a.D + ch];
-  a.o.p[s * a.o.row + h * a.o.head + ch] = Elem<NS>::put(v / l);
+  bool fine = true;
+  if (tid < a.D) {
+    for (int i = 1; i < slices; ++i) v += red[i * a.D + ch];
+    v /= l;
+    fine = fabsf(v) < INFINITY && l > SUM_LEAST && l < SUM_MOST;
+  }
+  if (__syncthreads_or(!fine)) {
+    if (tid < 64) step_row<NS>(a, s, h);
+  } else if (tid < a.D) {
+    a.o.p[s * a.o.row + h * a.o.head + ch] = Elem<NS>::put(v);
+  }
 }
 
 int lanes_per_key(int D) {

@@ -127,6 +127,28 @@ def test_scores_past_the_exponent(scn, dtype, exponent, D, lens, left, right, si
     check("lse", lse, want["lse"], tol["lse"])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("exponent", EXPONENTS)
+@pytest.mark.parametrize("H,K,D,cap,length", [(4, 2, 64, 300, 299), (3, 1, 40, 5000, 4998),
+                                              (1, 1, 128, 40, 0)])
+def test_steps_of_scores_past_the_exponent(scn, dtype, exponent, H, K, D, cap, length):
+    q = whole(1, H, D, 1, exponent - exponent // 2, dtype)
+    kc = whole(cap, K, D, 2, exponent // 2, dtype)
+    k = whole(1, K, D, 4, exponent // 2, dtype)
+    g = torch.Generator().manual_seed(3)
+    vc, v = (torch.randn(m, K, D, generator=g).to(TYPES[dtype]).cuda() for m in (cap, 1))
+    o = scn.attn_step(q, k, v, kc[None], vc[None],
+                      torch.tensor([length], dtype=torch.int32, device="cuda"), scale=0.25)
+    m = length + 1
+    s = 0.25 * np.einsum("hd,mhd->hm", f64(q)[0], np.repeat(f64(kc)[:m], H // K, 1))
+    w = np.exp(s - s.max(1, keepdims=True))
+    w /= w.sum(1, keepdims=True)
+    V = np.repeat(f64(vc)[:m], H // K, 1)
+    u = ref.unit(dtype == "bf16")
+    want, mag = np.einsum("hm,mhd->hd", w, V), np.einsum("hm,mhd->hd", w, np.abs(V))
+    check("o", o, want[None], ((16 + np.sqrt(m) + 64) * E * mag + u * np.abs(want))[None])
+
+
 # --------------------------------------------------------------------------
 # values near the type's largest: weights are at most 1, but their terms before the
 # division by their sum need not be
@@ -151,6 +173,21 @@ def test_values_near_the_largest(scn, dtype, D):
     want = ref.attention(f64(q), f64(k), f64(v), lens, None, 0, 0, D ** -0.5, dtype == "bf16")
     check("o", o, *want["o"])
     check("lse", lse, *want["lse"])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D,cap,length", [(64, 200, 199), (40, 5000, 4999)])
+def test_steps_of_values_near_the_largest(scn, dtype, D, cap, length):
+    H, K = 4, 2
+    g = torch.Generator().manual_seed(7)
+    q, k, kc = (torch.randn(m, h, D, generator=g).to(TYPES[dtype]).cuda()
+                for m, h in ((1, H), (1, K), (cap, K)))
+    v, vc = large_values(1, K, D, 8, dtype), large_values(cap, K, D, 9, dtype)
+    want, tol = ref.step(f64(q), f64(k), f64(v), f64(kc)[None], f64(vc)[None], [length], None, 0,
+                         D ** -0.5, dtype == "bf16")
+    o = scn.attn_step(q, k, v, kc[None], vc[None],
+                      torch.tensor([length], dtype=torch.int32, device="cuda"))
+    check("o", o, want, tol)
 
 
 # --------------------------------------------------------------------------
@@ -182,6 +219,31 @@ def one_row(q, K, V, scale, bf16):
 
 
 INF = float("inf")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [24, 40, 64, 80, 128])
+@pytest.mark.parametrize("cap,at", [(50, 49), (50, 10), (4000, 1234), (4000, 3999)])
+@pytest.mark.parametrize("what", ["inf", "-inf", "both", "nan", "key"])
+def test_steps_see_infinities(scn, dtype, D, cap, at, what):
+    H = K = 2
+    t = TYPES[dtype]
+    g = torch.Generator().manual_seed(11)
+    q, kc, vc = (torch.randn(m, h, D, generator=g).to(t).cuda()
+                 for m, h in ((1, H), (cap, K), (cap, K)))
+    if what == "key":  # an infinite first channel: no weight for the first head, NaN for the other
+        kc[at, :, 0] = -torch.sign(q[0, :, 0]) * INF
+        kc[at, 1, 0] *= -1
+    elif what == "both":  # of both signs in one channel
+        vc[at, :, 3], vc[at // 2, :, 3] = INF, -INF
+    else:
+        vc[at, :, 3] = {"inf": INF, "-inf": -INF, "nan": float("nan")}[what]
+        vc[at, 0, D - 1] = -INF
+    want, tol = one_row(f64(q)[0], f64(kc), f64(vc), D ** -0.5, dtype == "bf16")
+    k, v = kc[cap - 1:].clone(), vc[cap - 1:].clone()  # the new token's
+    o = scn.attn_step(q, k, v, kc[None], vc[None],
+                      torch.tensor([cap - 1], dtype=torch.int32, device="cuda"))
+    check("o", o, want[None], tol[None])
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
