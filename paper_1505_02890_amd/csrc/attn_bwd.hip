@@ -21,7 +21,6 @@ namespace scn {
 namespace {
 
 constexpr int SPLIT_SINKS = 256;
-constexpr int FEW_KEYS = 64;
 
 template <int NS>
 struct BwdArgs {
@@ -169,14 +168,15 @@ __global__ void __launch_bounds__(64 * QW * KW, NS == 3 && DP > 32 ? 1 : 2)
   const int64_t at = h * a.n + sp.base + i;
   const float lse2 = a.lse[at] * LOG2E;
   // <do, o> has the rounding of o to bf16, the same for all keys of a row, where the sum of
-  // dS is 0 by definition.  (Left in, dq and dk are off by 1.7 to 3 times their own
-  // rounding where a row sees few keys, 1.5 to 1.7 times elsewhere; without, 1.4 to 1.5,
-  // from dS in bf16.)  Up to 64 channels the sum of dS is kept (`over`), taken off dQ as
-  // over P K at the end, and delta set right for the keys' pass: 140 to 174 us at 60,007
-  // rows of 4 heads, 64 channels, 1025 keys each.  Wider heads lack the registers (478 to
-  // 615 us for the gradients of 30,000 rows of 4 heads, 128 channels): see below.
-  constexpr bool EXACT = NS == 1 && DP <= 64;
-  float over = 0.f;
+  // dS is 0 by definition.  (Left in, dq and dk are off by 1.7 to 4 times their own rounding
+  // where a row sees few keys or few of its keys hold its weight.)  The sum of dS is
+  // kept (`over`) and sets delta right for the keys' pass.  Up to 64 channels it is taken off
+  // dQ as over P K at the end: 140 to 174 us at 60,007 rows of 4 heads, 64 channels, 1025
+  // keys each.  Wider heads lack the registers (478 to 615 us for the gradients of 30,000
+  // rows of 4 heads, 128 channels): blocks with a row where it counts take their keys again
+  // with the delta set right.
+  constexpr bool EXACT = NS == 1 && DP <= 64, AGAIN = NS == 1 && DP > 64;
+  float over = 0.f, size = 0.f;
   v16f dQ[DP / 32], PK[EXACT ? DP / 32 : 1];
 #pragma unroll
   for (int d = 0; d < DP / 32; ++d) dQ[d] = zero16();
@@ -244,7 +244,8 @@ __global__ void __launch_bounds__(64 * QW * KW, NS == 3 && DP > 32 ? 1 : 2)
     for (int r = 0; r < 16; ++r) {
       S[r] = __builtin_amdgcn_exp2f(fmaf(S[r], c2, -lse2));
       P[r] = S[r] * (P[r] - delta);
-      if constexpr (EXACT) over += P[r];
+      if constexpr (EXACT || AGAIN) over += P[r];
+      if constexpr (AGAIN) size += fabsf(P[r]);
     }
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
@@ -307,25 +308,6 @@ __global__ void __launch_bounds__(64 * QW * KW, NS == 3 && DP > 32 ? 1 : 2)
     }
     return v;
   };
-  // Wide heads: blocks whose first or last row sees few keys (and so the fewest) take the
-  // sum of P dP over that of P for delta, in a sweep of its own.
-  auto keys = [&](int i) { return a.w.hi(i, sp.m) - a.w.lo(i) + 1 + min(a.w.sinks, a.w.lo(i)); };
-  if (NS == 1 && !EXACT && min(keys(sp.first), keys(min(sp.first + QB, sp.m) - 1)) < FEW_KEYS) {
-    float e = 0.f, z = 0.f;
-    sweep([&](int t) {
-      v16f S, P;
-      scores(t, tile(t), S, P);
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const float p = __builtin_amdgcn_exp2f(fmaf(S[r], c2, -lse2));
-        e = fmaf(p, p == 0.f ? 0.f : P[r], e);  // dP of a masked key may be infinite
-        z += p;
-      }
-    });
-    e = joined(e);
-    z = joined(z);
-    if (fabsf(e / z) < INFINITY) delta = e / z;
-  }
   sweep(take);
   if constexpr (EXACT) {
     over = joined(over);
@@ -335,6 +317,18 @@ __global__ void __launch_bounds__(64 * QW * KW, NS == 3 && DP > 32 ? 1 : 2)
     for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
       for (int r = 0; r < 16; ++r) dQ[d][r] = fmaf(-over, PK[d][r], dQ[d][r]);
+  }
+  if constexpr (AGAIN) {
+    over = joined(over);
+    size = joined(size);
+    if (fabsf(over) < INFINITY) delta += over;
+    // The threshold is what the rounding of dS leaves of it: rows of scores of N(0, 1.5)
+    // and 512 keys stay below, with N(0, 2) one in 200 is above, with N(0, 4) one in five.
+    if (__syncthreads_or(fabsf(over) > 0x1p-9f * size)) {
+#pragma unroll
+      for (int d = 0; d < DP / 32; ++d) dQ[d] = zero16();
+      sweep(take);
+    }
   }
   if (mine && half == 0 && kw == 0) a.delta[at] = delta;
   if constexpr (KW > 1) {
