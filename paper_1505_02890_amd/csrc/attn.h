@@ -412,6 +412,10 @@ struct RowSum {
 // that factor passes 2^64, and weights end at 0 or infinity; sums outside these bounds say
 // so (what is lost within them is below 2^-86 of the sum).
 constexpr float SUM_LEAST = 0x1p-40f, SUM_MOST = 0x1p60f;
+// The backward passes form weights from log sums in fp32, each off by up to some 2^-23 of its
+// log sum relatively.  Rows past this bound (2^-10 so) are formed again, from their own
+// scores' maximum and sum.
+constexpr float LSE_MOST = 8192.f;
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f;
 constexpr int ATTN_D = 128;                     // most channels of a head

@@ -32,42 +32,54 @@ struct BwdArgs {
   Heads<T> dq, dk, dv;
   const float* lse;  // [Hq][n]
   float* delta;      // [Hq][n]
+  float* lse2;       // [Hq][n]: lse in log 2, or NaN where it is past LSE_MOST ...
+  float* rest;       // [Hq][n]: ... and what it lacks there
   float* share;      // the sinks' shares [chunk][Hk][sinks][2][D], or null
   int sc;            // queries of a share
   float scale;
   Window w;
 };
 
-// dq of one row once more in fp32, over the keys that it sees
+// dq of one row once more in fp32, over the keys that it sees, from weights of its own.
+// The keys' pass gets their delta, and what the row's lse is short of their log sum.
 template <int NS>
-__device__ inline void dq_row(const BwdArgs<NS>& a, const Span& sp, int h, int i, float delta) {
+__device__ inline void dq_row(const BwdArgs<NS>& a, const Span& sp, int h, int i) {
   typedef Elem<NS> E;
   const int lane = threadIdx.x & 63;
   const auto* const q = a.q.p + (sp.base + i) * a.q.row + h * a.q.head;
   const auto* const g = a.d_o.p + (sp.base + i) * a.d_o.row + h * a.d_o.head;
   const auto* const k = a.k.p + sp.base * a.k.row + (h / a.group) * a.k.head;
   const auto* const v = a.v.p + sp.base * a.v.row + (h / a.group) * a.v.head;
-  const float lse = a.lse[h * a.n + sp.base + i];
   const int lo = a.w.lo(i), hi = a.w.hi(i, sp.m), ns = min(a.w.sinks, lo);
   const int cnt = ns + hi - lo + 1;
+  auto key = [&](int x) { return x < ns ? x : lo + x - ns; };
+  auto score = [&](int x) { return row_dot<NS>(q, k + key(x) * a.k.row, a.D) * a.scale; };
+  auto dp = [&](int x) { return row_dot<NS>(g, v + key(x) * a.v.row, a.D); };
+  RowSum r;
+  for (int x = lane; x < cnt; x += 64) r.add(score(x));
+  r.join();
+  float delta = 0.f;
+  for (int x = lane; x < cnt; x += 64) delta = fmaf(r.weight(score(x)), dp(x), delta);
+  delta = wave_sum(delta);
   float o0 = 0.f, o1 = 0.f;
   for (int x0 = 0; x0 < cnt; x0 += 64) {
-    float ds = 0.f;
-    if (x0 + lane < cnt) {
-      const int x = x0 + lane, j = x < ns ? x : lo + x - ns;
-      const float p = expf(row_dot<NS>(q, k + j * a.k.row, a.D) * a.scale - lse);
-      ds = p * (row_dot<NS>(g, v + j * a.v.row, a.D) - delta);
-    }
+    const int x = x0 + lane;
+    const float ds = x < cnt ? r.weight(score(x)) * (dp(x) - delta) : 0.f;
     for (int y = 0; y < min(64, cnt - x0); ++y) {
-      const int x = x0 + y, j = x < ns ? x : lo + x - ns;
+      const auto* const kj = k + key(x0 + y) * a.k.row;
       const float d = __shfl(ds, y);
-      if (lane < a.D) o0 = fmaf(d, E::get(k[j * a.k.row + lane]), o0);
-      if (64 + lane < a.D) o1 = fmaf(d, E::get(k[j * a.k.row + 64 + lane]), o1);
+      if (lane < a.D) o0 = fmaf(d, E::get(kj[lane]), o0);
+      if (64 + lane < a.D) o1 = fmaf(d, E::get(kj[64 + lane]), o1);
     }
   }
   auto* const o = a.dq.p + (sp.base + i) * a.dq.row + h * a.dq.head;
   if (lane < a.D) o[lane] = E::put(o0 * a.scale);
   if (64 + lane < a.D) o[64 + lane] = E::put(o1 * a.scale);
+  if (lane == 0) {
+    const int64_t at = h * a.n + sp.base + i;
+    a.delta[at] = delta;
+    a.rest[at] = (r.top - a.lse[at]) + logf(r.sum);
+  }
 }
 
 // dk and dv of one row once more in fp32, over the queries that see it
@@ -88,7 +100,8 @@ __device__ inline void dkv_row(const BwdArgs<NS>& a, const Span& sp, int hk, int
       const int i = x0 + lane;
       if (i <= hi) {
         const int64_t at = h * a.n + sp.base + i;
-        p = expf(row_dot<NS>(q + i * a.q.row, k, a.D) * a.scale - a.lse[at]);
+        p = row_dot<NS>(q + i * a.q.row, k, a.D) * a.scale - a.lse[at];
+        p = expf(fabsf(a.lse[at]) <= LSE_MOST ? p : p - a.rest[at]);
         ds = p * (row_dot<NS>(g + i * a.d_o.row, v, a.D) - a.delta[at]);
       }
       for (int y = 0; y < min(64, hi - x0 + 1); ++y) {
@@ -167,6 +180,7 @@ __global__ void __launch_bounds__(64 * QW * KW, NS == 3 && DP > 32 ? 1 : 2)
   delta = both_sum(delta);
   const int64_t at = h * a.n + sp.base + i;
   const float lse2 = a.lse[at] * LOG2E;
+  const bool far = !(fabsf(a.lse[at]) <= LSE_MOST);  // the row is formed again
   // <do, o> has the rounding of o to bf16, the same for all keys of a row, where the sum of
   // dS is 0 by definition.  (Left in, dq and dk are off by 1.7 to 4 times their own rounding
   // where a row sees few keys or few of its keys hold its weight.)  The sum of dS is
@@ -330,7 +344,10 @@ __global__ void __launch_bounds__(64 * QW * KW, NS == 3 && DP > 32 ? 1 : 2)
       sweep(take);
     }
   }
-  if (mine && half == 0 && kw == 0) a.delta[at] = delta;
+  if (mine && half == 0 && kw == 0) {
+    a.delta[at] = delta;
+    a.lse2[at] = far ? NAN : lse2;  // keys that see the row are formed again
+  }
   if constexpr (KW > 1) {
     float* const x = reinterpret_cast<float*>(smem) + lane;
     if (kw > 0)
@@ -356,13 +373,9 @@ __global__ void __launch_bounds__(64 * QW * KW, NS == 3 && DP > 32 ? 1 : 2)
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d) store_cols<NS>(o, dQ[d], a.scale, d, a.D, lane);
   }
-  const uint64_t bad = __ballot(mine && !fine);
+  const uint64_t bad = __ballot(mine && (far || !fine));
   uint32_t rows = (uint32_t)bad | (uint32_t)(bad >> 32);
-  while (rows) {
-    const int r = __builtin_ctz(rows);
-    rows &= rows - 1;
-    dq_row<NS>(a, sp, h, i0 + r, __shfl(delta, r));
-  }
+  for (; rows; rows &= rows - 1) dq_row<NS>(a, sp, h, i0 + __builtin_ctz(rows));
 }
 
 // What a wave with 32 keys does with 32 queries of a tile: dV += P^T dO, dK += dS^T Q
@@ -459,7 +472,7 @@ struct QueryTiles {
     g.load(a.d_o.p + sp.base * a.d_o.row + h * a.d_o.head, a.d_o.row, go, i0, last + 1 - i0, a.D);
     if (tid < TB) {
       const int64_t at = h * a.n + sp.base + min(i0 + tid, last);
-      lse2 = a.lse[at] * LOG2E;
+      lse2 = a.lse2[at];
       delta = a.delta[at];
     }
   }
@@ -865,7 +878,7 @@ size_t scn_attn_bwd_workspace_bytes(int64_t n, int32_t batch, int32_t D, int32_t
                                     int64_t left, int64_t sinks) {
   if (n <= 0 || n > ATTN_ROWS || batch < 1 || D < 1 || D > ATTN_D || Hq < 1 || Hk < 1 || sinks < 0)
     return 0;
-  int64_t f = delta_floats(n, Hq);
+  int64_t f = 3 * delta_floats(n, Hq);
   if (split_sinks(n, left, sinks))
     f += sink_chunks(n, batch) * Hk * std::min(sinks, n) * 2 * D;
   return (size_t)f * 4;
@@ -898,20 +911,22 @@ scn_status scn_attn_bwd(int32_t type, int64_t n, int32_t batch, const int32_t* r
     return SCN_ERR_WORKSPACE;
   }
   float* const delta = static_cast<float*>(ws);
-  float* const share = split_sinks(n, left, sinks) ? delta + delta_floats(n, Hq) : nullptr;
+  float* const lse2 = delta + delta_floats(n, Hq);
+  float* const rest = lse2 + delta_floats(n, Hq);
+  float* const share = split_sinks(n, left, sinks) ? rest + delta_floats(n, Hq) : nullptr;
   const Window w{bound(left, n), bound(right, n), bound(sinks, n)};
   if (type == SCN_BF16) {
     typedef uint16_t T;
     return run<1>(BwdArgs<1>{n, batch, D, Hq, Hk, Hq / Hk, ranges, view<const T>(q),
                              view<const T>(k), view<const T>(v), view<const T>(o),
                              view<const T>(d_o), view<T>(dq), view<T>(dk), view<T>(dv), lse, delta,
-                             share, share_rows(n), scale, w}, st);
+                             lse2, rest, share, share_rows(n), scale, w}, st);
   }
   typedef float T;
   return run<3>(BwdArgs<3>{n, batch, D, Hq, Hk, Hq / Hk, ranges, view<const T>(q),
                            view<const T>(k), view<const T>(v), view<const T>(o),
                            view<const T>(d_o), view<T>(dq), view<T>(dk), view<T>(dv), lse, delta,
-                           share, share_rows(n), scale, w}, st);
+                           lse2, rest, share, share_rows(n), scale, w}, st);
 }
 
 }  // extern "C"

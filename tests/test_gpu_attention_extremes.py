@@ -102,7 +102,7 @@ def one_hot(q, k, v, lens, see, scale, bf16, do):
             tol["dv"][r, g] += ep.T @ np.abs(G)
     for x in ("dq", "dk", "dv"):
         tol[x] += u * (np.abs(val[x]) + tol[x])
-    return val, tol
+    return val, {x: t + 1e-30 for x, t in tol.items()}  # (fp32 ends at 1e-45)
 
 
 EXPONENTS = [0, 8, 13, 20, 31, 40, 90]
@@ -125,6 +125,29 @@ def test_scores_past_the_exponent(scn, dtype, exponent, D, lens, left, right, si
                         f64(do))
     check("o", o, want["o"], tol["o"])
     check("lse", lse, want["lse"], tol["lse"])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("exponent", EXPONENTS)
+@pytest.mark.parametrize("D,lens,left,right,sinks", [
+    (32, [130, 1, 70], None, None, 0), (64, [300, 41], 60, 3, 2), (128, [200], None, 0, 0),
+    (32, [400], 10, 0, 2)])
+def test_gradients_of_scores_past_the_exponent(scn, dtype, exponent, D, lens, left, right, sinks):
+    n, H, K, scale = sum(lens), 4, 2, 0.25
+    q = whole(n, H, D, 1, exponent - exponent // 2, dtype)
+    k = whole(n, K, D, 2, exponent // 2, dtype)
+    g = torch.Generator().manual_seed(3)
+    v, do = (torch.randn(n, h, D, generator=g).to(TYPES[dtype]).cuda() for h in (K, H))
+    how = dict(left=left, right=right, sinks=sinks, scale=scale)
+    want, tol = one_hot(f64(q), f64(k), f64(v), lens,
+                        lambda m: ref.visible(m, left, right, sinks), scale, dtype == "bf16",
+                        f64(do))
+    # o and lse as a forward rounds them
+    o = torch.tensor(want["o"], dtype=torch.float32).to(TYPES[dtype]).cuda()
+    lse = torch.tensor(want["lse"], dtype=torch.float32).cuda()
+    d = scn.attn_bwd(q, k, v, o, lse, do, bounds(lens), **how)
+    for x in ("dq", "dk", "dv"):
+        check(x, d[x], want[x], tol[x])
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
