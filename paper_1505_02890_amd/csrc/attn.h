@@ -365,6 +365,21 @@ __device__ inline bool finite16(const v16f& v) {
   return s == 0.f;
 }
 
+// Whether the row's results (v times f, f positive; both halves hold some) are so small that their
+// fp32 operands may have lost low parts (split.h): nothing of 2^-95 or more, and not zero.
+// A larger one says that what was lost is below 2^-38 of it, as scores say of theirs:
+// they are off by what is below 2^-133 of a query, times its keys.
+template <int N>
+__device__ inline bool tiny(const v16f (&v)[N], float f) {
+  float m = 0.f;
+#pragma unroll
+  for (int d = 0; d < N; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) m = larger(m, fabsf(v[d][r]));
+  m = both_larger(m);
+  return m > 0.f && m * f < 0x1p-95f;
+}
+
 __device__ inline float wave_max(float v) {
 #pragma unroll
   for (int d = 32; d; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));

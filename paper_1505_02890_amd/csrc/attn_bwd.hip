@@ -368,6 +368,7 @@ __global__ void __launch_bounds__(64 * QW * KW, NS == 3 && DP > 32 ? 1 : 2)
   bool fine = true;
 #pragma unroll
   for (int d = 0; d < DP / 32; ++d) fine &= finite16(dQ[d]);
+  if constexpr (NS == 3) fine &= !tiny(dQ, 1.f);
   if (mine) {
     auto* const o = a.dq.p + (sp.base + i) * a.dq.row + h * a.dq.head;
 #pragma unroll
@@ -732,6 +733,7 @@ __global__ void __launch_bounds__(64 * KW * QW, NS == 3 || DP > 64 ? 1 : 2)
   bool fine = true;
 #pragma unroll
   for (int d = 0; d < DP / 32; ++d) fine &= finite16(dK[d]) && finite16(dV[d]);
+  if constexpr (NS == 3) fine &= !tiny(dK, 1.f) && !tiny(dV, 1.f);
   if (mine) {
     auto* const dk = a.dk.p + (sp.base + j) * a.dk.row + hk * a.dk.head;
     auto* const dv = a.dv.p + (sp.base + j) * a.dv.row + hk * a.dv.head;

@@ -288,3 +288,41 @@ def test_rows_see_infinities(scn, dtype, D, what):
     for i in (0, at // 2, at - 1, at, at + 1, n - 1):
         want, tol = one_row(Q[i], KK[:i + 1], V[:i + 1], D ** -0.5, dtype == "bf16")
         check(f"o[{i}]", got[i], want, tol)
+
+
+# --------------------------------------------------------------------------
+# fp32 values whose parts in bf16 end early: bf16 holds nothing below 2^-133, so a value of
+# 2^-112 keeps 21 bits of 24, and one of 2^-125 eight
+# --------------------------------------------------------------------------
+
+@pytest.mark.parametrize("power", [-112, -120, -124])
+@pytest.mark.parametrize("D,lens,left,right,sinks", [
+    (32, [130, 1, 70], None, 0, 0), (64, [300, 41], 60, 3, 2), (128, [200], None, None, 0),
+    (24, [400], 10, 0, 2)])
+def test_tiny_values_keep_their_bits(scn, D, lens, left, right, sinks, power):
+    # values and gradients scaled by a power of two: results scale with them (but for what
+    # lies below the smallest fp32)
+    n, H, K = sum(lens), 2, 1
+    up, floor = 2.0 ** -power, 2.0 ** -149 * 2.0 ** -power
+    g = torch.Generator().manual_seed(14)
+    q, k = (torch.randn(n, h, D, generator=g).cuda() for h in (H, K))
+    v = torch.randn(n, K, D, generator=g)
+    do = torch.randn(n, H, D, generator=g).cuda()
+    small = (v.double() * 2.0 ** power).float()
+    how = dict(left=left, right=right, sinks=sinks)
+    o, _ = scn.attn_fwd(q, k, small.cuda(), bounds(lens), **how)
+    args = (lens, left, right, sinks, D ** -0.5, False)
+    want = ref.attention(f64(q), f64(k), small.double().numpy() * up, *args)
+    check("o", f64(o) * up, want["o"][0], want["o"][1] + 2 * floor)
+    o, lse = scn.attn_fwd(q, k, v.cuda(), bounds(lens), **how)
+    less = (do.double() * 2.0 ** power).float()
+    d = scn.attn_bwd(q, k, v.cuda(), o, lse, less, bounds(lens), **how)
+    want = ref.attention(f64(q), f64(k), v.double().numpy(), *args, f64(less) * up)
+    # every sum's terms are rounded to multiples of 2^-149: D of them in a dP, weighted by p,
+    # one in its dS, and one a term in the result
+    a, b = (np.abs(f64(t)).max() for t in (q, k))
+    m = max(lens)
+    extra = {"dv": H * m * floor, "dq": 2 * (b + 1) * (D + 2 + m) * floor,
+             "dk": H * m * (a + 1) * (D + 3) * floor}
+    for x in ("dq", "dk", "dv"):
+        check(x, f64(d[x]) * up, want[x][0], want[x][1] + extra[x])
