@@ -53,6 +53,8 @@ struct Heads {
 // tiles whatever the lengths, so a grid of n / rows + B blocks covers them and no
 // length has to be known on the host (blocks past a sample's rows leave at once).
 // Bounds are clamped to [0, n], so that a bad range reads no row outside the arrays.
+// Where only samples of more than `cut` rows have tiles, min(b, ranges[b] / cut) stands for
+// b: it grows by one at each such sample, but the tiles are n / rows + min(B, n / cut).
 struct Span {
   int64_t base;  // first row of the sample
   int m;         // its rows
@@ -63,14 +65,19 @@ __device__ inline int64_t range_at(const int32_t* ranges, int b, int64_t n) {
   const int64_t v = ranges[b];
   return v < 0 ? 0 : v > n ? n : v;
 }
+__device__ inline int tile_start(int base, int b, int rows, int cut) {
+  return base / rows + (cut ? min(b, base / cut) : b);
+}
 // Every lane of the wave takes part.  The sample is the last b with
 // tile_start(b) <= tile, found 64 ways at a time.
-__device__ inline Span find_span(const int32_t* ranges, int batch, int64_t n, int tile, int rows) {
+__device__ inline Span find_span(const int32_t* ranges, int batch, int64_t n, int tile, int rows,
+                                 int cut = 0) {
   const int lane = threadIdx.x & 63;
   int lo = 0, len = batch;
   while (len > 1) {
     const int stride = (len + 63) >> 6, b = lo + lane * stride;
-    const bool below = lane * stride < len && (int)range_at(ranges, b, n) / rows + b <= tile;
+    const bool below = lane * stride < len &&
+                       tile_start((int)range_at(ranges, b, n), b, rows, cut) <= tile;
     const int c = __popcll(__ballot(below));
     const int step = max(c - 1, 0) * stride;
     lo += step;
@@ -82,7 +89,7 @@ __device__ inline Span find_span(const int32_t* ranges, int batch, int64_t n, in
   const int end = __builtin_amdgcn_readfirstlane((int)range_at(ranges, s.sample + 1, n));
   s.base = base;
   s.m = max(0, end - base);
-  const int64_t local = tile - (base / rows + s.sample);
+  const int64_t local = tile - tile_start(base, s.sample, rows, cut);
   s.first = local < 0 || local * rows >= s.m ? s.m : (int)(local * rows);
   return s;
 }

@@ -35,7 +35,7 @@ struct BwdArgs {
   float* lse2;       // [Hq][n]: lse in log 2, or NaN where it is past LSE_MOST ...
   float* rest;       // [Hq][n]: ... and what it lacks there
   float* share;      // the sinks' shares [chunk][Hk][sinks][2][D], or null
-  int sc;            // queries of a share
+  int sc, cut;       // queries of a share; samples of more rows than cut have shares
   float scale;
   Window w;
 };
@@ -501,11 +501,11 @@ __global__ void __launch_bounds__(128, 1) attn_sink_kernel(BwdArgs<NS> a, int ns
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int hk = blockIdx.x % a.Hk, j0 = blockIdx.x / a.Hk % nst * 32;
   const int chunk = blockIdx.x / a.Hk / nst;
-  const Span sp = find_span(a.ranges, a.batch, a.n, chunk, a.sc);
-  const int ns = min(a.w.sinks, sp.m);
+  const Span sp = find_span(a.ranges, a.batch, a.n, chunk, a.sc, a.cut);
+  const int ns = a.w.sinks;
   const int end = min(sp.first + a.sc, sp.m) - 1;       // the share's queries
   const int first = max(sp.first, j0 + a.w.left + 1);   // ... past the window of j0
-  if (sp.first >= sp.m || j0 >= ns || first > end) return;
+  if (sp.m <= a.cut || sp.first >= sp.m || first > end) return;
   const int j = min(j0 + n32, ns - 1);
   const float c2 = a.scale * LOG2E;
   Frag<NS> K[DP / 16], V[DP / 16];
@@ -560,20 +560,19 @@ __global__ void __launch_bounds__(128, 1) attn_sink_kernel(BwdArgs<NS> a, int ns
     }
 }
 
-// A sink's shares, added up in order into the first of them: block (sample, head, sink),
-// an element a thread.
+// A sink's shares, added up in order into the first of them: block (sample of more than cut
+// rows, head, sink), an element a thread.
 template <int NS>
 __global__ void __launch_bounds__(256) attn_share_kernel(BwdArgs<NS> a) {
   const int j = blockIdx.x % a.w.sinks, hk = blockIdx.x / a.w.sinks % a.Hk;
-  const int b = blockIdx.x / a.w.sinks / a.Hk;
-  const int base = (int)range_at(a.ranges, b, a.n);
-  const int m = (int)range_at(a.ranges, b + 1, a.n) - base;
+  const Span sp = find_span(a.ranges, a.batch, a.n, blockIdx.x / a.w.sinks / a.Hk, INT32_MAX, a.cut);
+  if ((int)threadIdx.x >= 2 * a.D || sp.m <= a.cut || sp.first > 0) return;
   const int far = (j & ~31) + a.w.left + 1;  // the first query past the window
-  if ((int)threadIdx.x >= 2 * a.D || j >= m || far >= m) return;
   const int64_t step = (int64_t)a.Hk * a.w.sinks * 2 * a.D;
-  float* const p = a.share + (int64_t)(base / a.sc + b + far / a.sc) * step +
-                   ((int64_t)hk * a.w.sinks + j) * 2 * a.D + threadIdx.x;
-  const int n = (m + a.sc - 1) / a.sc - far / a.sc;
+  float* const p =
+      a.share + (int64_t)(tile_start((int)sp.base, sp.sample, a.sc, a.cut) + far / a.sc) * step +
+      ((int64_t)hk * a.w.sinks + j) * 2 * a.D + threadIdx.x;
+  const int n = (sp.m + a.sc - 1) / a.sc - far / a.sc;
   float s = 0.f;
   int c = 0;
   for (; c + 8 <= n; c += 8) {
@@ -618,7 +617,8 @@ __global__ void __launch_bounds__(64 * KW * QW, NS == 3 || DP > 64 ? 1 : 2)
   const int j = min(j0 + n32, sp.m - 1);
   const float c2 = a.scale * LOG2E;
   // sinks whose far queries other blocks have taken are ordinary keys here
-  const int sinks = a.share ? 0 : a.w.sinks;
+  const bool shared = a.share && sp.m > a.cut;
+  const int sinks = shared ? 0 : a.w.sinks;
   const Window w{a.w.left, a.w.right, sinks};
 
   Frag<NS> K[DP / 16], V[DP / 16];
@@ -711,9 +711,10 @@ __global__ void __launch_bounds__(64 * KW * QW, NS == 3 || DP > 64 ? 1 : 2)
     }
   }
   const bool mine = j0 + n32 < sp.m;
-  const int far = (j & ~31) + a.w.left + 1;  // first query past the window of the sink tile
-  if (a.share && mine && j < a.w.sinks && far < sp.m) {
-    const int64_t c = sp.base / a.sc + sp.sample + far / a.sc;  // where their sum lies
+  if (shared && mine && j < a.w.sinks) {
+    const int far = (j & ~31) + a.w.left + 1;  // first query past the window of the sink tile
+    // where their sum lies
+    const int64_t c = tile_start((int)sp.base, sp.sample, a.sc, a.cut) + far / a.sc;
     const float* const p = a.share + ((c * a.Hk + hk) * a.w.sinks + j) * 2 * a.D;
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d)
@@ -753,10 +754,12 @@ __global__ void __launch_bounds__(64 * KW * QW, NS == 3 || DP > 64 ? 1 : 2)
 }
 
 // Sinks get their own blocks when a window ends before them (a left bound) and they
-// are few; many sinks keep the blocks of their keys busy anyway.
+// are few; many sinks keep the blocks of their keys busy anyway.  So do those of samples
+// with fewer than SPLIT_SINKS queries past the window, however many samples there are.
 bool split_sinks(int64_t n, int64_t left, int64_t sinks) {
   return left >= 0 && left < n && sinks > 0 && sinks <= SPLIT_SINKS;
 }
+int sink_cut(int64_t left) { return (int)left + SPLIT_SINKS; }
 // Shares of at least 256 queries (some tiles' work for a block), and not more than about
 // 256 of them to add up.
 int share_rows(int64_t n) {
@@ -764,7 +767,9 @@ int share_rows(int64_t n) {
   while (n / sc > 256) sc *= 2;
   return sc;
 }
-int64_t sink_chunks(int64_t n, int batch) { return n / share_rows(n) + batch; }
+int64_t sink_chunks(int64_t n, int batch, int64_t left) {
+  return ceil_div(n, share_rows(n)) + std::min<int64_t>(batch, n / sink_cut(left));
+}
 
 template <int NS, int DP, int KW, int QW, int U>
 scn_status launch_dkv(const BwdArgs<NS>& a, hipStream_t st) {
@@ -801,8 +806,9 @@ scn_status launch_dq(const BwdArgs<NS>& a, hipStream_t st) {
 template <int NS, int DP>
 scn_status launch_sinks(const BwdArgs<NS>& a, hipStream_t st) {
   const int nst = (a.w.sinks + 31) / 32;
-  const int64_t blocks = sink_chunks(a.n, a.batch) * a.Hk * nst;
-  if (std::max(blocks, (int64_t)a.w.sinks * a.Hk * a.batch) > INT32_MAX) {
+  const int64_t blocks = sink_chunks(a.n, a.batch, a.w.left) * a.Hk * nst;
+  const int64_t sums = std::min<int64_t>(a.batch, a.n / a.cut) * a.Hk * a.w.sinks;
+  if (std::max(blocks, sums) > INT32_MAX) {
     set_error("scn_attn_bwd: more than 2^31 blocks of sinks and heads");
     return SCN_ERR_OVERFLOW;
   }
@@ -812,8 +818,7 @@ scn_status launch_sinks(const BwdArgs<NS>& a, hipStream_t st) {
   if (scn_status rc = allow_lds(reinterpret_cast<const void*>(fn), limit, smem)) return rc;
   hipLaunchKernelGGL(fn, dim3((unsigned)blocks), dim3(128), smem, st, a, nst);
   SCN_LAUNCH_CHECK();
-  hipLaunchKernelGGL(attn_share_kernel<NS>, dim3((unsigned)(a.w.sinks * a.Hk * a.batch)), dim3(256),
-                     0, st, a);
+  hipLaunchKernelGGL(attn_share_kernel<NS>, dim3((unsigned)sums), dim3(256), 0, st, a);
   SCN_LAUNCH_CHECK();
   return SCN_OK;
 }
@@ -882,7 +887,7 @@ size_t scn_attn_bwd_workspace_bytes(int64_t n, int32_t batch, int32_t D, int32_t
     return 0;
   int64_t f = 3 * delta_floats(n, Hq);
   if (split_sinks(n, left, sinks))
-    f += sink_chunks(n, batch) * Hk * std::min(sinks, n) * 2 * D;
+    f += sink_chunks(n, batch, left) * Hk * std::min(sinks, n) * 2 * D;
   return (size_t)f * 4;
 }
 
@@ -915,20 +920,21 @@ scn_status scn_attn_bwd(int32_t type, int64_t n, int32_t batch, const int32_t* r
   float* const delta = static_cast<float*>(ws);
   float* const lse2 = delta + delta_floats(n, Hq);
   float* const rest = lse2 + delta_floats(n, Hq);
-  float* const share = split_sinks(n, left, sinks) ? rest + delta_floats(n, Hq) : nullptr;
+  const int cut = split_sinks(n, left, sinks) ? sink_cut(left) : 0;
+  float* const share = cut && n > cut ? rest + delta_floats(n, Hq) : nullptr;
   const Window w{bound(left, n), bound(right, n), bound(sinks, n)};
   if (type == SCN_BF16) {
     typedef uint16_t T;
     return run<1>(BwdArgs<1>{n, batch, D, Hq, Hk, Hq / Hk, ranges, view<const T>(q),
                              view<const T>(k), view<const T>(v), view<const T>(o),
                              view<const T>(d_o), view<T>(dq), view<T>(dk), view<T>(dv), lse, delta,
-                             lse2, rest, share, share_rows(n), scale, w}, st);
+                             lse2, rest, share, share_rows(n), cut, scale, w}, st);
   }
   typedef float T;
   return run<3>(BwdArgs<3>{n, batch, D, Hq, Hk, Hq / Hk, ranges, view<const T>(q),
                            view<const T>(k), view<const T>(v), view<const T>(o),
                            view<const T>(d_o), view<T>(dq), view<T>(dk), view<T>(dv), lse, delta,
-                           lse2, rest, share, share_rows(n), scale, w}, st);
+                           lse2, rest, share, share_rows(n), cut, scale, w}, st);
 }
 
 }  // extern "C"
