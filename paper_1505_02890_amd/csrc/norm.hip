@@ -207,12 +207,14 @@ __global__ void __launch_bounds__(NT) norm_rotate_bwd_kernel(NormArgs<NS> a) {
         m = fmaf(g[i][j] * wv[j], x[i][j], m);
       }
       const float r = rsqrtf(fmaf(group_sum<LP>(s), a.inv, a.eps));
-      const float z = r * r * r * (group_sum<LP>(m) * a.inv);
+      // (r^3 would pass fp32's range where its product with x and the mean does not)
+      const float z = r * (group_sum<LP>(m) * a.inv);
       float d[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        d[j] = r * (g[i][j] * wv[j]) - z * x[i][j];
-        dw[j] = fmaf(g[i][j], x[i][j] * r, dw[j]);
+        const float n = x[i][j] * r;
+        d[j] = r * (g[i][j] * wv[j] - z * n);
+        dw[j] = fmaf(g[i][j], n, dw[j]);
       }
       if (on) store8<NS>(op + i * out.head, d, a.past);
     }
