@@ -84,12 +84,15 @@ class SiteAttention:
     def forward(self, sites: "scn.Rulebook", coords: torch.Tensor, ranges: torch.Tensor,
                 x: torch.Tensor):
         """sites: a rulebook of filter 1, stride 1 over coords (int32 [n, 1 +
-        axes], key order); ranges from ``site_ranges``; x [n, channels].
+        axes], key order); ranges from ``site_ranges``; x [n, channels].  Sites of
+        no sample (their first coordinate past the ranges) pass unchanged.
         Returns (y [n, channels], what ``backward`` needs)."""
         p = self.params
         q, k, v = self._project(sites, x)
         qr, kr = scn.norm_rotate_fwd(q, k, p["wq"], p["wk"], coords, self.freq, self.sections)
-        o, lse = scn.attn_fwd(qr, kr, v, ranges, self.left, self.right, self.sinks)
+        # (zeros: rows of no sample are not written, and give nothing)
+        o, lse = scn.attn_fwd(qr, kr, v, ranges, self.left, self.right, self.sinks,
+                              out=torch.zeros(q.shape, dtype=q.dtype, device=q.device))
         y, of = self._out(sites, o, x)
         return y, (sites, coords, ranges, x, q, k, v, qr, kr, o, lse, of)
 
@@ -100,7 +103,7 @@ class SiteAttention:
         out = scn.conv_bwd(sites, of, self._zero[:of.shape[1]], p["Wo"], None, None, dy,
                            need=("dx", "dW"))
         do = out["dx"].to(self.dtype).view(n, self.heads, self.dim)
-        dqkv = torch.empty(n, (self.heads + 2 * self.kv) * self.dim, dtype=self.dtype,
+        dqkv = torch.zeros(n, (self.heads + 2 * self.kv) * self.dim, dtype=self.dtype,
                            device=x.device)
         dq, dk, dv = self._parts(dqkv)
         scn.attn_bwd(qr, kr, v, o, lse, do, ranges, self.left, self.right, self.sinks,
