@@ -119,7 +119,12 @@ class SiteAttention:
 
     def open(self, streams: int, capacity: int) -> Streams:
         """Empty caches; `capacity` points of each stream, sinks included (the
-        window's left + 1 + sinks holds all that a causal window sees)."""
+        window's left + 1 + sinks holds all that a causal window sees).  Of
+        causal layers (right = 0) only: a newest point sees none after it."""
+        if self.right != 0:
+            raise ValueError(f"streams need a causal layer (right=0), this one has {self.right}")
+        if capacity <= self.sinks:
+            raise ValueError(f"capacity must be above the {self.sinks} sinks, got {capacity}")
         dev = self.freq.device
         k = torch.zeros(streams, capacity, self.kv, self.dim, dtype=self.dtype, device=dev)
         one = torch.zeros(streams, 4, dtype=torch.int32, device=dev)  # one row a stream

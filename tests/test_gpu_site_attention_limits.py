@@ -1,4 +1,4 @@
-"""The attention layer: sites of no sample."""
+"""The attention layer: sites of no sample, and streams of layers that are not causal."""
 from __future__ import annotations
 
 import pytest
@@ -55,3 +55,16 @@ def test_sites_of_no_sample(scn, dtype):
     assert torch.allclose(dx[:inside], wdx, rtol=0, atol=1e-5)
     for name in grads:  # sums over other numbers of rows, in other orders
         assert torch.allclose(grads[name], wgrads[name], rtol=1e-4, atol=1e-4), name
+
+
+@pytest.mark.parametrize("right", [None, 1, 40])
+def test_streams_need_a_causal_layer(scn, right):
+    # a stream's newest point cannot see the ones after it
+    with pytest.raises(ValueError, match="causal"):
+        layer_of(torch.float32, left=20, right=right).open(2, 30)
+
+
+@pytest.mark.parametrize("capacity", [0, 3, 4])
+def test_streams_need_room_past_the_sinks(scn, capacity):
+    with pytest.raises(ValueError, match="capacity"):
+        layer_of(torch.float32, left=20, right=0, sinks=4).open(2, capacity)
