@@ -403,7 +403,13 @@ template <int NS>
 __device__ inline float row_dot(const typename Elem<NS>::T* a, const typename Elem<NS>::T* b,
                                 int D) {
   float s = 0.f;
-  for (int c = 0; c < D; ++c) s = fmaf(Elem<NS>::get(a[c]), Elem<NS>::get(b[c]), s);
+  for (int c = 0; c < D; c += 8) {
+    float x[8], y[8];
+    load8<NS>(a + c, x);
+    load8<NS>(b + c, y);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s = fmaf(x[j], y[j], s);
+  }
   return s;
 }
 
@@ -434,6 +440,12 @@ struct RowSum {
 // that factor passes 2^64, and weights end at 0 or infinity; sums outside these bounds say
 // so (what is lost within them is below 2^-86 of the sum).
 constexpr float SUM_LEAST = 0x1p-40f, SUM_MOST = 0x1p60f;
+// A sum that is NaN, and not for scores' size: a score is NaN, and so is all that the
+// row gives.  (Of fp32 operands, and beside zeros that fill a head's last tile, an
+// infinite operand may be the reason.)
+__device__ inline bool nan_score(float top, float sum) {
+  return sum != sum && (fabsf(top) < 0x1p30f || top == -INFINITY);
+}
 // The backward passes form weights from log sums in fp32, each off by up to some 2^-23 of its
 // log sum relatively.  Rows past this bound (2^-10 so) are formed again, from their own
 // scores' maximum and sum.

@@ -91,6 +91,19 @@ __device__ inline void dkv_row(const BwdArgs<NS>& a, const Span& sp, int hk, int
   const auto* const v = a.v.p + (sp.base + j) * a.v.row + hk * a.v.head;
   const int lo = max(0, j - a.w.right);
   const int hi = j < a.w.sinks ? sp.m - 1 : min(sp.m - 1, j + a.w.left);
+  auto* const dk = a.dk.p + (sp.base + j) * a.dk.row + hk * a.dk.head;
+  auto* const dv = a.dv.p + (sp.base + j) * a.dv.row + hk * a.dv.head;
+  // a row of no weights (its lse is NaN) leaves nothing to add up
+  bool none = false;
+  for (int h = hk * a.group; h < (hk + 1) * a.group; ++h)
+    for (int i = lo + lane; i <= hi; i += 64) {
+      const float l = a.lse[h * a.n + sp.base + i];
+      none |= l != l;
+    }
+  if (__ballot(none)) {
+    for (int c = lane; c < a.D; c += 64) dk[c] = dv[c] = E::put(NAN);
+    return;
+  }
   float k0 = 0.f, k1 = 0.f, v0 = 0.f, v1 = 0.f;
   for (int h = hk * a.group; h < (hk + 1) * a.group; ++h) {
     const auto* const q = a.q.p + sp.base * a.q.row + h * a.q.head;
@@ -119,8 +132,6 @@ __device__ inline void dkv_row(const BwdArgs<NS>& a, const Span& sp, int hk, int
       }
     }
   }
-  auto* const dk = a.dk.p + (sp.base + j) * a.dk.row + hk * a.dk.head;
-  auto* const dv = a.dv.p + (sp.base + j) * a.dv.row + hk * a.dv.head;
   if (lane < a.D) {
     dk[lane] = E::put(k0 * a.scale);
     dv[lane] = E::put(v0);
@@ -180,7 +191,8 @@ __global__ void __launch_bounds__(64 * QW * KW, NS == 3 && DP > 32 ? 1 : 2)
   delta = both_sum(delta);
   const int64_t at = h * a.n + sp.base + i;
   const float lse2 = a.lse[at] * LOG2E;
-  const bool far = !(fabsf(a.lse[at]) <= LSE_MOST);  // the row is formed again
+  const bool far = !(fabsf(a.lse[at]) <= LSE_MOST);  // the row is formed again ...
+  const bool none = a.lse[at] != a.lse[at];           // ... if it has weights at all
   // <do, o> has the rounding of o to bf16, the same for all keys of a row, where the sum of
   // dS is 0 by definition.  (Left in, dq and dk are off by 1.7 to 4 times their own rounding
   // where a row sees few keys or few of its keys hold its weight.)  The sum of dS is
@@ -374,7 +386,7 @@ __global__ void __launch_bounds__(64 * QW * KW, NS == 3 && DP > 32 ? 1 : 2)
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d) store_cols<NS>(o, dQ[d], a.scale, d, a.D, lane);
   }
-  const uint64_t bad = __ballot(mine && (far || !fine));
+  const uint64_t bad = __ballot(mine && !none && (far || !fine));
   uint32_t rows = (uint32_t)bad | (uint32_t)(bad >> 32);
   for (; rows; rows &= rows - 1) dq_row<NS>(a, sp, h, i0 + __builtin_ctz(rows));
 }

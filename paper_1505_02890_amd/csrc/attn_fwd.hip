@@ -304,6 +304,7 @@ __global__ void __launch_bounds__(64 * QW * KW, NS == 3 && DP > 96 ? 1 : 2)
 #pragma unroll
   for (int d = 0; d < DP / 32; ++d) fine &= finite16(O[d]);
   if constexpr (NS == 3) fine &= !tiny(O, inv);
+  if constexpr (NS == 1) fine |= a.D == DP && nan_score(top, sum);  // NaN, as it stands
   const bool mine = i0 + n32 < sp.m;
   if (mine) {
     auto* const o = a.o.p + (sp.base + i) * a.o.row + h * a.o.head;

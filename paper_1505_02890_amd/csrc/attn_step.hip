@@ -43,13 +43,14 @@ __device__ inline void join(float& m, float& l, float m2, float l2, float& f, fl
   m = t;
 }
 
-// One stream's head once more in fp32, term by term, by one wave: the maximum and the sum
-// first, a key per lane, then the values by their weights, channels along the lanes.  For
-// results that came out infinite or NaN (an infinite value that the token sees, but also
-// one that a weight's low part, or a zero that fills a tile, was multiplied with), and for
-// bf16 scores whose weights all ended at 0 or infinity (attn.h: SUM_LEAST).
-template <int NS>
-__device__ inline void step_row(const StepArgs<NS>& a, int s, int h) {
+// One stream's head once more in fp32, term by term, by W waves (this is wave w; all of a
+// block if W > 1, which hands over in `x`): the maximum and the sum first, a key per lane,
+// then the values by their weights, channels along the lanes.  For results that came out
+// infinite or NaN (an infinite value that the token sees, but also one that a weight's low
+// part, or a zero that fills a tile, was multiplied with), and for bf16 scores whose weights
+// all ended at 0 or infinity (attn.h: SUM_LEAST).
+template <int NS, int W>
+__device__ inline void step_row(const StepArgs<NS>& a, int s, int h, int w, float* x) {
   typedef Elem<NS> E;
   const int lane = threadIdx.x & 63, hk = h / a.group;
   const int p = min(max(0, a.length[s]), INT32_MAX - 1);
@@ -57,26 +58,48 @@ __device__ inline void step_row(const StepArgs<NS>& a, int s, int h) {
   const int cnt = ns + p - lo + 1, ring = a.cap - a.sinks;
   const int r0 = lo < a.sinks ? 0 : (lo - a.sinks) % ring;
   const auto* const q = a.q.p + s * a.q.row + h * a.q.head;
-  // the x-th key's row: the token's own (the last) as it came, the others in the cache
-  auto row = [&](int x, const Ring& r, const typename E::T* cache,
+  // the i-th key's row: the token's own (the last) as it came, the others in the cache
+  auto row = [&](int i, const Ring& r, const typename E::T* cache,
                  const Heads<const typename E::T>& now) {
-    const int y = r0 + x - ns;
-    const int64_t t = x < ns ? x : a.sinks + (y < ring ? y : y - ring);
-    return x == cnt - 1 ? now.p + s * now.row + hk * now.head
+    const int y = r0 + i - ns;
+    const int64_t t = i < ns ? i : a.sinks + (y < ring ? y : y - ring);
+    return i == cnt - 1 ? now.p + s * now.row + hk * now.head
                         : cache + s * r.stream + hk * r.head + t * r.row;
   };
-  auto score = [&](int x) { return row_dot<NS>(q, row(x, a.ks, a.kc, a.k), a.D) * a.scale; };
+  auto score = [&](int i) { return row_dot<NS>(q, row(i, a.ks, a.kc, a.k), a.D) * a.scale; };
   RowSum r;
-  for (int x = lane; x < cnt; x += 64) r.add(score(x));
+  for (int64_t i = w * 64 + lane; i < cnt; i += 64 * W) r.add(score((int)i));
   r.join();
+  if constexpr (W > 1) {
+    if (lane == 0) {
+      x[w] = r.top;
+      x[W + w] = r.sum;
+    }
+    __syncthreads();
+    if (lane < W) r = RowSum{x[lane], x[W + lane]};
+    else r = RowSum{};
+    r.join();
+    __syncthreads();
+  }
   float o0 = 0.f, o1 = 0.f;
-  for (int x0 = 0; x0 < cnt; x0 += 64) {
-    const float w = x0 + lane < cnt ? r.weight(score(x0 + lane)) : 0.f;
-    for (int y = 0; y < min(64, cnt - x0); ++y) {
-      const auto* const v = row(x0 + y, a.vs, a.vc, a.v);
-      const float wy = __shfl(w, y);
+  for (int64_t i0 = w * 64; i0 < cnt; i0 += 64 * W) {
+    const int n = (int)min<int64_t>(64, cnt - i0);
+    const float weight = lane < n ? r.weight(score((int)i0 + lane)) : 0.f;
+    for (int y = 0; y < n; ++y) {
+      const auto* const v = row((int)i0 + y, a.vs, a.vc, a.v);
+      const float wy = __shfl(weight, y);
       if (lane < a.D) o0 = fmaf(wy, E::get(v[lane]), o0);
       if (64 + lane < a.D) o1 = fmaf(wy, E::get(v[64 + lane]), o1);
+    }
+  }
+  if constexpr (W > 1) {
+    x[w * 128 + lane] = o0;
+    x[w * 128 + 64 + lane] = o1;
+    __syncthreads();
+    if (w > 0) return;
+    for (int g = 1; g < W; ++g) {
+      o0 += x[g * 128 + lane];
+      o1 += x[g * 128 + 64 + lane];
     }
   }
   auto* const o = a.o.p + s * a.o.row + h * a.o.head;
@@ -201,7 +224,7 @@ __global__ void __launch_bounds__(NT) attn_step_kernel(StepArgs<NS> a) {
     if (a.splits == 1) {
       v /= ll;
       red[0][g][ch] = v;
-      if (!(fabsf(v) < INFINITY)) bad[g] = true;
+      if (!(fabsf(v) < INFINITY || ll != ll)) bad[g] = true;
     } else {
       float* const out = a.part + (((int64_t)s * a.Hq + h0 + g) * a.splits + split) * (a.D + 2);
       out[ch] = v;
@@ -218,7 +241,7 @@ __global__ void __launch_bounds__(NT) attn_step_kernel(StepArgs<NS> a) {
       if (!bad[g]) a.o.p[s * a.o.row + (h0 + g) * a.o.head + ch] = E::put(red[0][g][ch]);
     }
     for (int g = wave; g < nh; g += NT / 64)
-      if (bad[g]) step_row<NS>(a, s, h0 + g);
+      if (bad[g]) step_row<NS, 1>(a, s, h0 + g, 0, nullptr);
   }
   // The new rows go to the cache.  No block reads that row: what it held is a
   // capacity's ring before the new token, past the reach.
@@ -398,6 +421,7 @@ __global__ void __launch_bounds__(NT, 2) attn_step_wide_kernel(StepArgs<1> a) {
           fine &= finite16(O[d]);
           store_cols<1>(o, O[d], inv, d, a.D, lane);
         }
+        fine |= a.D == DP && nan_score(top, sum);  // NaN, as it stands
       } else {
         float* const o =
             a.part + (((int64_t)s * a.Hq + h0 + n32) * a.splits + split) * (a.D + 2);
@@ -416,7 +440,7 @@ __global__ void __launch_bounds__(NT, 2) attn_step_wide_kernel(StepArgs<1> a) {
     }
     const uint64_t bad = __ballot(!fine);
     uint32_t heads = (uint32_t)bad | (uint32_t)(bad >> 32);
-    for (; heads; heads &= heads - 1) step_row<1>(a, s, h0 + __builtin_ctz(heads));
+    for (; heads; heads &= heads - 1) step_row<1, 1>(a, s, h0 + __builtin_ctz(heads), 0, nullptr);
   }
   if (split == 0 && pass == 0 && tid < a.D) {
     const int64_t r = p < a.sinks ? p : a.sinks + (p - a.sinks) % ring;
@@ -465,10 +489,11 @@ __global__ void __launch_bounds__(NT) attn_step_join_kernel(StepArgs<NS> a) {
   if (tid < a.D) {
     for (int i = 1; i < slices; ++i) v += red[i * a.D + ch];
     v /= l;
-    fine = fabsf(v) < INFINITY && l > SUM_LEAST && l < SUM_MOST;
+    fine = (fabsf(v) < INFINITY && l > SUM_LEAST && l < SUM_MOST) ||
+           (NS == 3 ? l != l : a.D % 32 == 0 && nan_score(m, l));
   }
   if (__syncthreads_or(!fine)) {
-    if (tid < 64) step_row<NS>(a, s, h);
+    step_row<NS, NT / 64>(a, s, h, tid >> 6, w);
   } else if (tid < a.D) {
     a.o.p[s * a.o.row + h * a.o.head + ch] = Elem<NS>::put(v);
   }

@@ -326,3 +326,32 @@ def test_tiny_values_keep_their_bits(scn, D, lens, left, right, sinks, power):
              "dk": H * m * (a + 1) * (D + 3) * floor}
     for x in ("dq", "dk", "dv"):
         check(x, f64(d[x]) * up, want[x][0], want[x][1] + extra[x])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [24, 32, 64, 128])
+@pytest.mark.parametrize("what", ["q", "k"])
+def test_rows_of_nan_are_those_that_see_it(scn, dtype, D, what):
+    # a query or a key of NaN: its rows, and the keys that they see, have no finite result; all
+    # others have what they have without it
+    m, H, K, left, sinks, at = 300, 2, 1, 40, 1, 100
+    t = TYPES[dtype]
+    g = torch.Generator().manual_seed(13)
+    q, k, v, do = (torch.randn(m, h, D, generator=g).to(t).cuda() for h in (H, K, K, H))
+    want = ref.attention(f64(q), f64(k), f64(v), [m], left, 0, sinks, D ** -0.5, dtype == "bf16",
+                         f64(do))
+    (q if what == "q" else k)[at] = float("nan")
+    how = dict(left=left, right=0, sinks=sinks)
+    o, lse = scn.attn_fwd(q, k, v, bounds([m]), **how)
+    d = scn.attn_bwd(q, k, v, o, lse, do, bounds([m]), **how)
+    i = np.arange(m)
+    rows = (i == at) if what == "q" else (i >= at) & (i <= at + left)
+    see = ref.visible(m, left, 0, sinks)
+    keys = see[rows].any(0)
+    for name, got, none in (("o", o, rows), ("dq", d["dq"], rows), ("dk", d["dk"], keys),
+                            ("dv", d["dv"], keys)):
+        got = f64(got)
+        assert np.isnan(got[none]).all(), name
+        check(name, got[~none], want[name][0][~none], want[name][1][~none])
+    assert np.isnan(f64(lse)[:, rows]).all()
+    check("lse", f64(lse)[:, ~rows], want["lse"][0][:, ~rows], want["lse"][1][:, ~rows])
