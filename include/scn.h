@@ -383,13 +383,26 @@ scn_status scn_maxpool_bwd(const scn_rulebook* rb, const uint8_t* argmax, const 
 
 /*
  * Attention among the active sites.  A sample's rows are a sequence of tokens:
- * they lie together, in key order, and a site's lattice coordinates are its
+ * they lie together, in the caller's order (a rulebook's rows are in key order;
+ * causal attention along a stroke takes a row a point, in the order of
+ * writing, which no rulebook keeps), and a site's lattice coordinates are its
  * position.  The calls below take features in fp32 or bf16 and hold every sum,
- * statistic and gradient accumulation in fp32 (fp32 operands are multiplied
- * split into three bf16 values, as in scn_conv_fwd; results that come out
- * infinite or NaN are formed again term by term in fp32 over visible sites
- * only, so what a masked site holds never shows).  All of them are
- * deterministic, launch on `stream` and neither wait nor allocate.
+ * statistic and gradient accumulation in fp32.  All of them are deterministic,
+ * launch on `stream` and neither wait nor allocate.
+ *
+ * fp32 operands are multiplied split into three bf16 values, as in
+ * scn_conv_fwd.  bf16 operands are multiplied as they are; the attention's
+ * weights, and in the gradients dS, are rounded to bf16 for their products with
+ * rows of v, k, q and do (scn_attn_step keeps 16 bits of them), so results are
+ * off by some 1.4 times what rounding them to bf16 alone would cost.
+ *
+ * Rows of results that this does not serve are formed again in fp32, term by
+ * term over the sites that they see: those that come out infinite or NaN (what
+ * a masked site holds never shows, and values near the type's largest do not
+ * overflow), those of scores from 2^31 on, in the gradients those of log sums
+ * past 8192, and fp32 results below 2^-95.  Such rows take some hundred times as long.
+ * Where the definition itself gives NaN (a score of NaN or +inf, all scores
+ * -inf), so do the calls.
  */
 #define SCN_F32 0
 #define SCN_BF16 1
@@ -430,7 +443,8 @@ scn_status scn_site_ranges(const int32_t* coords, int64_t n, int32_t width, int3
  *   y_2j+1 = u_2j sin a_j + u_2j+1 cos a_j,   a_j = coords[t][1 + axis(j)] freq[j]
  * The pairs j are dealt to the axes in order: the first sections[0] pairs turn
  * with coordinate 1 of the site, the next sections[1] with coordinate 2, ..;
- * pairs past the last section are not rotated.  Angles are reduced in 64 bits.
+ * pairs past the last section are not rotated.  Angles are reduced in 64 bits;
+ * the mean is in fp32 (rows of 2^-60 to 2^60 have room in it, whatever eps).
  *  type      SCN_F32 or SCN_BF16, of q, k and the results.
  *  n, D, Hq, Hk   rows, channels of a head (a multiple of 8, at most 128),
  *            heads of q and of k (Hk may be 0: k, wk and kr are then not read).
@@ -473,10 +487,12 @@ scn_status scn_norm_rotate_bwd(int32_t type, int64_t n, int32_t D, int32_t Hq, i
  * left and right: negative for no bound.  right = 0 is causal; the first
  * `sinks` rows of a sample stay visible to all that follow them.
  *  n, ranges  rows, and device int32[batch + 1] as scn_site_ranges gives
- *             (ascending; rows outside every range are not written).
+ *             (ascending; rows outside every range are not written, here and
+ *             in the gradients).
  *  D, Hq, Hk  channels of a head (a multiple of 8, at most 128), query heads,
  *             key and value heads (Hq a multiple of Hk).
- *  o          of the type (written);  lse  device float[Hq][n] (written), or NULL.
+ *  o          of the type (written, apart from q, k and v);  lse  device
+ *             float[Hq][n] (written), or NULL.
  * Errors: SCN_ERR_INVALID (also a scale that is not positive and finite),
  * SCN_ERR_UNSUPPORTED (D), SCN_ERR_OVERFLOW (n above 2^30), SCN_ERR_HIP.
  */
@@ -485,7 +501,8 @@ scn_status scn_attn_fwd(int32_t type, int64_t n, int32_t batch, const int32_t* r
                         const scn_heads* v, float scale, int64_t left, int64_t right,
                         int64_t sinks, const scn_heads* o, float* lse, hipStream_t stream);
 
-/* Bytes of device workspace scn_attn_bwd needs. */
+/* Bytes of device workspace scn_attn_bwd needs: 12 a row and query head, and with
+ * sinks and a left bound at most twice the keys and values in fp32. */
 size_t scn_attn_bwd_workspace_bytes(int64_t n, int32_t batch, int32_t D, int32_t Hq, int32_t Hk,
                                     int64_t left, int64_t sinks);
 
@@ -494,7 +511,8 @@ size_t scn_attn_bwd_workspace_bytes(int64_t n, int32_t batch, int32_t D, int32_t
  *   p_ij = exp(s_ij - lse_i),  ds_ij = p_ij (<do_i, v_j> - <do_i, o_i>)
  *   dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_i ds_ij q_i,
  *   dv_j = sum_i p_ij do_i
- * over the pairs seen; dk and dv sum over their head's query heads too.
+ * over the pairs seen; dk and dv sum over their head's query heads too.  No
+ * result may overlap an input.
  * Errors: as scn_attn_fwd, and SCN_ERR_WORKSPACE.
  */
 scn_status scn_attn_bwd(int32_t type, int64_t n, int32_t batch, const int32_t* ranges, int32_t D,

@@ -605,7 +605,9 @@ def attn_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, ranges: torch.Te
     [n, Hk, D], float32 or bfloat16, any row and head strides; ``ranges`` from
     ``site_ranges``.  Row i of a sample sees row j if j <= i + right and
     (j >= i - left or j < sinks); None is no bound, right=0 causal.  scale is
-    D ** -0.5 unless given.  Returns (o [n, Hq, D], lse float32 [Hq, n])."""
+    D ** -0.5 unless given.  Returns (o [n, Hq, D], lse float32 [Hq, n]).  Rows
+    outside every range (of samples past the batch) are not written: they hold
+    what ``out`` held, or nothing that means anything.  ``out`` may not overlap q, k or v."""
     dtype, dev, n, hq, hk, d, vq, vk, vv = _qkv(q, k, v)
     batch, pr, scale, l, r = _attn_args(ranges, dev, left, right, sinks, scale, d)
     o, vo = _out_rows(out, q, (n, hq, d), "out")
@@ -622,7 +624,8 @@ def attn_bwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Tensor,
              scale: Optional[float] = None, out=(None, None, None),
              ws: Optional[torch.Tensor] = None):
     """Gradients of ``attn_fwd`` (``scn_attn_bwd``): a dict with dq, dk and dv,
-    in ``out`` where given."""
+    in ``out`` where given (apart from the inputs).  Rows outside every range are
+    not written, as in ``attn_fwd``."""
     dtype, dev, n, hq, hk, d, vq, vk, vv = _qkv(q, k, v)
     batch, pr, scale, l, r = _attn_args(ranges, dev, left, right, sinks, scale, d)
     vo = _rows(o, dtype, dev, (n, hq, d), "o")

@@ -2,8 +2,12 @@
 
 A filter mixes sites two or three lattice steps apart.  This layer lets every
 active site of a sample draw on the others, whichever lie far away: the sites
-are the tokens, their lattice coordinates the positions, and the key order of
-the rows the sequence.
+are the tokens, their lattice coordinates the positions, and the order of the
+rows the sequence: a rulebook's rows are in key order.  A causal layer along a
+stroke needs the points in the order of writing, which a rulebook does not keep
+(nor a point that is visited twice): its rows are the points, and its
+convolutions, which are 1x1, run on a rulebook over any n distinct sites, as
+``_strokes`` has them.
 
     q, k, v = x Wqkv                      (1x1 convolution, heads side by side)
     q, k    = norm and rotation of each head by the site's coordinates
@@ -83,8 +87,9 @@ class SiteAttention:
 
     def forward(self, sites: "scn.Rulebook", coords: torch.Tensor, ranges: torch.Tensor,
                 x: torch.Tensor):
-        """sites: a rulebook of filter 1, stride 1 over coords (int32 [n, 1 +
-        axes], key order); ranges from ``site_ranges``; x [n, channels].  Sites of
+        """sites: a rulebook of filter 1, stride 1 over n sites in row order;
+        coords int32 [n, 1 + axes], the sample ascending (``out_coords``, or the
+        points of strokes); ranges from ``site_ranges``; x [n, channels].  Sites of
         no sample (their first coordinate past the ranges) pass unchanged.
         Returns (y [n, channels], what ``backward`` needs)."""
         p = self.params

@@ -100,9 +100,6 @@ struct Window {
   int left, right, sinks;
   __device__ inline int lo(int i) const { return max(0, i - left); }
   __device__ inline int hi(int i, int m) const { return min(m - 1, i + right); }
-  __device__ inline bool sees(int i, int j) const {
-    return j <= i + right && (j >= i - left || j < sinks);
-  }
 };
 
 template <int NS>

@@ -10,11 +10,14 @@
 // shares that a fourth adds up in order.  P and dS are rounded to bf16 for their products
 // (in three parts for fp32), all sums are in fp32.
 //
-// The vector unit and the waits between a tile's steps bound both passes.  60,007 rows, 4
-// heads of 64 channels, bf16, windows of 1025 rows and a sink: queries' pass 174 us,
-// keys' pass 174, sinks 16 and 5.  34,567 rows, 4 heads on 2 of 32 channels, fp32, 256
-// rows back and two sinks: 66, 90, 24 and 5 us.  More keys a barrier (64 for 32), four
-// waves side by side, or three waves a SIMD by spilling measure the same or worse.
+// The waits between a tile's steps bound both passes: of the waves' cycles 26 to 41% go to
+// loads and barriers and 20 to 33% to issuing, the vector unit issues in 25 to 44%, the
+// matrix cores are busy in 25 to 31%.  60,007 rows, 4 heads of 64 channels, bf16, windows of
+// 1025 rows and a sink: queries' pass 174 us, keys' pass 171, sinks 17 and 5.  34,567 rows, 4
+// heads on 2 of 32 channels, fp32, 256 rows back and two sinks: 69, 90, 22 and 5 us.  30,000
+// rows, 4 heads on 2 of 128 channels, bf16, windows of 1025: 158, 227, 25 and 5 us.  More
+// keys a barrier (64 for 32), four waves side by side, or three waves a SIMD by spilling
+// measure the same or worse.
 #include "attn.h"
 
 namespace scn {
@@ -767,7 +770,9 @@ __global__ void __launch_bounds__(64 * KW * QW, NS == 3 || DP > 64 ? 1 : 2)
 
 // Sinks get their own blocks when a window ends before them (a left bound) and they
 // are few; many sinks keep the blocks of their keys busy anyway.  So do those of samples
-// with fewer than SPLIT_SINKS queries past the window, however many samples there are.
+// with fewer than SPLIT_SINKS queries past the window (gradients of 2000 samples of 50
+// rows, 16 sinks: 435 us against 638 with blocks of their own; 800 of 125 in fp32: 329 against
+// 370).
 bool split_sinks(int64_t n, int64_t left, int64_t sinks) {
   return left >= 0 && left < n && sinks > 0 && sinks <= SPLIT_SINKS;
 }
@@ -841,8 +846,8 @@ scn_status launch_sinks(const BwdArgs<NS>& a, hipStream_t st) {
 //    heads, 64 channels: 188 against 207 before the reads ahead), and with more than 64
 //    channels, where two groups' tiles and sums crowd the registers (30,000 rows of 2 key
 //    heads, 128 channels: 223 against 272).  The queries' pass of wide heads does so from
-//    512 blocks of 128 queries on (both passes: 486 against 502 at 30,000 rows of 4 heads,
-//    165 against 145 at 2000).
+//    512 blocks of 128 queries on (forward and gradients: 511 against 522 at 30,000 rows of 4
+//    heads, 158 against 142 at 2000).
 //  - Few blocks, counted against the query heads that each has to take in turn: a wave's
 //    32 keys by four groups (2000 rows of 4 heads: 54 to 27; 32,001 rows, 4 heads on one:
 //    310 to 190).

@@ -10,13 +10,15 @@
 // most 1.4 times as far off as its own rounding; the sum has the unrounded terms.  fp32:
 // each operand in three bf16 parts, six products.
 //
-// The vector unit bounds it: 32 x 32 scores of 64 channels cost some 74 vector
-// instructions, 400 cycles, beside 256 on the matrix cores.  All pairs of 16,384 rows, 4
-// heads of 64 channels, bf16: 330 us, 834 TFLOP/s; the vector unit issues in 67% of the
-// cycles, the matrix cores are busy in 44%, and neither a third wave, wave priorities nor
-// another order of the instructions gain.  Windows of 1025 rows (60,007 rows, 4 heads):
-// 110 us, 570 TFLOP/s, vector unit 44%, the rest being masked ends, the sinks' tile and
-// blocks starting.
+// 32 x 32 scores of 64 channels cost some 74 vector instructions, 400 cycles, beside 256 on
+// the matrix cores.  All pairs of 16,384 rows, 4 heads of 64 channels, bf16: 330 us, 834
+// TFLOP/s; the vector unit issues in 55% of the cycles, the matrix cores are busy in 36%, the
+// waves wait to issue for 34% of theirs, and neither a third wave, wave priorities nor another
+// order of the instructions gain.  Windows of 1025 rows (60,007 rows, 4 heads): 110 us, 570
+// TFLOP/s, vector unit 44%, matrix cores 23%; the waves wait for loads and barriers for 28%
+// of their cycles, to issue for 27%.  Causal samples (32,001 rows of 16 samples): 74 us, 33% and
+// 19%, one wave a SIMD in the mean where two fit, for a sample's last tiles see the most keys
+// and come last.
 #include <cmath>
 
 #include "attn.h"

@@ -7,8 +7,9 @@
 // Both passes read and write each row once: memory bounds them.  A lane holds
 // eight channels of a row in registers, LP lanes a head; the row's sines and
 // cosines are formed once and serve HC heads.  Measured: 300,001 rows of 4 + 4 heads of
-// 64 channels, bf16, forward 113 us (5.5 TB/s), backward 225 (4.1); 131,072 rows of
-// 8 + 2 heads of 32, fp32, forward 63 us (5.4).
+// 64 channels, bf16, forward 114 us (5.4 TB/s), backward 219 (4.2: its waves wait for
+// memory in 80% of their cycles as the forward's do, with 2.6 of them a SIMD to its 3.7);
+// 131,072 rows of 8 + 2 heads of 32, fp32, forward 64 us (5.3).
 #include "attn.h"
 
 namespace scn {
