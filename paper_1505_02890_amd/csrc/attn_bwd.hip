@@ -351,8 +351,8 @@ __global__ void __launch_bounds__(64 * QW * KW, NS == 3 && DP > 32 ? 1 : 2)
     over = joined(over);
     size = joined(size);
     if (fabsf(over) < INFINITY) delta += over;
-    // The threshold is what the rounding of dS leaves of it: rows of scores of N(0, 1.5)
-    // and 512 keys stay below, with N(0, 2) one in 200 is above, with N(0, 4) one in five.
+    // The threshold is what the rounding of dS leaves of it: rows of 1024 keys and scores of
+    // N(0, 1.5) stay below, with N(0, 2) one in 200 is above, with N(0, 4) one in five.
     if (__syncthreads_or(fabsf(over) > 0x1p-9f * size)) {
 #pragma unroll
       for (int d = 0; d < DP / 32; ++d) dQ[d] = zero16();
