@@ -548,6 +548,120 @@ scn_status scn_attn_step(int32_t type, int32_t streams, int64_t capacity, int32_
                          const scn_heads* o, void* ws, size_t ws_bytes, hipStream_t stream);
 
 /*
+ * Cross attention: the rows of a sample attend to states of the same sample that are rows
+ * of other arrays, of another number (a pooled level's sites to the finer level's, the points
+ * of a stroke to a text's states).  With i a row of q in sample b, j the states of b, query
+ * head h and its key head h / (Hq/Hk):
+ *   s_ij = scale <q_i, k_j>,  lse_i = log sum_j exp s_ij,  o_i = sum_j exp(s_ij - lse_i) v_j
+ * A sample without states gives o = 0 and lse = -inf.  One row a sample is a step of streams
+ * whose states stay.
+ *  nq, nk     rows of q and o, and of k and v.
+ *  q_ranges, k_ranges  device int32[batch + 1], as scn_site_ranges gives (ascending; rows
+ *             outside every range are not written).
+ *  D, Hq, Hk, scale, o, lse  as in scn_attn_fwd, lse device float[Hq][nq].
+ *  ws         scn_cross_attn_fwd_workspace_bytes bytes, 16-byte aligned (0: none needed).
+ * Types, strides, numerics and rows formed again: as scn_attn_fwd.
+ * Errors: SCN_ERR_INVALID, SCN_ERR_UNSUPPORTED (D), SCN_ERR_OVERFLOW (nk or nq Hq/Hk above
+ * 2^30), SCN_ERR_WORKSPACE, SCN_ERR_HIP.
+ */
+scn_status scn_cross_attn_fwd(int32_t type, int64_t nq, int64_t nk, int32_t batch,
+                              const int32_t* q_ranges, const int32_t* k_ranges, int32_t D,
+                              int32_t Hq, int32_t Hk, const scn_heads* q, const scn_heads* k,
+                              const scn_heads* v, float scale, const scn_heads* o, float* lse,
+                              void* ws, size_t ws_bytes, hipStream_t stream);
+size_t scn_cross_attn_fwd_workspace_bytes(int32_t type, int64_t nq, int64_t nk, int32_t batch,
+                                          int32_t D, int32_t Hq, int32_t Hk);
+
+/*
+ * Gradients of scn_cross_attn_fwd (o and lse are its results) for a given do, by the formulas
+ * of scn_attn_bwd.  Rows of q in samples without states, and states of samples without rows
+ * of q, get 0.  No result may overlap an input.
+ * Errors: as the forward.
+ */
+scn_status scn_cross_attn_bwd(int32_t type, int64_t nq, int64_t nk, int32_t batch,
+                              const int32_t* q_ranges, const int32_t* k_ranges, int32_t D,
+                              int32_t Hq, int32_t Hk, const scn_heads* q, const scn_heads* k,
+                              const scn_heads* v, const scn_heads* o, const float* lse,
+                              const scn_heads* d_o, float scale, const scn_heads* dq,
+                              const scn_heads* dk, const scn_heads* dv, void* ws, size_t ws_bytes,
+                              hipStream_t stream);
+size_t scn_cross_attn_bwd_workspace_bytes(int32_t type, int64_t nq, int64_t nk, int32_t batch,
+                                          int32_t D, int32_t Hq, int32_t Hk);
+
+/* Rows of channels: channel c of row t at ((T*)p)[t*row + c].  p is a device pointer, aligned
+ * to its elements; row >= 0 is a stride in elements. */
+typedef struct scn_rows {
+  void* p;
+  int64_t row;
+} scn_rows;
+
+/*
+ * The norms around a block of a network, with the block's gate and the residual, in one pass:
+ * n(t) = t / sqrt(mean_c t_c^2 + eps), and for each row
+ *   y = alpha x + sigmoid(z) wf n(f),   h = wh n(y)
+ * x is the residual, f the block's result, z the logits of its gate, y the next residual and
+ * h what the next block reads (formed from y before y is rounded).
+ *  res_type   SCN_F32 or SCN_BF16, of x and y;  type  of f, z and h (SCN_F32 only beside an
+ *             fp32 residual).
+ *  n, C       rows and channels, C in [1, 4096].
+ *  f          NULL: y = alpha x (the norm before a first block); z then NULL too.
+ *  z          NULL: no gate.
+ *  wf, wh     device float[C], or NULL for ones.
+ *  y, h       written; NULL: not wanted (f or h must be given).  y may be x; h may be f or z.
+ * Sums are in fp32, and in 64 bits for rows whose squares leave fp32's range.
+ * Errors: SCN_ERR_INVALID, SCN_ERR_UNSUPPORTED (C, types), SCN_ERR_OVERFLOW (n above 2^30),
+ * SCN_ERR_HIP.
+ */
+scn_status scn_block_norm_fwd(int32_t res_type, int32_t type, int64_t n, int32_t C,
+                              const scn_rows* x, const scn_rows* f, const scn_rows* z,
+                              const float* wf, const float* wh, float alpha, float eps,
+                              const scn_rows* y, const scn_rows* h, hipStream_t stream);
+
+/* Bytes of device workspace scn_block_norm_bwd needs if dwf or dwh is given. */
+size_t scn_block_norm_bwd_workspace_bytes(int64_t n, int32_t C);
+
+/*
+ * Gradients of scn_block_norm_fwd for given dy (of y's uses but the norm; NULL: none) and dh
+ * (NULL: no h): dx, df and dz (with f and z alone), and dwf, dwh (device float[C], sums over
+ * rows; NULL: not computed).  dx may be dy; df and dz may be dh, f or z.
+ * Errors: as the forward, and SCN_ERR_WORKSPACE.
+ */
+scn_status scn_block_norm_bwd(int32_t res_type, int32_t type, int64_t n, int32_t C,
+                              const scn_rows* x, const scn_rows* f, const scn_rows* z,
+                              const float* wf, const float* wh, float alpha, float eps,
+                              const scn_rows* dy, const scn_rows* dh, const scn_rows* dx,
+                              const scn_rows* df, const scn_rows* dz, float* dwf, float* dwh,
+                              void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* A tensor of n elements side by side, SCN_F32 or SCN_BF16; p is a device pointer. */
+typedef struct scn_tensor {
+  void* p;
+  int64_t n;
+  int32_t type;
+} scn_tensor;
+
+/* Bytes of device workspace scn_grad_clip needs for `count` tensors. */
+size_t scn_grad_clip_workspace_bytes(int64_t count);
+
+/*
+ * The norm of all gradients of a model taken together, and their clipping by it:
+ *   norm = sqrt(sum over all tensors of t^2),   out = norm > most ? t most / norm : t
+ * The sum is in 64 bits, always in the same order.  A norm that is not finite leaves all
+ * gradients as they are (the caller sees it in `norm`).  Nothing waits for the device.
+ *  grads      host array of `count` tensors (the addresses are read during the call alone).
+ *  out        host array of `count` device pointers for the results, of the gradients' types;
+ *             NULL: in place.  An entry may be its gradient's own place.
+ *  most       >= 0, or infinity for the norm alone.
+ *  norm       device float (written).
+ *  ws         8-byte aligned.
+ * Errors: SCN_ERR_INVALID (also results that overlap each other or another gradient, such as
+ * one tensor listed twice in place), SCN_ERR_OVERFLOW (2^40 elements in all, 2^20 tensors),
+ * SCN_ERR_WORKSPACE, SCN_ERR_NOMEM (host memory), SCN_ERR_HIP.
+ */
+scn_status scn_grad_clip(int64_t count, const scn_tensor* grads, void* const* out, double most,
+                         float* norm, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/*
  * Device memory the library allocates for itself: rulebook storage and the
  * temporaries of scn_rulebook_build* and scn_conv_fwd (workspaces of the
  * backward passes are the caller's).  By default it comes from the library's

@@ -13,12 +13,17 @@ from ._lib import (  # noqa: F401
     attn_bwd,
     attn_fwd,
     attn_step,
+    block_norm_bwd,
+    block_norm_fwd,
     build_chain,
     build_rulebook,
     build_rulebook_nd,
+    clip_grads,
     conv_bwd,
     conv_bwd_workspace,
     conv_fwd,
+    cross_attn_bwd,
+    cross_attn_fwd,
     lib,
     maxpool_bwd,
     maxpool_fwd,

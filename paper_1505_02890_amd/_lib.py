@@ -39,7 +39,10 @@ EXPORTED = (
     "scn_ceiling_mfma_f32", "scn_ceiling_mfma_bf16", "scn_site_ranges", "scn_norm_rotate_fwd",
     "scn_norm_rotate_bwd_workspace_bytes", "scn_norm_rotate_bwd", "scn_attn_fwd",
     "scn_attn_bwd_workspace_bytes", "scn_attn_bwd", "scn_attn_step_workspace_bytes",
-    "scn_attn_step",
+    "scn_attn_step", "scn_cross_attn_fwd", "scn_cross_attn_fwd_workspace_bytes",
+    "scn_cross_attn_bwd", "scn_cross_attn_bwd_workspace_bytes", "scn_block_norm_fwd",
+    "scn_block_norm_bwd_workspace_bytes", "scn_block_norm_bwd", "scn_grad_clip_workspace_bytes",
+    "scn_grad_clip",
 )
 
 _ALLOC_FN = ctypes.CFUNCTYPE(ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p, ctypes.c_void_p)
@@ -71,6 +74,10 @@ class _Heads(ctypes.Structure):
 class _Cache(ctypes.Structure):
     _fields_ = [("p", ctypes.c_void_p), ("stream", ctypes.c_int64), ("row", ctypes.c_int64),
                 ("head", ctypes.c_int64)]
+
+
+class _Rows(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("row", ctypes.c_int64)]
 
 
 _lib = None
@@ -128,6 +135,18 @@ def lib() -> ctypes.CDLL:
         "scn_attn_step_workspace_bytes": (sz, [i32, i32, i64, i32, i32, i32, i64, i64]),
         "scn_attn_step": (st, [i32, i32, i64, i32, i32, i32, P, P, P, P, P, P, f32, i64, i64, P,
                                P, sz, P]),
+        "scn_cross_attn_fwd": (st, [i32, i64, i64, i32, P, P, i32, i32, i32, P, P, P, f32, P, P, P,
+                                    sz, P]),
+        "scn_cross_attn_fwd_workspace_bytes": (sz, [i32, i64, i64, i32, i32, i32, i32]),
+        "scn_cross_attn_bwd": (st, [i32, i64, i64, i32, P, P, i32, i32, i32, P, P, P, P, P, P, f32,
+                                    P, P, P, P, sz, P]),
+        "scn_cross_attn_bwd_workspace_bytes": (sz, [i32, i64, i64, i32, i32, i32, i32]),
+        "scn_block_norm_fwd": (st, [i32, i32, i64, i32, P, P, P, P, P, f32, f32, P, P, P]),
+        "scn_block_norm_bwd_workspace_bytes": (sz, [i64, i32]),
+        "scn_block_norm_bwd": (st, [i32, i32, i64, i32, P, P, P, P, P, f32, f32, P, P, P, P, P, P,
+                                    P, P, sz, P]),
+        "scn_grad_clip_workspace_bytes": (sz, [i64]),
+        "scn_grad_clip": (st, [i64, P, P, ctypes.c_double, P, P, sz, P]),
         "scn_set_allocator": (None, [_ALLOC_FN, _FREE_FN, P]),
         "scn_set_dense_forward": (st, [i64, i32]),
         "scn_last_error": (ctypes.c_char_p, []),
@@ -670,6 +689,214 @@ def attn_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_cache: torch.
         None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(),
         _raw_stream(dev)), "scn_attn_step")
     return o
+
+
+def _cross(q, k, v, q_ranges, k_ranges, scale):
+    shape, dtype, dev = _first(q, "q")
+    n, hq, d = shape
+    m, hk = (k.shape[0], k.shape[1]) if isinstance(k, torch.Tensor) and k.dim() == 3 else (0, 0)
+    vq = _rows(q, dtype, dev, shape, "q")
+    vk = _rows(k, dtype, dev, (m, hk, d), "k")
+    vv = _rows(v, dtype, dev, (m, hk, d), "v")
+    if hk < 1 or hq % hk:
+        raise ValueError(f"{hq} query heads cannot share {hk} key heads evenly")
+    batch = q_ranges.shape[0] - 1 if isinstance(q_ranges, torch.Tensor) and q_ranges.dim() == 1 else 0
+    if batch < 1:
+        raise ValueError("q_ranges must hold at least two bounds")
+    pq = _vector(q_ranges, torch.int32, dev, (batch + 1,), "q_ranges")
+    pk = _vector(k_ranges, torch.int32, dev, (batch + 1,), "k_ranges")
+    if pq is None or pk is None:
+        raise TypeError("k_ranges must be a CUDA (HIP) tensor")
+    return (dtype, dev, n, m, batch, pq, pk, d, hq, hk, vq, vk, vv,
+            d ** -0.5 if scale is None else scale)
+
+
+def cross_attn_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_ranges: torch.Tensor,
+                   k_ranges: torch.Tensor, scale: Optional[float] = None,
+                   out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
+    """Attention of each sample's rows to the same sample's states
+    (``scn_cross_attn_fwd``).  q [n, Hq, D], k and v [m, Hk, D], float32 or
+    bfloat16, any row and head strides; the ranges int32 [batch + 1] as
+    ``site_ranges`` gives, of q's rows and of the states.  scale is D ** -0.5 unless
+    given.  Returns (o [n, Hq, D], lse float32 [Hq, n]); rows of samples without
+    states get 0 and -inf, and rows outside every range are not written.  ``out``
+    may not overlap q, k or v.  Streams whose states stay take their newest rows
+    with ranges 0, 1, 2, .."""
+    dtype, dev, n, m, batch, pq, pk, d, hq, hk, vq, vk, vv, scale = _cross(
+        q, k, v, q_ranges, k_ranges, scale)
+    o, vo = _out_rows(out, q, (n, hq, d), "out")
+    lse = torch.empty((hq, n), dtype=torch.float32, device=q.device)
+    if ws is None:
+        need = lib().scn_cross_attn_fwd_workspace_bytes(SCN_TYPE[dtype], n, m, batch, d, hq, hk)
+        ws = _bytes(need, q.device) if need else None
+    _check(lib().scn_cross_attn_fwd(
+        SCN_TYPE[dtype], n, m, batch, pq, pk, d, hq, hk, _ref(vq), _ref(vk), _ref(vv), scale,
+        _ref(vo), lse.data_ptr(), None if ws is None else ws.data_ptr(),
+        0 if ws is None else ws.numel(), _raw_stream(dev)), "scn_cross_attn_fwd")
+    return o, lse
+
+
+def cross_attn_bwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Tensor,
+                   lse: torch.Tensor, do: torch.Tensor, q_ranges: torch.Tensor,
+                   k_ranges: torch.Tensor, scale: Optional[float] = None,
+                   out=(None, None, None), ws: Optional[torch.Tensor] = None):
+    """Gradients of ``cross_attn_fwd`` (``scn_cross_attn_bwd``): a dict with dq, dk
+    and dv, in ``out`` where given (apart from the inputs).  States of samples
+    without rows of q, and rows of q without states, get 0; rows outside every range
+    are not written."""
+    dtype, dev, n, m, batch, pq, pk, d, hq, hk, vq, vk, vv, scale = _cross(
+        q, k, v, q_ranges, k_ranges, scale)
+    vo = _rows(o, dtype, dev, (n, hq, d), "o")
+    vg = _rows(do, dtype, dev, (n, hq, d), "do")
+    pl = _vector(lse, torch.float32, dev, (hq, n), "lse")
+    dq, wq = _out_rows(out[0], q, (n, hq, d), "out[0]")
+    dk, wk = _out_rows(out[1], q, (m, hk, d), "out[1]")
+    dv, wv = _out_rows(out[2], q, (m, hk, d), "out[2]")
+    if ws is None:
+        ws = _bytes(lib().scn_cross_attn_bwd_workspace_bytes(SCN_TYPE[dtype], n, m, batch, d, hq,
+                                                             hk), q.device)
+    _check(lib().scn_cross_attn_bwd(
+        SCN_TYPE[dtype], n, m, batch, pq, pk, d, hq, hk, _ref(vq), _ref(vk), _ref(vv), _ref(vo), pl,
+        _ref(vg), scale, _ref(wq), _ref(wk), _ref(wv), ws.data_ptr(), ws.numel(),
+        _raw_stream(dev)), "scn_cross_attn_bwd")
+    return {"dq": dq, "dk": dk, "dv": dv}
+
+
+# ---------------------------------------------------------------------------
+# norms around a block, clipping
+# ---------------------------------------------------------------------------
+
+def _matrix(t, dtype, device: int, shape, name: str):
+    """ctypes view of a [rows, channels] tensor (any row stride with contiguous
+    channels), or None."""
+    if t is None:
+        return None
+    if not (isinstance(t, torch.Tensor) and t.dtype == dtype and t.is_cuda and
+            t.get_device() == device and t.shape == shape):
+        _refuse_rows(t, dtype, device, shape, name)
+    row, one = t.stride()
+    if one != 1 and shape[1] > 1:
+        raise ValueError(f"{name} must have contiguous channels")
+    return _Rows(t.data_ptr(), row if shape[0] > 1 else 0)
+
+
+def _out_matrix(t, dtype, device, shape, name: str):
+    """(result, its view), allocated here unless given; a given result's rows must
+    not overlap."""
+    if t is None:
+        t = torch.empty(shape, dtype=dtype, device=device)
+        return t, _Rows(t.data_ptr(), shape[1])
+    v = _matrix(t, dtype, device.index, shape, name)
+    if shape[0] > 1 and v.row < shape[1]:
+        raise ValueError(f"{name} must not be expanded")
+    return t, v
+
+
+def _block(x, f, z, wf, wh, h):
+    """The call's types, sizes and views; h: whose type the block's rows have without f."""
+    for t, name in ((x, "x"), (f if f is not None else h if h is not None else x, "f")):
+        if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype not in SCN_TYPE:
+            _refuse_rows(t, None, -1, (), name)
+        if t.dim() != 2:
+            raise ValueError(f"{name} must have two dimensions, got {tuple(t.shape)}")
+        typ = t.dtype
+    dev = x.get_device()
+    if dev != torch.cuda.current_device():
+        raise ValueError(f"x is on cuda:{dev}, which is not the current device")
+    if x.dtype == torch.bfloat16 and typ == torch.float32:
+        raise TypeError("a residual of bfloat16 beside rows of float32")
+    shape = tuple(x.shape)
+    return (typ, dev, shape, _matrix(x, x.dtype, dev, shape, "x"), _matrix(f, typ, dev, shape, "f"),
+            _matrix(z, typ, dev, shape, "z"), _vector(wf, torch.float32, dev, (shape[1],), "wf"),
+            _vector(wh, torch.float32, dev, (shape[1],), "wh"))
+
+
+def block_norm_fwd(x: torch.Tensor, f: Optional[torch.Tensor], z: Optional[torch.Tensor],
+                   wf: Optional[torch.Tensor], wh: Optional[torch.Tensor], alpha: float = 1.0,
+                   eps: float = 1e-6, need=("y", "h"), out=(None, None)):
+    """A block's residual, gate and norms in one pass (``scn_block_norm_fwd``):
+    y = alpha x + sigmoid(z) wf n(f) and h = wh n(y), n(t) = t / sqrt(mean t^2 +
+    eps) over each row.  x [n, C] is the residual, float32 or bfloat16; f [n, C] the
+    block's result (None: y = alpha x) and z [n, C] its gate's logits (None: no gate),
+    of one type, bfloat16 beside a float32 residual too; any row strides.  wf, wh
+    float32 [C] or None.  Returns (y, h), None where not in ``need`` (y of x's type, h
+    of f's, or of out[1]'s or x's without f), in ``out`` where given (y may be x, h may
+    be f or z)."""
+    typ, dev, shape, vx, vf, vz, pf, ph = _block(x, f, z, wf, wh, out[1])
+    y, vy = _out_matrix(out[0], x.dtype, x.device, shape, "out[0]") if "y" in need else (None, None)
+    h, vh = _out_matrix(out[1], typ, x.device, shape, "out[1]") if "h" in need else (None, None)
+    _check(lib().scn_block_norm_fwd(
+        SCN_TYPE[x.dtype], SCN_TYPE[typ], shape[0], shape[1], _ref(vx), _ref(vf), _ref(vz), pf, ph,
+        alpha, eps, _ref(vy), _ref(vh), _raw_stream(dev)), "scn_block_norm_fwd")
+    return y, h
+
+
+def block_norm_bwd(x: torch.Tensor, f: Optional[torch.Tensor], z: Optional[torch.Tensor],
+                   wf: Optional[torch.Tensor], wh: Optional[torch.Tensor],
+                   dy: Optional[torch.Tensor], dh: Optional[torch.Tensor], alpha: float = 1.0,
+                   eps: float = 1e-6, need=("dwf", "dwh"), out=(None, None, None),
+                   ws: Optional[torch.Tensor] = None):
+    """Gradients of ``block_norm_fwd`` (``scn_block_norm_bwd``) for given dy (None:
+    y has no other use than h) and dh (None: no h): a dict with dx, df and dz (with f
+    and z alone; in ``out`` where given: dx may be dy, df and dz may be dh, f or z) and
+    the requested ones of dwf, dwh."""
+    typ, dev, shape, vx, vf, vz, pf, ph = _block(x, f, z, wf, wh, dh)
+    vgy = _matrix(dy, x.dtype, dev, shape, "dy")
+    vgh = _matrix(dh, typ, dev, shape, "dh")
+    res, vdf, vdz = {}, None, None
+    res["dx"], vdx = _out_matrix(out[0], x.dtype, x.device, shape, "out[0]")
+    if f is not None:
+        res["df"], vdf = _out_matrix(out[1], typ, x.device, shape, "out[1]")
+    if z is not None:
+        res["dz"], vdz = _out_matrix(out[2], typ, x.device, shape, "out[2]")
+    pw = {}
+    for name in ("dwf", "dwh"):
+        if name in need and (name == "dwh" or f is not None):
+            res[name] = torch.empty(shape[1], dtype=torch.float32, device=x.device)
+            pw[name] = res[name].data_ptr()
+    if ws is None:
+        ws = _bytes(lib().scn_block_norm_bwd_workspace_bytes(*shape) if pw else 0, x.device)
+    _check(lib().scn_block_norm_bwd(
+        SCN_TYPE[x.dtype], SCN_TYPE[typ], shape[0], shape[1], _ref(vx), _ref(vf), _ref(vz), pf, ph,
+        alpha, eps, _ref(vgy), _ref(vgh), _ref(vdx), _ref(vdf), _ref(vdz), pw.get("dwf"),
+        pw.get("dwh"), ws.data_ptr(), ws.numel(), _raw_stream(dev)), "scn_block_norm_bwd")
+    return res
+
+
+def clip_grads(grads: Sequence[torch.Tensor], max_norm: float,
+               out: Optional[Sequence[torch.Tensor]] = None,
+               ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Clips gradients by the norm of all of them together (``scn_grad_clip``), in
+    place or into ``out``: where the norm is finite and above ``max_norm`` (infinity:
+    never) they are scaled by max_norm / norm.  Contiguous tensors, float32 and
+    bfloat16 in any mix.  Returns the norm before, a float32 scalar on the device;
+    nothing waits for it."""
+    dev = torch.cuda.current_device()
+    rows, outs = [], None
+    for i, t in enumerate(grads):
+        if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype not in SCN_TYPE:
+            _refuse_rows(t, None, -1, (), f"grads[{i}]")
+        if t.get_device() != dev:
+            raise ValueError(f"grads[{i}] is on cuda:{t.get_device()}, which is not the current "
+                             "device")
+        if not t.is_contiguous():
+            raise ValueError(f"grads[{i}] must be contiguous")
+        rows.append((t.data_ptr(), t.numel(), SCN_TYPE[t.dtype]))
+    if out is not None:
+        if len(out) != len(rows):
+            raise ValueError(f"out must hold {len(rows)} tensors, got {len(out)}")
+        for i, (o, t) in enumerate(zip(out, grads)):
+            if _vector(o, t.dtype, dev, t.shape, f"out[{i}]") is None:
+                raise TypeError(f"out[{i}] must be a CUDA (HIP) tensor")
+        outs = np.array([o.data_ptr() for o in out], dtype=np.uint64)
+    table = np.array(rows, dtype=np.int64).reshape(len(rows), 3)  # scn_tensor
+    norm = torch.empty((), dtype=torch.float32, device=f"cuda:{dev}")
+    if ws is None:
+        ws = _bytes(lib().scn_grad_clip_workspace_bytes(len(rows)), norm.device)
+    _check(lib().scn_grad_clip(
+        len(rows), table.ctypes.data, None if outs is None else outs.ctypes.data, max_norm,
+        norm.data_ptr(), ws.data_ptr(), ws.numel(), _raw_stream(dev)), "scn_grad_clip")
+    return norm
 
 
 def version() -> str:

@@ -18,7 +18,8 @@ LIB_PATH = os.path.join(HERE, "libscn.so")
 ARCH = "gfx950"
 
 SOURCES = ["common.hip", "rulebook.hip", "keyed.hip", "conv.hip", "tile.hip", "pool.hip",
-           "ceiling.hip", "norm.hip", "attn_fwd.hip", "attn_bwd.hip", "attn_step.hip"]
+           "ceiling.hip", "norm.hip", "attn_fwd.hip", "attn_bwd.hip", "attn_step.hip",
+           "cross_fwd.hip", "cross_bwd.hip", "block.hip", "clip.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 

@@ -1,0 +1,303 @@
+// The norm of many tensors taken together, and their scaling to a largest norm.
+//
+//   norm = sqrt(sum over all of t^2),   out = norm > most ? t most / norm : t
+// Two kernels: one sums squares, in 64 bits (no square of an fp32 number leaves their
+// range, and the sum's rounding is far below fp32's), a number a block; in the other every
+// block adds up those numbers in the same order, so that the scale need not be waited for,
+// and scales its share, or leaves at once where nothing changes in place.  Memory bounds
+// both.  The tensors' addresses travel in the kernels' arguments, up to TABLE of them a launch.
+#include <algorithm>
+#include <cmath>
+#include <new>
+#include <vector>
+
+#include "attn.h"
+
+namespace scn {
+namespace {
+
+constexpr int NT = 256;
+constexpr int TABLE = 128;       // tensors of a launch (28 bytes each; arguments end at 4 KB)
+constexpr int CHUNK = 8192;      // elements that a block takes at a time
+constexpr int BLOCKS = 2048;     // of all launches together, each at least LEAST
+constexpr int LEAST = 64;
+
+struct Table {
+  const void* in[TABLE];
+  void* out[TABLE];
+  int64_t n[TABLE];        // elements; bit 62: bf16
+  int32_t start[TABLE];    // chunks of the tensors before
+  int32_t count, chunks;
+  int32_t moved;           // whether any result is not its gradient's place
+};
+constexpr int64_t IS_BF16 = int64_t(1) << 62;
+
+typedef uint32_t v4u_any __attribute__((ext_vector_type(4), aligned(2)));
+typedef float v4f_any __attribute__((ext_vector_type(4), aligned(4)));
+
+// What the block does with each of its chunks: what(tensor, first element, elements)
+template <class F>
+__device__ inline void each_chunk(const Table& t, const F& what) {
+  for (int c = blockIdx.x; c < t.chunks; c += gridDim.x) {
+    int lo = 0, hi = t.count;  // the last tensor that starts at c or before
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (t.start[mid] <= c) lo = mid;
+      else hi = mid;
+    }
+    const int64_t n = t.n[lo] & ~IS_BF16, first = (int64_t)(c - t.start[lo]) * CHUNK;
+    what(lo, first, (int)min((int64_t)CHUNK, n - first));
+  }
+}
+
+__device__ inline double block_sum(double v) {
+  __shared__ double red[NT / 64];
+#pragma unroll
+  for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = red[0];
+#pragma unroll
+  for (int w = 1; w < NT / 64; ++w) v += red[w];
+  return v;
+}
+
+__global__ void __launch_bounds__(NT) grad_squares_kernel(Table t, double* part) {
+  double s[4] = {0., 0., 0., 0.};
+  each_chunk(t, [&](int i, int64_t first, int n) {
+    if (t.n[i] & IS_BF16) {
+      const uint16_t* const p = static_cast<const uint16_t*>(t.in[i]) + first;
+      constexpr int N = CHUNK / NT / 8;
+      v4u x[N];
+#pragma unroll
+      for (int u = 0; u < N; ++u) {
+        const int e = (u * NT + threadIdx.x) * 8;
+        x[u] = v4u{0, 0, 0, 0};
+        if (e + 8 <= n) x[u] = *reinterpret_cast<const v4u_any*>(p + e);
+      }
+      if ((int)threadIdx.x < (n & 7)) {
+        const double v = Elem<1>::get(p[(n & ~7) + threadIdx.x]);
+        s[0] = fma(v, v, s[0]);
+      }
+#pragma unroll
+      for (int u = 0; u < N; ++u)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const double a = __uint_as_float(x[u][j] << 16), b = __uint_as_float(x[u][j] & 0xffff0000u);
+          s[j] = fma(a, a, s[j]);
+          s[j] = fma(b, b, s[j]);
+        }
+    } else {
+      const float* const p = static_cast<const float*>(t.in[i]) + first;
+      constexpr int N = CHUNK / NT / 4;
+      v4f x[N];
+#pragma unroll
+      for (int u = 0; u < N; ++u) {
+        const int e = (u * NT + threadIdx.x) * 4;
+        x[u] = v4f{0.f, 0.f, 0.f, 0.f};
+        if (e + 4 <= n) x[u] = *reinterpret_cast<const v4f_any*>(p + e);
+      }
+      if ((int)threadIdx.x < (n & 3)) {
+        const double v = p[(n & ~3) + threadIdx.x];
+        s[0] = fma(v, v, s[0]);
+      }
+#pragma unroll
+      for (int u = 0; u < N; ++u)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[j] = fma((double)x[u][j], (double)x[u][j], s[j]);
+    }
+  });
+  const double v = block_sum((s[0] + s[1]) + (s[2] + s[3]));
+  if (threadIdx.x == 0) part[blockIdx.x] = v;
+}
+
+// `norm` (of the first launch alone) gets the norm.
+__global__ void __launch_bounds__(NT) grad_scale_kernel(Table t, const double* part, int parts,
+                                                        double most, float* norm) {
+  double s = 0.;
+#pragma unroll 4
+  for (int i = threadIdx.x; i < parts; i += NT) s += part[i];
+  const double all = sqrt(block_sum(s));
+  if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)all;
+  // (a norm that is not finite leaves all as it is)
+  const bool clip = all > most && all < (double)INFINITY;
+  const double by = clip ? most / all : 1.;
+  const float byf = (float)by;
+  if (!clip && !t.moved) return;
+  each_chunk(t, [&](int i, int64_t first, int n) {
+    if (!clip && t.in[i] == t.out[i]) return;
+    if (t.n[i] & IS_BF16) {
+      const uint16_t* const p = static_cast<const uint16_t*>(t.in[i]) + first;
+      uint16_t* const o = static_cast<uint16_t*>(t.out[i]) + first;
+      constexpr int N = CHUNK / NT / 8;
+      v4u x[N];
+#pragma unroll
+      for (int u = 0; u < N; ++u) {
+        const int e = (u * NT + threadIdx.x) * 8;
+        if (e + 8 <= n) x[u] = *reinterpret_cast<const v4u_any*>(p + e);
+      }
+      if ((int)threadIdx.x < (n & 7)) {
+        const int e = (n & ~7) + threadIdx.x;
+        o[e] = clip ? Elem<1>::put(Elem<1>::get(p[e]) * byf) : p[e];
+      }
+#pragma unroll
+      for (int u = 0; u < N; ++u) {
+        const int e = (u * NT + threadIdx.x) * 8;
+        if (e + 8 > n) continue;
+        if (clip)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            x[u][j] = cvt2_bf16(__uint_as_float(x[u][j] << 16) * byf,
+                                __uint_as_float(x[u][j] & 0xffff0000u) * byf);
+        *reinterpret_cast<v4u_any*>(o + e) = x[u];
+      }
+    } else {
+      const float* const p = static_cast<const float*>(t.in[i]) + first;
+      float* const o = static_cast<float*>(t.out[i]) + first;
+      constexpr int N = CHUNK / NT / 4;
+      v4f x[N];
+#pragma unroll
+      for (int u = 0; u < N; ++u) {
+        const int e = (u * NT + threadIdx.x) * 4;
+        if (e + 4 <= n) x[u] = *reinterpret_cast<const v4f_any*>(p + e);
+      }
+      if ((int)threadIdx.x < (n & 3)) {
+        const int e = (n & ~3) + threadIdx.x;
+        o[e] = (float)(p[e] * by);
+      }
+      // (products in 64 bits round once)
+#pragma unroll
+      for (int u = 0; u < N; ++u) {
+        const int e = (u * NT + threadIdx.x) * 4;
+        if (e + 4 > n) continue;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[u][j] = (float)(x[u][j] * by);
+        *reinterpret_cast<v4f_any*>(o + e) = x[u];
+      }
+    }
+  });
+}
+
+int launches(int64_t count) { return (int)std::max<int64_t>(1, ceil_div(count, TABLE)); }
+int blocks_each(int n) { return std::max(LEAST, BLOCKS / n); }
+
+int64_t size_of(const scn_tensor& t) { return t.type == SCN_BF16 ? 2 : 4; }
+
+// Results must lie apart from each other and from all gradients but their own.
+bool apart(int64_t count, const scn_tensor* grads, void* const* out) {
+  struct Piece {
+    uintptr_t lo, hi;
+    bool result;
+  };
+  std::vector<Piece> all;
+  all.reserve(2 * count);
+  for (int64_t i = 0; i < count; ++i) {
+    if (grads[i].n == 0) continue;
+    const uintptr_t in = reinterpret_cast<uintptr_t>(grads[i].p), size = grads[i].n * size_of(grads[i]);
+    const uintptr_t to = out ? reinterpret_cast<uintptr_t>(out[i]) : in;
+    all.push_back({to, to + size, true});
+    if (to != in) all.push_back({in, in + size, false});
+  }
+  std::sort(all.begin(), all.end(), [](const Piece& a, const Piece& b) { return a.lo < b.lo; });
+  uintptr_t any = 0, result = 0;  // ends of the pieces so far, and of the results among them
+  for (const Piece& p : all) {
+    if (p.lo < (p.result ? any : result)) return false;
+    any = std::max(any, p.hi);
+    if (p.result) result = std::max(result, p.hi);
+  }
+  return true;
+}
+
+}  // namespace
+}  // namespace scn
+
+using namespace scn;
+
+extern "C" {
+
+size_t scn_grad_clip_workspace_bytes(int64_t count) {
+  if (count < 0) return 0;
+  const int n = launches(count);
+  return (size_t)n * blocks_each(n) * sizeof(double);
+}
+
+scn_status scn_grad_clip(int64_t count, const scn_tensor* grads, void* const* out, double most,
+                         float* norm, void* ws, size_t ws_bytes, hipStream_t st) {
+  clear_error();
+  const char* const who = "scn_grad_clip";
+  if (count < 0 || (count > 0 && !grads) || !norm || !(most >= 0.)) {
+    set_error("%s: bad count, no gradients, no norm, or a largest norm that is negative or NaN", who);
+    return SCN_ERR_INVALID;
+  }
+  if (count > (1 << 20)) {
+    set_error("%s: more than 2^20 tensors", who);
+    return SCN_ERR_OVERFLOW;
+  }
+  int64_t total = 0;
+  for (int64_t i = 0; i < count; ++i) {
+    const scn_tensor& t = grads[i];
+    if ((t.type != SCN_F32 && t.type != SCN_BF16) || t.n < 0) {
+      set_error("%s: tensor %lld has an unknown type or a negative size", who, (long long)i);
+      return SCN_ERR_INVALID;
+    }
+    const void* const o = out ? out[i] : t.p;
+    if (t.n > 0 && (!t.p || !o || (reinterpret_cast<uintptr_t>(t.p) | reinterpret_cast<uintptr_t>(o)) %
+                                          size_of(t) != 0)) {
+      set_error("%s: tensor %lld or its result is null or misaligned", who, (long long)i);
+      return SCN_ERR_INVALID;
+    }
+    if (t.n > (int64_t(1) << 40) - total) {
+      set_error("%s: more than 2^40 elements", who);
+      return SCN_ERR_OVERFLOW;
+    }
+    total += t.n;
+  }
+  if (!ws || reinterpret_cast<uintptr_t>(ws) % 8 != 0 ||
+      ws_bytes < scn_grad_clip_workspace_bytes(count)) {
+    set_error("%s: workspace missing, misaligned or too small", who);
+    return SCN_ERR_WORKSPACE;
+  }
+  try {
+    if (!apart(count, grads, out)) {
+      set_error("%s: results overlap each other or another gradient", who);
+      return SCN_ERR_INVALID;
+    }
+  } catch (const std::bad_alloc&) {
+    set_error("%s: no host memory", who);
+    return SCN_ERR_NOMEM;
+  }
+  double* const part = static_cast<double*>(ws);
+  const int each = blocks_each(launches(count));
+  int parts = 0;
+  for (int pass = 0; pass < 2; ++pass) {
+    int64_t i = 0;
+    bool first = true;
+    do {
+      Table t;
+      t.count = t.chunks = t.moved = 0;
+      for (; i < count && t.count < TABLE; ++i) {
+        if (grads[i].n == 0) continue;
+        t.in[t.count] = grads[i].p;
+        t.out[t.count] = out ? out[i] : grads[i].p;
+        t.n[t.count] = grads[i].n | (grads[i].type == SCN_BF16 ? IS_BF16 : 0);
+        t.moved |= t.in[t.count] != t.out[t.count];
+        t.start[t.count++] = t.chunks;
+        t.chunks += (int32_t)ceil_div(grads[i].n, CHUNK);
+      }
+      const int blocks = std::max(1, std::min(t.chunks, each));
+      if (pass == 0) {
+        hipLaunchKernelGGL(grad_squares_kernel, dim3((unsigned)blocks), dim3(NT), 0, st, t,
+                           part + parts);
+        parts += blocks;
+      } else {
+        hipLaunchKernelGGL(grad_scale_kernel, dim3((unsigned)blocks), dim3(NT), 0, st, t, part,
+                           parts, most, first ? norm : nullptr);
+      }
+      SCN_LAUNCH_CHECK();
+      first = false;
+    } while (i < count);
+  }
+  return SCN_OK;
+}
+
+}  // extern "C"
