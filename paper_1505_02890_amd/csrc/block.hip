@@ -37,7 +37,6 @@ struct BlockArgs {
   Rows<T> h;     // or df
   Rows<T> dz;
   float* part;   // [2][blocks][C]: dwf, dwh
-  bool past;     // results past the caches
 };
 
 // Eight channels from any element on.  (The hardware takes loads and stores of 16 bytes at
@@ -66,27 +65,19 @@ __device__ inline void get8(const typename Elem<NS>::T* p, int n, float (&v)[8])
   }
 }
 template <int NS>
-__device__ inline void put8(typename Elem<NS>::T* p, int n, const float (&v)[8], bool past) {
+__device__ inline void put8(typename Elem<NS>::T* p, int n, const float (&v)[8]) {
   if (n < 8) {
 #pragma unroll
     for (int j = 0; j < 8; ++j)
       if (j < n) p[j] = Elem<NS>::put(v[j]);
   } else if constexpr (NS == 1) {
-    v4u_any a, *const q = reinterpret_cast<v4u_any*>(p);
+    v4u_any a;
 #pragma unroll
     for (int j = 0; j < 4; ++j) a[j] = cvt2_bf16(v[2 * j], v[2 * j + 1]);
-    if (past) __builtin_nontemporal_store(a, q);
-    else *q = a;
+    *reinterpret_cast<v4u_any*>(p) = a;
   } else {
-    v4f_any *const q = reinterpret_cast<v4f_any*>(p), *const r = reinterpret_cast<v4f_any*>(p + 4);
-    const v4f_any a = {v[0], v[1], v[2], v[3]}, b = {v[4], v[5], v[6], v[7]};
-    if (past) {
-      __builtin_nontemporal_store(a, q);
-      __builtin_nontemporal_store(b, r);
-    } else {
-      *q = a;
-      *r = b;
-    }
+    *reinterpret_cast<v4f_any*>(p) = v4f_any{v[0], v[1], v[2], v[3]};
+    *reinterpret_cast<v4f_any*>(p + 4) = v4f_any{v[4], v[5], v[6], v[7]};
   }
 }
 
@@ -97,21 +88,9 @@ struct Group {
   static constexpr int ROWS = THREADS / LP;  // rows of a block at once
   static constexpr int WAVES = LP > 64 ? LP / 64 : 1;
   // (two places in turn: a sum's readers are past it when the one after the next is written)
-  double (*red)[WAVES];
+  float (*red)[WAVES];
   int turn = 0;
 
-  template <class T>
-  __device__ inline T across(T v) {
-    if constexpr (LP > 64) {
-      turn ^= 1;
-      if ((threadIdx.x & 63) == 0) reinterpret_cast<T*>(red[turn])[threadIdx.x >> 6] = v;
-      __syncthreads();
-      v = T(0);
-#pragma unroll
-      for (int w = 0; w < WAVES; ++w) v += reinterpret_cast<const T*>(red[turn])[w];
-    }
-    return v;
-  }
   __device__ inline float sum(float v) {
     v = group_sum<(LP < 16 ? LP : 16)>(v);
     if constexpr (LP >= 32) {
@@ -120,43 +99,61 @@ struct Group {
       v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
     }
     if constexpr (LP >= 64) v = both_sum(v);
-    return across(v);
-  }
-  __device__ inline double sum(double v) {
+    if constexpr (LP > 64) {
+      turn ^= 1;
+      if ((threadIdx.x & 63) == 0) red[turn][threadIdx.x >> 6] = v;
+      __syncthreads();
+      v = 0.f;
 #pragma unroll
-    for (int d = 1; d < LP && d < 64; d <<= 1) v += __shfl_xor(v, d);
-    return across(v);
+      for (int w = 0; w < WAVES; ++w) v += red[turn][w];
+    }
+    return v;
+  }
+  // <a, b> over the row.  Channels below `own` of a lane are its neighbour's too, which
+  // counts them; only rows of other than whole eights have such.
+  __device__ inline float dot(const float (&a)[8], const float (&b)[8], int own, bool odd) {
+    float s = 0.f;
+    if (odd) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s = fmaf(j >= own ? a[j] : 0.f, b[j], s);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s = fmaf(a[j], b[j], s);
+    }
+    return sum(s);
   }
 };
 
-// v to its norm; returns 1 / sqrt(mean v^2 + eps).  Channels below `own` of a lane are its
-// neighbour's too, which counts them.  Rows whose squares leave fp32's range take 64 bits.
+// v to its norm; returns 1 / sqrt(mean v^2 + eps).  Rows whose squares leave fp32's range, or
+// its best part where eps does not hide it, are scaled by a power of two first.
 template <int LP>
-__device__ inline float norm8(Group<LP>& g, const float (&v)[8], int own, float eps, float inv,
-                              float (&out)[8]) {
-  float s = 0.f;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) s = fmaf(j >= own ? v[j] : 0.f, v[j], s);
-  s = g.sum(s);
-  if (s > 0x1p-100f && s < 0x1p120f) {
-    const float r = rsqrtf(fmaf(s, inv, eps));
+__device__ inline float norm8(Group<LP>& g, const float (&v)[8], int own, bool odd, float eps,
+                              float inv, float (&out)[8]) {
+  const float s = g.dot(v, v, own, odd);
+  if (s < 0x1p120f && (s > 0x1p-100f || eps > 0x1p-80f)) {
+    const float r = __builtin_amdgcn_rsqf(fmaf(s, inv, eps));
 #pragma unroll
     for (int j = 0; j < 8; ++j) out[j] = v[j] * r;
     return r;
   }
-  double d = 0.;
+  const float by = s < 1.f ? 0x1p100f : 0x1p-72f;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) d += j >= own ? (double)v[j] * v[j] : 0.;
-  d = g.sum(d);
-  const double r = 1. / sqrt(d * inv + eps);
+  for (int j = 0; j < 8; ++j) out[j] = v[j] * by;
+  const float r = __builtin_amdgcn_rsqf(fmaf(g.dot(out, out, own, odd), inv, eps * by * by));
 #pragma unroll
-  for (int j = 0; j < 8; ++j) out[j] = (float)(v[j] * r);
-  return (float)r;
+  for (int j = 0; j < 8; ++j) out[j] *= r;
+  return fminf(r * by, 0x1.fffffep127f);
 }
 
-// sigmoid(z) and what it lacks to 1, both without cancellation
+// sigmoid(z) and what it lacks to 1, both without cancellation and within some units: with
+// t = -|z| log2(e) rounded, exp(-|z|) = 2^t (1 + what t lacks ln 2)
 __device__ inline void gate(float z, float& g, float& rest) {
-  const float e = expf(-fabsf(z)), a = 1.f / (1.f + e), b = e * a;
+  const float y = -fabsf(z), t = y * 0x1.715476p+0f;
+  const float lack = fmaf(y, 0x1.4ae0bep-26f, fmaf(y, 0x1.715476p+0f, -t));
+  float e = __builtin_amdgcn_exp2f(t);
+  e = fmaf(e, lack * LN2, e);
+  e = y < -126.f ? 0.f : e;  // (an infinite z has no t to lack from)
+  const float a = __builtin_amdgcn_rcpf(1.f + e), b = e * a;
   g = z < 0.f ? b : a;
   rest = z < 0.f ? a : b;
 }
@@ -186,9 +183,10 @@ __device__ inline void ones8(const float* w, const Channels& ch, float (&v)[8]) 
 
 template <int RS, int TS, int LP>
 __global__ void __launch_bounds__(Group<LP>::THREADS) block_fwd_kernel(BlockArgs<RS, TS> a) {
-  __shared__ double red[2][Group<LP>::WAVES];
+  __shared__ float red[2][Group<LP>::WAVES];
   Group<LP> g{red};
   const Channels ch = Channels::of<LP>(a.C);
+  const bool odd = a.C % 8 != 0;
   float wf[8], wh[8];
   ones8(a.wf, ch, wf);
   ones8(a.wh, ch, wh);
@@ -208,7 +206,7 @@ __global__ void __launch_bounds__(Group<LP>::THREADS) block_fwd_kernel(BlockArgs
     for (int j = 0; j < 8; ++j) x[j] *= a.alpha;
     if (a.f.p) {
       float u[8];
-      norm8(g, f, ch.own, a.eps, a.inv, u);
+      norm8(g, f, ch.own, odd, a.eps, a.inv, u);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         float s = 1.f, rest;
@@ -216,13 +214,13 @@ __global__ void __launch_bounds__(Group<LP>::THREADS) block_fwd_kernel(BlockArgs
         x[j] = fmaf(s, u[j] * wf[j], x[j]);
       }
     }
-    if (a.y.p && ch.on) put8<RS>(a.y.p + t * a.y.row + ch.c, ch.n, x, a.past);
+    if (a.y.p && ch.on) put8<RS>(a.y.p + t * a.y.row + ch.c, ch.n, x);
     if (!a.h.p) continue;
     float u[8];
-    norm8(g, x, ch.own, a.eps, a.inv, u);
+    norm8(g, x, ch.own, odd, a.eps, a.inv, u);
 #pragma unroll
     for (int j = 0; j < 8; ++j) u[j] *= wh[j];
-    if (ch.on) put8<TS>(a.h.p + t * a.h.row + ch.c, ch.n, u, a.past);
+    if (ch.on) put8<TS>(a.h.p + t * a.h.row + ch.c, ch.n, u);
   }
 }
 
@@ -231,10 +229,11 @@ __global__ void __launch_bounds__(Group<LP>::THREADS) block_fwd_kernel(BlockArgs
 template <int RS, int TS, int LP>
 __global__ void __launch_bounds__(Group<LP>::THREADS) block_bwd_kernel(BlockArgs<RS, TS> a) {
   constexpr int ROWS = Group<LP>::ROWS;
-  __shared__ double red[2][Group<LP>::WAVES];
+  __shared__ float red[2][Group<LP>::WAVES];
   __shared__ float share[NT / 64][2][LP * 8];
   Group<LP> g{red};
   const Channels ch = Channels::of<LP>(a.C);
+  const bool odd = a.C % 8 != 0;
   float wf[8], wh[8], dwf[8], dwh[8];
   ones8(a.wf, ch, wf);
   ones8(a.wh, ch, wh);
@@ -261,44 +260,41 @@ __global__ void __launch_bounds__(Group<LP>::THREADS) block_bwd_kernel(BlockArgs
       if (a.z.p) gate(z[j], s[j], rest[j]);
     }
     if (a.f.p) {
-      rf = norm8(g, f, ch.own, a.eps, a.inv, f);
+      rf = norm8(g, f, ch.own, odd, a.eps, a.inv, f);
 #pragma unroll
       for (int j = 0; j < 8; ++j) x[j] = fmaf(s[j], f[j] * wf[j], x[j]);
     }
     if (a.dh.p) {
-      const float ry = norm8(g, x, ch.own, a.eps, a.inv, x);
-      float m = 0.f;
+      const float ry = norm8(g, x, ch.own, odd, a.eps, a.inv, x);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         dwh[j] = fmaf(dh[j], x[j], dwh[j]);
         dh[j] *= wh[j];
-        m = fmaf(j >= ch.own ? dh[j] : 0.f, x[j], m);
       }
-      m = g.sum(m) * a.inv;
+      const float m = g.dot(dh, x, ch.own, odd) * a.inv;
 #pragma unroll
       for (int j = 0; j < 8; ++j) dy[j] = fmaf(ry, dh[j] - x[j] * m, dy[j]);
     }
     if (a.f.p) {
-      float m = 0.f, d[8];
+      float d[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const float du = dy[j] * s[j];
         z[j] = du * (f[j] * wf[j]) * rest[j];
         dwf[j] = fmaf(du, f[j], dwf[j]);
         d[j] = du * wf[j];
-        m = fmaf(j >= ch.own ? d[j] : 0.f, f[j], m);
       }
-      m = g.sum(m) * a.inv;
+      const float m = g.dot(d, f, ch.own, odd) * a.inv;
 #pragma unroll
       for (int j = 0; j < 8; ++j) d[j] = rf * (d[j] - f[j] * m);
       if (ch.on) {
-        put8<TS>(a.h.p + t * a.h.row + ch.c, ch.n, d, a.past);
-        if (a.dz.p) put8<TS>(a.dz.p + t * a.dz.row + ch.c, ch.n, z, a.past);
+        put8<TS>(a.h.p + t * a.h.row + ch.c, ch.n, d);
+        if (a.dz.p) put8<TS>(a.dz.p + t * a.dz.row + ch.c, ch.n, z);
       }
     }
 #pragma unroll
     for (int j = 0; j < 8; ++j) dy[j] *= a.alpha;
-    if (ch.on) put8<RS>(a.y.p + t * a.y.row + ch.c, ch.n, dy, a.past);
+    if (ch.on) put8<RS>(a.y.p + t * a.y.row + ch.c, ch.n, dy);
   }
   if (!a.part) return;
   if constexpr (LP <= 64) {
@@ -335,29 +331,33 @@ __global__ void __launch_bounds__(Group<LP>::THREADS) block_bwd_kernel(BlockArgs
   }
 }
 
-// dwf and dwh: the blocks' shares part[2][blocks][C], in a fixed order: block (weight, 32
-// channels), 32 threads to a channel
+// dwf and dwh: the blocks' shares part[2][blocks][C], in a fixed order: block (weight, eight
+// channels), 128 threads to a channel
 __global__ void __launch_bounds__(1024) block_dw_kernel(const float* part, int blocks, int C,
                                                         float* dwf, float* dwh) {
-  __shared__ float red[32][33];
+  __shared__ float red[16][8];
   float* const out = blockIdx.x & 1 ? dwh : dwf;
   if (!out) return;
-  const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5;
-  const int c = (blockIdx.x >> 1) * 32 + lane;
+  const int c = (blockIdx.x >> 1) * 8 + threadIdx.x % 8;
   const float* const p = part + (int64_t)(blockIdx.x & 1) * blocks * C;
   float v = 0.f;
   if (c < C)
-#pragma unroll 4
-    for (int i = slice; i < blocks; i += 32) v += p[(int64_t)i * C + c];
-  red[slice][lane] = v;
-  __syncthreads();
-  v = red[lane][slice];  // slice's channel, a share a lane
+#pragma unroll 8
+    for (int i = threadIdx.x / 8; i < blocks; i += 128) v += p[(int64_t)i * C + c];
 #pragma unroll
-  for (int d = 1; d < 32; d <<= 1) v += __shfl_xor(v, d);
-  if (lane == 0 && (blockIdx.x >> 1) * 32 + slice < C) out[(blockIdx.x >> 1) * 32 + slice] = v;
+  for (int d = 8; d < 64; d <<= 1) v += __shfl_xor(v, d);
+  if ((threadIdx.x & 63) < 8) red[threadIdx.x >> 6][threadIdx.x & 7] = v;
+  __syncthreads();
+  if (threadIdx.x >= 8 || c >= C) return;
+  for (int i = 1; i < 16; ++i) v += red[i][threadIdx.x];
+  out[c] = v;
 }
 
-constexpr int BLOCKS = 1024;  // of a backward call with gradients of weights
+// Blocks of a call at most.  Forward: 300,001 rows of 256 channels, bf16, take 139 us in one row a
+// lane group, 150 in 4096 blocks and 177 in 2048.  Backward: as many as reside at once, whose
+// registers hold the weights' gradients (257 us in 1024, the same in 2048, 290 in 768).
+constexpr int FWD_BLOCKS = 1 << 16;
+constexpr int BWD_BLOCKS = 1024;
 
 int lanes(int C) {
   int lp = 4;
@@ -464,12 +464,10 @@ template <int RS, int TS>
 scn_status run(const BlockCall& c, int blocks, hipStream_t st) {
   typedef typename Elem<RS>::T R;
   typedef typename Elem<TS>::T T;
-  const int64_t bytes = c.n * c.C * (int64_t)(sizeof(R) + sizeof(T) * (c.dz ? 2 : 1));
   const BlockArgs<RS, TS> a{c.n, c.C, c.alpha, c.eps, 1.f / (float)c.C, rows<const R>(c.x),
                             rows<const R>(c.dy), rows<const T>(c.f), rows<const T>(c.z),
                             rows<const T>(c.dh), c.wf, c.wh, rows<R>(c.y), rows<T>(c.h),
-                            rows<T>(c.dz), c.part,
-                            c.C * (int64_t)sizeof(T) % 64 == 0 && bytes >= int64_t(64) << 20};
+                            rows<T>(c.dz), c.part};
   switch (lanes(c.C)) {
     case 4: launch<RS, TS, 4>(a, c.bwd, blocks, st); break;
     case 8: launch<RS, TS, 8>(a, c.bwd, blocks, st); break;
@@ -505,12 +503,12 @@ scn_status scn_block_norm_fwd(int32_t res_type, int32_t type, int64_t n, int32_t
                     false};
   if (scn_status rc = check(c)) return rc;
   if (n == 0) return SCN_OK;
-  return run(c, row_blocks(n, C, 1 << 16), st);
+  return run(c, row_blocks(n, C, FWD_BLOCKS), st);
 }
 
 size_t scn_block_norm_bwd_workspace_bytes(int64_t n, int32_t C) {
   if (n < 1 || n > ATTN_ROWS || C < 1 || C > BLOCK_C) return 0;
-  return (size_t)row_blocks(n, C, BLOCKS) * 2 * C * 4;
+  return (size_t)row_blocks(n, C, BWD_BLOCKS) * 2 * C * 4;
 }
 
 scn_status scn_block_norm_bwd(int32_t res_type, int32_t type, int64_t n, int32_t C,
@@ -532,11 +530,11 @@ scn_status scn_block_norm_bwd(int32_t res_type, int32_t type, int64_t n, int32_t
     }
     c.part = static_cast<float*>(ws);
   }
-  const int blocks = n > 0 ? row_blocks(n, C, BLOCKS) : 0;
+  const int blocks = n > 0 ? row_blocks(n, C, BWD_BLOCKS) : 0;
   if (n > 0)
     if (scn_status rc = run(c, blocks, st)) return rc;
   if (want) {
-    hipLaunchKernelGGL(block_dw_kernel, dim3((unsigned)(2 * ceil_div(C, 32))), dim3(1024), 0, st,
+    hipLaunchKernelGGL(block_dw_kernel, dim3((unsigned)(2 * ceil_div(C, 8))), dim3(1024), 0, st,
                        c.part, blocks, C, dwf, dwh);
     SCN_LAUNCH_CHECK();
   }
