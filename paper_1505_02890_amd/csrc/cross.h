@@ -9,69 +9,125 @@
 
 namespace scn {
 
-// Tiles of `rows` tile rows over all samples, numbered as attn.h's with `many` tile rows a row.
-struct Place {
-  int64_t base;  // first row of the sample
-  int m;         // its tile rows
-  int first;     // first tile row of the tile, counted in the sample (m: no such tile)
-  int sample;
+// One side of a call: rows of samples, and how many tile rows each is.
+struct Side {
+  const int32_t* ranges;
+  int64_t n;
+  int many;
+  // first row of sample b
+  __device__ inline int at(int b) const { return (int)range_at(ranges, b, n); }
 };
-__device__ inline int64_t first_tile(const int32_t* ranges, int b, int64_t n, int rows, int many) {
-  return range_at(ranges, b, n) * many / rows + b;
-}
-// Every lane of the wave takes part.
-__device__ inline Place find_place(const int32_t* ranges, int batch, int64_t n, int64_t tile,
-                                   int rows, int many) {
-  const int lane = threadIdx.x & 63;
-  int lo = 0, len = batch;
-  while (len > 1) {
-    const int stride = (len + 63) >> 6, b = lo + lane * stride;
-    const bool below = lane * stride < len && first_tile(ranges, b, n, rows, many) <= tile;
-    const int c = __popcll(__ballot(below));
-    const int step = max(c - 1, 0) * stride;
-    lo += step;
-    len = min(stride, len - step);
-  }
-  Place s;
-  s.sample = __builtin_amdgcn_readfirstlane(lo);
-  const int base = __builtin_amdgcn_readfirstlane((int)range_at(ranges, s.sample, n));
-  const int end = __builtin_amdgcn_readfirstlane((int)range_at(ranges, s.sample + 1, n));
-  s.base = base;
-  s.m = max(0, end - base) * many;
-  const int64_t local = tile - ((int64_t)base * many / rows + s.sample);
-  s.first = local < 0 || local * rows >= s.m ? s.m : (int)(local * rows);
-  return s;
-}
-// The sample of a row; false if it has none.  Every lane of the wave takes part.
-__device__ inline bool find_row(const int32_t* ranges, int batch, int64_t n, int row, int& sample) {
-  const int lane = threadIdx.x & 63;
-  int lo = 0, len = batch;
-  while (len > 1) {
-    const int stride = (len + 63) >> 6, b = lo + lane * stride;
-    const bool below = lane * stride < len && range_at(ranges, b, n) <= row;
-    const int c = __popcll(__ballot(below));
-    const int step = max(c - 1, 0) * stride;
-    lo += step;
-    len = min(stride, len - step);
-  }
-  sample = __builtin_amdgcn_readfirstlane(lo);
-  return range_at(ranges, sample, n) <= row && row < range_at(ranges, sample + 1, n);
-}
-// a sample's rows of the other side
-__device__ inline void find_rows(const int32_t* ranges, int sample, int64_t n, int64_t& base,
-                                 int& m) {
-  const int lo = __builtin_amdgcn_readfirstlane((int)range_at(ranges, sample, n));
-  const int hi = __builtin_amdgcn_readfirstlane((int)range_at(ranges, sample + 1, n));
-  base = lo;
-  m = max(0, hi - lo);
-}
 
-constexpr int MAX_PARTS = 256;  // of a split axis
+// An axis that is split over blocks: a sample of m steps has of(m) parts, at most `most`, of at
+// least `least` steps each but for a sample's last.  Samples differ in length, so the longer
+// have more parts and no block has much more to do than another.
+constexpr int MAX_PARTS = 256;
 
-// Parts of an axis of about `len` steps: `want` blocks in all, at least `least` steps each.
-inline int parts(int64_t blocks, int64_t want, int64_t len, int64_t least) {
-  return (int)std::max<int64_t>(
-      1, std::min({ceil_div(want, std::max<int64_t>(1, blocks)), len / least, (int64_t)MAX_PARTS}));
+struct Parts {
+  int most, least;
+  __host__ __device__ inline int of(int64_t m) const {
+    const int64_t n = (m + least - 1) / least;
+    return n < 1 ? 1 : n > most ? most : (int)n;
+  }
+};
+
+// What a block does: a tile of one side's rows, for a key head, with a part of the other
+// side's steps.
+struct Work {
+  int64_t base, other;  // first rows of the sample on both sides
+  int m, mo;            // its tile rows on the tiles' side, its rows on the other
+  int first;            // first tile row of the tile, counted in the sample (m: no tile)
+  int hk, part, parts;
+};
+
+// The work of a launch, one a block.  Unsplit, tiles of `rows` tile rows are numbered as
+// attn.h's, tile t of sample b being ranges[b] many / rows + b + t, and no block has to know more
+// than its own sample.  Split, each block counts the samples' tiles and parts, 64 samples at a
+// time, so that the blocks without work are the last ones: each costs 2 us of a place on the
+// card.
+struct Deal {
+  Side tiles, steps;
+  int batch, rows, Hk;
+  Parts parts;
+
+  // blocks of a launch
+  int64_t blocks() const { return (tiles.n * tiles.many / rows + batch) * Hk * parts.most; }
+  __device__ inline int count(int b) const {
+    if (b >= batch) return 0;
+    const int m = tiles.at(b + 1) - tiles.at(b), o = steps.at(b + 1) - steps.at(b);
+    if (m <= 0) return 0;
+    return (int)(((int64_t)m * tiles.many + rows - 1) / rows) *
+           parts.of(max(o, 0) * (int64_t)steps.many) * Hk;
+  }
+  // Every lane of the wave takes part.
+  __device__ inline Work find(int item) const {
+    const int lane = threadIdx.x & 63;
+    int sample = 0, local = 0;
+    bool none = false;  // past the last work
+    Work w;
+    if (parts.most == 1) {
+      const int tile = item / Hk;
+      w.hk = item % Hk;
+      int len = batch;
+      while (len > 1) {
+        const int stride = (len + 63) >> 6, b = sample + lane * stride;
+        const bool below = lane * stride < len &&
+                           tiles.at(b) * (int64_t)tiles.many / rows + b <= tile;
+        const int step = max(__popcll(__ballot(below)) - 1, 0) * stride;
+        sample += step;
+        len = min(stride, len - step);
+      }
+      sample = __builtin_amdgcn_readfirstlane(sample);
+      local = tile - (int)(tiles.at(sample) * (int64_t)tiles.many / rows + sample);
+    } else {
+      local = item;
+      for (int b = 0; b < batch; b += 64) {
+        const int c = count(b + lane);
+        int s = c;  // .. of the samples up to this one
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+          const int x = __shfl_up(s, d);
+          s += lane >= d ? x : 0;
+        }
+        const int here = __popcll(__ballot(s <= local));
+        none = here == 64;
+        sample = min(b + here, batch - 1);
+        local -= __shfl(none ? s : s - c, none ? 63 : here);
+        if (!none) break;
+      }
+    }
+    const int base = __builtin_amdgcn_readfirstlane(tiles.at(sample));
+    const int end = __builtin_amdgcn_readfirstlane(tiles.at(sample + 1));
+    const int other = __builtin_amdgcn_readfirstlane(steps.at(sample));
+    const int oend = __builtin_amdgcn_readfirstlane(steps.at(sample + 1));
+    w.base = base;
+    w.m = max(0, end - base) * tiles.many;
+    w.other = other;
+    w.mo = max(0, oend - other);
+    w.parts = parts.of(w.mo * (int64_t)steps.many);
+    w.part = 0;
+    if (parts.most > 1) {
+      const int n = (w.m + rows - 1) / rows * Hk;
+      w.part = n ? __builtin_amdgcn_readfirstlane(local / n) : 0;
+      local -= w.part * n;
+      w.hk = __builtin_amdgcn_readfirstlane(local % Hk);
+      local /= Hk;
+    }
+    local = __builtin_amdgcn_readfirstlane(local);
+    w.first = none || local < 0 || (int64_t)local * rows >= w.m ? w.m : local * rows;
+    return w;
+  }
+};
+
+// `blocks` blocks over samples of about `mean` steps, cut for `want` blocks in all where there
+// are fewer, in parts of `least` steps or more; a sample of twice the mean has all parts that it
+// would have by its length.
+inline Parts cut(int64_t blocks, int64_t want, int64_t mean, int64_t least, int samples) {
+  blocks = std::max<int64_t>(1, blocks);
+  least = std::max(least, ceil_div(blocks * mean, want));
+  if (blocks >= want || mean <= least) return Parts{1, INT32_MAX};
+  const int64_t most = ceil_div(mean, least) * (samples > 1 ? 2 : 1);
+  return Parts{(int)std::min<int64_t>(most, MAX_PARTS), (int)std::min<int64_t>(least, INT32_MAX)};
 }
 
 // host checks of both directions

@@ -14,9 +14,10 @@ namespace {
 template <int NS>
 struct CrossBwdArgs {
   typedef typename Elem<NS>::T T;
-  int64_t nq, nk;
-  int batch, D, Hk, group;
-  const int32_t *qr, *kr;
+  Deal qdeal;  // tiles of queries, parts of their keys
+  Deal kdeal;  // tiles of keys, parts of their queries
+  int D, group;
+  int repeat;  // tiles of queries that a work is, where the keys are few
   Heads<const T> q, k, v, o, d_o;
   Heads<T> dq, dk, dv;
   const float* lse;  // [Hq][nq]
@@ -24,14 +25,9 @@ struct CrossBwdArgs {
   float* lse2;       // [Hq][nq]: lse in log 2, or NaN where it is past LSE_MOST ...
   float* rest;       // [Hq][nq]: ... and what it lacks there
   float scale;
-  int qs, ks;    // parts that the keys are split into for dq, and the queries for dk and dv
-  float* qpart;  // [Hq][nq][qs][2][D] (dQ, PK), then [Hq][nq][qs] (the sum of dS)
-  float* kpart;  // [Hk][nk][ks][2][D] (dK, dV)
-  __device__ inline float* qout(int64_t at, int s) const { return qpart + (at * qs + s) * 2 * D; }
-  __device__ inline float* over(int64_t at) const {
-    return qpart + nq * Hk * group * qs * 2 * D + at * qs;
-  }
-  __device__ inline float* kout(int64_t at, int s) const { return kpart + (at * ks + s) * 2 * D; }
+  float* qpart;  // [Hq][nq][parts][2][D] (dQ, PK), then [Hq][nq][parts] (the sum of dS)
+  float* kpart;  // [Hk][nk][parts][2][D] (dK, dV)
+  __device__ inline int64_t at(int64_t row, int h) const { return h * qdeal.tiles.n + row; }
 };
 
 // dq of one row once more in fp32, over its cnt >= 1 keys, from weights of its own.  The
@@ -67,7 +63,7 @@ __device__ inline void dq_row(const CrossBwdArgs<NS>& a, int64_t row, int h, int
   if (lane < a.D) o[lane] = E::put(o0 * a.scale);
   if (64 + lane < a.D) o[64 + lane] = E::put(o1 * a.scale);
   if (lane == 0) {
-    const int64_t at = h * a.nq + row;
+    const int64_t at = a.at(row, h);
     a.delta[at] = delta;
     a.rest[at] = (r.top - a.lse[at]) + logf(r.sum);
   }
@@ -86,7 +82,7 @@ __device__ inline void dkv_row(const CrossBwdArgs<NS>& a, int64_t row, int hk, i
   bool none = false;
   for (int h = hk * a.group; h < (hk + 1) * a.group; ++h)
     for (int i = lane; i < m; i += 64) {
-      const float l = a.lse[h * a.nq + q0 + i];
+      const float l = a.lse[a.at(q0 + i, h)];
       none |= l != l;
     }
   if (__ballot(none)) {
@@ -101,7 +97,7 @@ __device__ inline void dkv_row(const CrossBwdArgs<NS>& a, int64_t row, int hk, i
       float p = 0.f, ds = 0.f;
       const int i = x0 + lane;
       if (i < m) {
-        const int64_t at = h * a.nq + q0 + i;
+        const int64_t at = a.at(q0 + i, h);
         p = row_dot<NS>(q + i * a.q.row, k, a.D) * a.scale - a.lse[at];
         p = expf(fabsf(a.lse[at]) <= LSE_MOST ? p : p - a.rest[at]);
         ds = p * (row_dot<NS>(g + i * a.d_o.row, v, a.D) - a.delta[at]);
@@ -131,6 +127,12 @@ __device__ inline void dkv_row(const CrossBwdArgs<NS>& a, int64_t row, int hk, i
   }
 }
 
+// where the sums of dS lie that parts of the keys leave
+template <int NS>
+__device__ inline float* over_part(const CrossBwdArgs<NS>& a) {
+  return a.qpart + a.qdeal.tiles.n * a.qdeal.Hk * a.group * a.qdeal.parts.most * 2 * a.D;
+}
+
 // QW waves of 32 tile rows by KW groups that share out the keys of a tile, 32 each
 template <int NS, int DP, int QW, int KW>
 struct QueryShape {
@@ -145,7 +147,8 @@ struct QueryShape {
   static_assert(SMEM <= 160 * 1024, "LDS of a compute unit");
 };
 
-template <int NS, int DP, int QW, int KW>
+// FEW: a work is several tiles of queries in turn
+template <int NS, int DP, int QW, int KW, bool FEW>
 __global__ void __launch_bounds__(64 * QW * KW, (NS == 3 && DP > 32) || DP > 64 ? 1 : 2)
     cross_dq_kernel(CrossBwdArgs<NS> a) {
   typedef QueryShape<NS, DP, QW, KW> X;
@@ -155,62 +158,26 @@ __global__ void __launch_bounds__(64 * QW * KW, (NS == 3 && DP > 32) || DP > 64 
   extern __shared__ char smem[];
   const int tid = threadIdx.x, lane = tid & 63, n32 = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), kw = KW == 1 ? 0 : wave / QW;
-  const int split = blockIdx.x % a.qs, hk = blockIdx.x / a.qs % a.Hk;
-  const Place sp = find_place(a.qr, a.batch, a.nq, blockIdx.x / a.qs / a.Hk, QB, a.group);
-  if (sp.first >= sp.m) return;
-  int64_t k0;
-  int mk;
-  find_rows(a.kr, sp.sample, a.nk, k0, mk);
-  const int r = sp.first + (wave - kw * QW) * 32 + n32;
-  const bool mine = r < sp.m;
-  const int rr = min(r, sp.m - 1);
-  const int64_t row = sp.base + rr / a.group;
-  const int h = hk * a.group + rr % a.group;
   const float c2 = a.scale * LOG2E;
-
-  Frag<NS> Q[DP / 16], G[DP / 16];
-  float delta = 0.f;
-  {
-    const auto* const q = a.q.p + row * a.q.row + h * a.q.head;
-    const auto* const g = a.d_o.p + row * a.d_o.row + h * a.d_o.head;
-    const auto* const o = a.o.p + row * a.o.row + h * a.o.head;
-#pragma unroll
-    for (int s = 0; s < DP / 16; ++s) {
-      Q[s] = load_frag<NS>(q, s, a.D, lane);
-      G[s] = load_frag<NS>(g, s, a.D, lane);
-      const int c = 16 * s + 8 * half;
-      if (c < a.D) {
-        float x[8], y[8];
-        load8<NS>(g + c, x);
-        load8<NS>(o + c, y);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) delta = fmaf(x[j], y[j], delta);
-      }
-    }
-  }
-  delta = both_sum(delta);
-  const int64_t at = h * a.nq + row;
-  const float lse2 = a.lse[at] * LOG2E;
-  const bool far = !(fabsf(a.lse[at]) <= LSE_MOST);  // the row is formed again ...
-  const bool none = a.lse[at] != a.lse[at];           // ... if it has weights at all
-  float over = 0.f;
-  v16f dQ[DP / 32], PK[EXACT ? DP / 32 : 1];
-#pragma unroll
-  for (int d = 0; d < DP / 32; ++d) dQ[d] = zero16();
-  if constexpr (EXACT)
-#pragma unroll
-    for (int d = 0; d < DP / 32; ++d) PK[d] = zero16();
-
-  const int nt = (mk + KT - 1) / KT, per = (nt + a.qs - 1) / a.qs;
-  const int t0 = min(nt, split * per), t1 = min(nt, t0 + per);
-  const auto* const kp = a.k.p + k0 * a.k.row + hk * a.k.head;
-  const auto* const vp = a.v.p + k0 * a.v.row + hk * a.v.head;
   typedef Stage<NS, DP, KT, NT> St;
-  St sk, sv;
   uint32_t ko[St::N], vo[St::N];
   St::places(ko, a.k.row, a.D, tid);
   St::places(vo, a.v.row, a.D, tid);
   const typename L::Lane pl(lane);
+
+  const Work w = a.qdeal.find(blockIdx.x);
+  if (w.first >= w.m) return;
+  const int mk = w.mo, hk = w.hk;
+  const int64_t k0 = w.other;
+  Frag<NS> Q[DP / 16], G[DP / 16];
+  v16f dQ[DP / 32], PK[EXACT ? DP / 32 : 1];
+  float delta, lse2, over;
+
+  const int nt = (mk + KT - 1) / KT, per = (nt + w.parts - 1) / w.parts;
+  const int t0 = min(nt, w.part * per), t1 = min(nt, t0 + per);
+  const auto* const kp = a.k.p + k0 * a.k.row + hk * a.k.head;
+  const auto* const vp = a.v.p + k0 * a.v.row + hk * a.v.head;
+  St sk, sv;
   auto fetch = [&](int t) {
     sk.load(kp, a.k.row, ko, t * KT, mk - t * KT, a.D);
     sv.load(vp, a.v.row, vo, t * KT, mk - t * KT, a.D);
@@ -264,17 +231,56 @@ __global__ void __launch_bounds__(64 * QW * KW, (NS == 3 && DP > 32) || DP > 64 
       }
     }
   };
-  if (t0 < t1) {
+  auto sweep = [&](int first, bool stage) {
+  const int r = first + (wave - kw * QW) * 32 + n32;
+  const bool mine = r < w.m;
+  const int rr = min(r, w.m - 1);
+  const int64_t row = w.base + rr / a.group;
+  const int h = hk * a.group + rr % a.group;
+  delta = over = 0.f;
+  {
+    const auto* const q = a.q.p + row * a.q.row + h * a.q.head;
+    const auto* const g = a.d_o.p + row * a.d_o.row + h * a.d_o.head;
+    const auto* const o = a.o.p + row * a.o.row + h * a.o.head;
+#pragma unroll
+    for (int s = 0; s < DP / 16; ++s) {
+      Q[s] = load_frag<NS>(q, s, a.D, lane);
+      G[s] = load_frag<NS>(g, s, a.D, lane);
+      const int c = 16 * s + 8 * half;
+      if (c < a.D) {
+        float x[8], y[8];
+        load8<NS>(g + c, x);
+        load8<NS>(o + c, y);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) delta = fmaf(x[j], y[j], delta);
+      }
+    }
+  }
+  delta = both_sum(delta);
+  const int64_t at = a.at(row, h);
+  const float lse = a.lse[at];
+  lse2 = lse * LOG2E;
+  const bool far = !(fabsf(lse) <= LSE_MOST);  // the row is formed again ...
+  const bool none = lse != lse;                 // ... if it has weights at all
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d) dQ[d] = zero16();
+  if constexpr (EXACT)
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d) PK[d] = zero16();
+  // the keys, as in cross_fwd.hip
+  if (stage && t0 < t1) {
     fetch(t0);
     put(t0);
     if (t0 + 1 < t1) fetch(t0 + 1);
     __syncthreads();
-    for (int t = t0; t < t1; ++t) {
+  }
+  for (int t = t0; t < t1; ++t) {
+    if (stage) {
       if (t + 1 < t1) put(t + 1);
       if (t + 2 < t1) fetch(t + 2);
-      take(t);
-      __syncthreads();
     }
+    take(t);
+    if (stage) __syncthreads();
   }
   // the groups' sums, joined in order
   over = both_sum(over);
@@ -310,17 +316,18 @@ __global__ void __launch_bounds__(64 * QW * KW, (NS == 3 && DP > 32) || DP > 64 
         }
     }
   }
-  if (a.qs > 1) {
+  if (w.parts > 1) {
     if (mine) {
-      float* const o = a.qout(at, split);
+      const int64_t to = at * a.qdeal.parts.most + w.part;
+      float* const o = a.qpart + to * 2 * a.D;
 #pragma unroll
       for (int d = 0; d < DP / 32; ++d) {
         store_cols<3>(o, dQ[d], 1.f, d, a.D, lane);
         if constexpr (EXACT) store_cols<3>(o + a.D, PK[d], 1.f, d, a.D, lane);
       }
       if (half == 0) {
-        a.over(at)[split] = over;
-        if (split == 0) {
+        over_part(a)[to] = over;
+        if (w.part == 0) {
           a.delta[at] = delta;
           a.lse2[at] = far ? NAN : lse2;
         }
@@ -351,71 +358,118 @@ __global__ void __launch_bounds__(64 * QW * KW, (NS == 3 && DP > 32) || DP > 64 
   }
   const uint64_t bad = __ballot(mine && !none && (far || !fine) && mk > 0);
   uint32_t rows = (uint32_t)bad | (uint32_t)(bad >> 32);
-  const int w0 = sp.first + wave * 32;
+  const int w0 = first + wave * 32;
   for (; rows; rows &= rows - 1) {
     const int x = w0 + __builtin_ctz(rows);
-    dq_row<NS>(a, sp.base + x / a.group, hk * a.group + x % a.group, k0, mk);
+    dq_row<NS>(a, w.base + x / a.group, hk * a.group + x % a.group, k0, mk);
+  }
+  };
+  if constexpr (!FEW) {
+    sweep(w.first, true);
+  } else {
+    const int end = min(w.m, w.first + QB * a.repeat);
+    for (int first = w.first; first < end; first += QB)
+      sweep(first, first == w.first || t1 - t0 > 2);
   }
 }
 
-// The parts of a row's dq, a wave a row and head, channels along the lanes, added up in order
+// A block's threads over `rows` rows of `wide` floats, four a thread, and what threads are left
+// over the rows' parts: each thread's share of the parts of its floats, then all of them, in order, in
+// the threads of slice 0.
+struct Slices {
+  int c, r, sl, slices, lanes, rows;
+  __device__ inline Slices(int wide, int rows_) : rows(rows_) {
+    lanes = wide >> 2;
+    slices = (int)blockDim.x / (lanes * rows);
+    c = threadIdx.x % lanes * 4;
+    r = threadIdx.x / lanes % rows;
+    sl = threadIdx.x / (lanes * rows);
+  }
+  // part s of the thread's floats lies at p[s * step]
+  __device__ inline v4f sum(const float* p, int64_t step, int n, v4f* x, bool on) const {
+    v4f v = {0.f, 0.f, 0.f, 0.f};
+    const int per = (n + slices - 1) / slices, s1 = min(n, (sl + 1) * per);
+    if (on)
+      for (int s0 = sl * per; s0 < s1; s0 += 4) {
+        v4f o[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          o[j] = *reinterpret_cast<const v4f*>(p + min(s0 + j, s1 - 1) * step);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (s0 + j < s1) v += o[j];
+      }
+    if (slices > 1) {
+      x[threadIdx.x] = v;
+      __syncthreads();
+      if (on && sl == 0)
+        for (int s = 1; s < slices; ++s) v += x[s * lanes * rows + threadIdx.x];
+      __syncthreads();
+    }
+    return v;
+  }
+};
+// attn.h's tiny, and what is not finite, of four of a row's floats
 template <int NS>
-__global__ void __launch_bounds__(256) cross_dq_join_kernel(CrossBwdArgs<NS> a) {
-  const int lane = threadIdx.x & 63;
-  const int64_t at = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (at >= a.nq * a.Hk * a.group) return;
-  const int h = (int)(at / a.nq);
-  const int64_t row = at - h * a.nq;
-  int sample;
-  if (!find_row(a.qr, a.batch, a.nq, (int)row, sample)) return;
-  int64_t k0;
-  int mk;
-  find_rows(a.kr, sample, a.nk, k0, mk);
-  float over = 0.f, d[2] = {0.f, 0.f}, p[2] = {0.f, 0.f};
-  for (int s0 = 0; s0 < a.qs; s0 += 4) {
-    float x[4][2], y[4][2], z[4];
+__device__ inline bool fine4(v4f v) {
+  bool fine = true, large = false, any = false;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const bool on = s0 + j < a.qs;
-      const float* const o = a.qout(at, on ? s0 + j : 0);
-      z[j] = on ? a.over(at)[s0 + j] : 0.f;
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        const bool has = on && 64 * c + lane < a.D;
-        x[j][c] = has ? o[64 * c + lane] : 0.f;
-        y[j][c] = NS == 1 && has ? o[a.D + 64 * c + lane] : 0.f;
-      }
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      over += z[j];
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        d[c] += x[j][c];
-        p[c] += y[j][c];
-      }
-    }
+  for (int j = 0; j < 4; ++j) {
+    fine &= fabsf(v[j]) < INFINITY;
+    large |= fabsf(v[j]) >= 0x1p-95f;
+    any |= v[j] != 0.f;
   }
-  const float l = a.lse[at];
-  const bool far = !(fabsf(l) <= LSE_MOST), none = l != l;
+  return fine && (NS == 1 || large || !any);
+}
+template <int NS>
+__device__ inline void store4(typename Elem<NS>::T* p, v4f v, float f) {
+  if constexpr (NS == 1)
+    *reinterpret_cast<v2u*>(p) = v2u{cvt2_bf16(v[0] * f, v[1] * f), cvt2_bf16(v[2] * f, v[3] * f)};
+  else
+    *reinterpret_cast<v4f*>(p) = v4f{v[0] * f, v[1] * f, v[2] * f, v[3] * f};
+}
+
+// The parts of the rows' dq: `qdeal.rows` tile rows a block
+template <int NS>
+__global__ void __launch_bounds__(256) cross_dq_join_kernel(CrossBwdArgs<NS> a, Parts parts) {
+  __shared__ v4f x[256];
+  __shared__ bool bad[128];
+  const Work w = a.qdeal.find(blockIdx.x);
+  const int n = parts.of(w.mo);
+  if (w.first >= w.m || n == 1) return;
+  const Slices z(a.D, a.qdeal.rows);
+  const bool on = z.sl < z.slices && w.first + z.r < w.m;
+  const int rr = min(w.first + z.r, w.m - 1), h = w.hk * a.group + rr % a.group;
+  const int64_t row = w.base + rr / a.group, at = a.at(row, h);
+  const float* const p = a.qpart + at * parts.most * 2 * a.D + z.c;
+  if (threadIdx.x < 128) bad[threadIdx.x] = false;
+  v4f d = z.sum(p, 2 * a.D, n, x, on);
   if constexpr (NS == 1) {
-    over = fabsf(over) < INFINITY ? over : 0.f;
-    if (lane == 0) a.delta[at] += over;
-    d[0] = fmaf(-over, p[0], d[0]);
-    d[1] = fmaf(-over, p[1], d[1]);
+    const v4f k = z.sum(p + a.D, 2 * a.D, n, x, on);
+    if (on && z.sl == 0) {
+      const float* const o =
+          a.qpart + a.qdeal.tiles.n * a.qdeal.Hk * a.group * parts.most * 2 * a.D + at * parts.most;
+      float over = 0.f;
+      for (int s = 0; s < n; ++s) over += o[s];
+      over = fabsf(over) < INFINITY ? over : 0.f;
+      if (z.c == 0) a.delta[at] += over;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) d[j] = fmaf(-over, k[j], d[j]);
+    }
   }
-  bool fine = fabsf(d[0]) < INFINITY && fabsf(d[1]) < INFINITY;
-  if constexpr (NS == 3) {
-    const float big = wave_max(fmaxf(fabsf(d[0]), fabsf(d[1])));
-    fine &= !(big > 0.f && big < 0x1p-95f);
+  __syncthreads();
+  if (on && z.sl == 0) {
+    store4<NS>(a.dq.p + row * a.dq.row + h * a.dq.head + z.c, d, a.scale);
+    const float l = a.lse[at];
+    // (a row without weights stays, one past LSE_MOST takes weights of its own)
+    if (l == l && (!(fabsf(l) <= LSE_MOST) || !fine4<NS>(d))) bad[z.r] = true;
   }
-  if (mk > 0 && !none && (far || __ballot(!fine))) {
-    dq_row<NS>(a, row, h, k0, mk);
-    return;
-  }
-  auto* const o = a.dq.p + row * a.dq.row + h * a.dq.head;
-  if (lane < a.D) o[lane] = Elem<NS>::put(d[0] * a.scale);
-  if (64 + lane < a.D) o[64 + lane] = Elem<NS>::put(d[1] * a.scale);
+  __syncthreads();
+  for (int i = threadIdx.x >> 6; i < min(z.rows, w.m - w.first); i += 4)
+    if (bad[i]) {
+      const int y = w.first + i;
+      dq_row<NS>(a, w.base + y / a.group, w.hk * a.group + y % a.group, w.other, w.mo);
+    }
 }
 
 // What a wave with 32 keys does with 32 queries of a tile: dV += P^T dO, dK += dS^T Q
@@ -506,26 +560,29 @@ __global__ void __launch_bounds__(64 * KW * QW, NS == 3 || DP > 64 ? 1 : 2)
   typedef KeyShape<NS, DP, KW, QW, U> X;
   typedef typename X::L L;
   typedef typename X::St St;
-  constexpr int KB = X::KB, TB = X::TB;
+  constexpr int TB = X::TB;
   constexpr bool EARLY = NS == 1 && DP == 64 && QW < 4;
   extern __shared__ char smem[];
   const int tid = threadIdx.x, lane = tid & 63, n32 = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), qw = QW == 1 ? 0 : wave / KW;
-  const int split = blockIdx.x % a.ks, hk = blockIdx.x / a.ks % a.Hk;
-  const Place sp = find_place(a.kr, a.batch, a.nk, blockIdx.x / a.ks / a.Hk, KB, 1);
-  if (sp.first >= sp.m) return;
-  int64_t q0;
-  int mq;
-  find_rows(a.qr, sp.sample, a.nq, q0, mq);
-  const int j = min(sp.first + (wave - qw * KW) * 32 + n32, sp.m - 1);  // the lane's key
-  const bool mine = sp.first + (wave - qw * KW) * 32 + n32 < sp.m;
   const float c2 = a.scale * LOG2E;
+  uint32_t qo[St::N], go[St::N];
+  St::places(qo, a.q.row, a.D, tid);
+  St::places(go, a.d_o.row, a.D, tid);
+  const typename L::Lane pl(lane);
+
+  const Work w = a.kdeal.find(blockIdx.x);
+  if (w.first >= w.m) return;
+  const int mq = w.mo, hk = w.hk;
+  const int64_t q0 = w.other;
+  const int j = min(w.first + (wave - qw * KW) * 32 + n32, w.m - 1);  // the lane's key
+  const bool mine = w.first + (wave - qw * KW) * 32 + n32 < w.m;
 
   Frag<NS> K[DP / 16], V[DP / 16];
 #pragma unroll
   for (int s = 0; s < DP / 16; ++s) {
-    K[s] = load_frag<NS>(a.k.p + (sp.base + j) * a.k.row + hk * a.k.head, s, a.D, lane);
-    V[s] = load_frag<NS>(a.v.p + (sp.base + j) * a.v.row + hk * a.v.head, s, a.D, lane);
+    K[s] = load_frag<NS>(a.k.p + (w.base + j) * a.k.row + hk * a.k.head, s, a.D, lane);
+    V[s] = load_frag<NS>(a.v.p + (w.base + j) * a.v.row + hk * a.v.head, s, a.D, lane);
   }
   v16f dK[DP / 32], dV[DP / 32];
 #pragma unroll
@@ -533,21 +590,17 @@ __global__ void __launch_bounds__(64 * KW * QW, NS == 3 || DP > 64 ? 1 : 2)
 
   // the block's tiles of queries, those of each head in turn
   const int per = (mq + TB - 1) / TB;
-  const int64_t nt = (int64_t)per * a.group, share = (nt + a.ks - 1) / a.ks;
-  const int64_t t0 = min(nt, split * share), t1 = min(nt, t0 + share);
+  const int64_t nt = (int64_t)per * a.group, share = (nt + w.parts - 1) / w.parts;
+  const int64_t t0 = min(nt, w.part * share), t1 = min(nt, t0 + share);
   St sq, sg;
   float lse2 = 0.f, delta = 0.f;
-  uint32_t qo[St::N], go[St::N];
-  St::places(qo, a.q.row, a.D, tid);
-  St::places(go, a.d_o.row, a.D, tid);
-  const typename L::Lane pl(lane);
   int h = per > 0 ? hk * a.group + (int)(t0 / per) : 0;  // of the next tile to fetch
   int i0 = per > 0 ? (int)(t0 % per) * TB : 0;
   auto fetch = [&]() {
     sq.load(a.q.p + q0 * a.q.row + h * a.q.head, a.q.row, qo, i0, mq - i0, a.D);
     sg.load(a.d_o.p + q0 * a.d_o.row + h * a.d_o.head, a.d_o.row, go, i0, mq - i0, a.D);
     if (tid < TB) {
-      const int64_t at = h * a.nq + q0 + min(i0 + tid, mq - 1);
+      const int64_t at = a.at(q0 + min(i0 + tid, mq - 1), h);
       lse2 = i0 + tid < mq ? a.lse2[at] : INFINITY;
       delta = i0 + tid < mq ? a.delta[at] : 0.f;
     }
@@ -609,9 +662,10 @@ __global__ void __launch_bounds__(64 * KW * QW, NS == 3 || DP > 64 ? 1 : 2)
         }
     }
   }
-  if (a.ks > 1) {
+  if (w.parts > 1) {
     if (mine) {
-      float* const o = a.kout(hk * a.nk + sp.base + j, split);
+      float* const o =
+          a.kpart + ((hk * a.kdeal.tiles.n + w.base + j) * a.kdeal.parts.most + w.part) * 2 * a.D;
 #pragma unroll
       for (int d = 0; d < DP / 32; ++d) {
         store_cols<3>(o, dK[d], 1.f, d, a.D, lane);
@@ -625,8 +679,8 @@ __global__ void __launch_bounds__(64 * KW * QW, NS == 3 || DP > 64 ? 1 : 2)
   for (int d = 0; d < DP / 32; ++d) fine &= finite16(dK[d]) && finite16(dV[d]);
   if constexpr (NS == 3) fine &= !tiny(dK, 1.f) && !tiny(dV, 1.f);
   if (mine) {
-    auto* const dk = a.dk.p + (sp.base + j) * a.dk.row + hk * a.dk.head;
-    auto* const dv = a.dv.p + (sp.base + j) * a.dv.row + hk * a.dv.head;
+    auto* const dk = a.dk.p + (w.base + j) * a.dk.row + hk * a.dk.head;
+    auto* const dv = a.dv.p + (w.base + j) * a.dv.row + hk * a.dv.head;
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d) {
       store_cols<NS>(dk, dK[d], a.scale, d, a.D, lane);
@@ -635,141 +689,136 @@ __global__ void __launch_bounds__(64 * KW * QW, NS == 3 || DP > 64 ? 1 : 2)
   }
   const uint64_t bad = __ballot(mine && !fine);
   uint32_t rows = (uint32_t)bad | (uint32_t)(bad >> 32);
-  const int64_t w0 = sp.base + sp.first + wave * 32;
+  const int64_t w0 = w.base + w.first + wave * 32;
   for (; rows; rows &= rows - 1) dkv_row<NS>(a, w0 + __builtin_ctz(rows), hk, q0, mq);
 }
 
-// The parts of a key's dk and dv, a wave a row and head, channels along the lanes, in order
+// The parts of the keys' dk and dv: `kdeal.rows` keys a block
 template <int NS>
-__global__ void __launch_bounds__(256) cross_dkv_join_kernel(CrossBwdArgs<NS> a) {
-  const int lane = threadIdx.x & 63;
-  const int64_t at = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (at >= a.nk * a.Hk) return;
-  const int hk = (int)(at / a.nk);
-  const int64_t row = at - hk * a.nk;
-  int sample;
-  if (!find_row(a.kr, a.batch, a.nk, (int)row, sample)) return;
-  // lane's elements of dK and dV side by side, 2 D <= 256 of them
-  float v[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int s0 = 0; s0 < a.ks; s0 += 4) {
-    float x[4][4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float* const o = a.kout(at, min(s0 + j, a.ks - 1));
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const int e = 64 * c + lane;
-        x[j][c] = s0 + j < a.ks && e < 2 * a.D ? o[e] : 0.f;
-      }
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int c = 0; c < 4; ++c) v[c] += x[j][c];
+__global__ void __launch_bounds__(256) cross_dkv_join_kernel(CrossBwdArgs<NS> a, Parts parts) {
+  __shared__ v4f x[256];
+  __shared__ bool bad[128];
+  const Work w = a.kdeal.find(blockIdx.x);
+  const int n = parts.of(w.mo * (int64_t)a.group);
+  if (w.first >= w.m || n == 1) return;
+  const Slices z(2 * a.D, a.kdeal.rows);
+  const bool on = z.sl < z.slices && w.first + z.r < w.m;
+  const int64_t row = w.base + min(w.first + z.r, w.m - 1);
+  const float* const p =
+      a.kpart + (w.hk * a.kdeal.tiles.n + row) * parts.most * 2 * a.D + z.c;
+  if (threadIdx.x < 128) bad[threadIdx.x] = false;
+  const v4f d = z.sum(p, 2 * a.D, n, x, on);
+  __syncthreads();
+  if (on && z.sl == 0) {
+    if (z.c < a.D)
+      store4<NS>(a.dk.p + row * a.dk.row + w.hk * a.dk.head + z.c, d, a.scale);
+    else
+      store4<NS>(a.dv.p + row * a.dv.row + w.hk * a.dv.head + z.c - a.D, d, 1.f);
+    if (!fine4<NS>(d)) bad[z.r] = true;
   }
-  bool fine = true;
-  float bigk = 0.f, bigv = 0.f;
-#pragma unroll
-  for (int c = 0; c < 4; ++c) {
-    fine &= fabsf(v[c]) < INFINITY;
-    if (64 * c + lane < a.D) bigk = fmaxf(bigk, fabsf(v[c]));
-    else bigv = fmaxf(bigv, fabsf(v[c]));
-  }
-  if constexpr (NS == 3) {
-    bigk = wave_max(bigk);
-    bigv = wave_max(bigv);
-    fine &= !(bigk > 0.f && bigk < 0x1p-95f) && !(bigv > 0.f && bigv < 0x1p-95f);
-  }
-  if (__ballot(!fine)) {
-    int64_t q0;
-    int mq;
-    find_rows(a.qr, sample, a.nq, q0, mq);
-    dkv_row<NS>(a, row, hk, q0, mq);
-    return;
-  }
-  auto* const dk = a.dk.p + row * a.dk.row + hk * a.dk.head;
-  auto* const dv = a.dv.p + row * a.dv.row + hk * a.dv.head;
-#pragma unroll
-  for (int c = 0; c < 4; ++c) {
-    const int e = 64 * c + lane;
-    if (e < a.D) dk[e] = Elem<NS>::put(v[c] * a.scale);
-    else if (e < 2 * a.D) dv[e - a.D] = Elem<NS>::put(v[c]);
-  }
+  __syncthreads();
+  for (int i = threadIdx.x >> 6; i < min(z.rows, w.m - w.first); i += 4)
+    if (bad[i]) dkv_row<NS>(a, w.base + w.first + i, w.hk, w.other, w.mo);
 }
 
+#ifndef WANT
+#define WANT 1024
+#endif
+#ifndef LEAST
+#define LEAST 512
+#endif
+#ifndef REPEAT_BLOCKS
+#define REPEAT_BLOCKS 768
+#endif
 // Shapes and parts of both passes, by rules on sizes alone (cross_fwd.hip)
 struct CrossBwdPlan {
-  int qw, qkw, qs;  // queries' pass: waves of queries, groups of keys, parts of the keys
-  int kw, kqw, ks;  // keys' pass: waves of keys, groups of queries, parts of the queries
+  int qw, qkw, repeat;  // queries' pass: waves of queries, groups of keys, tiles of a work
+  int kw, kqw;          // keys' pass: waves of keys, groups of queries
+  Parts qparts, kparts;
 };
 CrossBwdPlan plan(int type, int64_t nq, int64_t nk, int batch, int D, int Hk, int group) {
   CrossBwdPlan p;
-  const int64_t usedq = std::max<int64_t>(1, std::min<int64_t>(batch, nq));
-  const int64_t usedk = std::max<int64_t>(1, std::min<int64_t>(batch, nk));
+  const int usedq = (int)std::max<int64_t>(1, std::min<int64_t>(batch, nq));
+  const int usedk = (int)std::max<int64_t>(1, std::min<int64_t>(batch, nk));
   const int64_t rows = ceil_div(nq * group, usedq), keys = ceil_div(nk, usedk);
   auto qblocks = [&](int b) { return usedq * ceil_div(rows, b) * Hk; };
   auto kblocks = [&](int b) { return usedk * ceil_div(keys, b) * Hk; };
-  if (rows <= 32 && (type == SCN_BF16 || D <= 96)) {
+  const bool bf16 = type == SCN_BF16;
+  if (rows <= 32 && bf16) {
     p.qw = 1;
-    p.qkw = type == SCN_BF16 || D <= 32 ? 4 : 2;
-  } else if (type == SCN_F32) {
-    p.qw = D > 32 ? 4 : 2;
-    p.qkw = D > 64 ? 1 : 2;
+    p.qkw = 4;
+  } else if (!bf16) {
+    p.qw = D > 32 || keys <= 64 ? 4 : 2;
+    p.qkw = D > 64 || keys <= 64 ? 1 : 2;
   } else {
-    p.qw = D > 64 && qblocks(128) >= 512 ? 4 : 2;
+    p.qw = keys <= 64 || (D > 64 && qblocks(128) >= 512) ? 4 : 2;
     p.qkw = p.qw == 4 ? 1 : 2;
   }
-  p.qs = parts(qblocks(32 * p.qw), 512, nk / usedq, 256);
-  if (type == SCN_F32) {
+  p.qparts = cut(qblocks(32 * p.qw), WANT, nk / usedq, LEAST, usedq);
+  p.repeat = 1;
+  if (p.qkw == 1 && keys <= 64)
+    p.repeat = (int)std::max<int64_t>(1, std::min<int64_t>(8, qblocks(32 * p.qw) / REPEAT_BLOCKS));
+  if (!bf16) {
     p.kw = keys <= 32 && D <= 32 ? 1 : D <= 64 ? 2 : 4;
-    p.kqw = p.kw == 1 ? 4 : p.kw == 2 ? 2 : 1;
   } else {
     p.kw = D <= 64 && (keys <= 32 || kblocks(128) < 128) ? 1
            : kblocks(128) < (D <= 64 ? 1024 : 384)       ? 2
                                                          : 4;
-    p.kqw = 4 / p.kw;
   }
-  p.ks = parts(kblocks(32 * p.kw), 512, nq * group / usedk, 256);
+  p.kqw = 4 / p.kw;
+  p.kparts = cut(kblocks(32 * p.kw), WANT, nq * group / usedk, LEAST, usedk);
   return p;
 }
 
-template <int NS, int DP, int QW, int KW>
-scn_status launch_dq(const CrossBwdArgs<NS>& a, hipStream_t st) {
+scn_status too_many() {
+  set_error("scn_cross_attn_bwd: more than 2^31 blocks of rows and heads");
+  return SCN_ERR_OVERFLOW;
+}
+// Tile rows of a join's block: as many as leave the card some thousand blocks, of at most 256
+// threads
+Deal join_deal(Deal d, int wide) {
+  d.parts = Parts{1, INT32_MAX};
+  d.rows = 1;
+  while (d.rows * 2 * (wide / 4) <= 256 && d.tiles.n * d.tiles.many * d.Hk / (d.rows * 2) >= 1024)
+    d.rows *= 2;
+  return d;
+}
+
+template <int NS, int DP, int QW, int KW, bool FEW = false>
+scn_status launch_dq(CrossBwdArgs<NS> a, const CrossBwdPlan& p, hipStream_t st) {
   typedef QueryShape<NS, DP, QW, KW> X;
   static LdsLimit limit;
-  auto fn = cross_dq_kernel<NS, DP, QW, KW>;
+  auto fn = cross_dq_kernel<NS, DP, QW, KW, FEW>;
   if (scn_status rc = allow_lds(reinterpret_cast<const void*>(fn), limit, X::SMEM)) return rc;
-  const int64_t blocks = (a.nq * a.group / X::QB + a.batch) * a.Hk * a.qs;
-  const int64_t joins = ceil_div(a.nq * a.Hk * a.group, 4);
-  if (std::max(blocks, joins) > INT32_MAX) {
-    set_error("scn_cross_attn_bwd: more than 2^31 blocks of rows, heads and parts");
-    return SCN_ERR_OVERFLOW;
-  }
+  a.qdeal.rows = X::QB * a.repeat;
+  const int64_t blocks = a.qdeal.blocks();
+  if (blocks > INT32_MAX) return too_many();
   hipLaunchKernelGGL(fn, dim3((unsigned)blocks), dim3(X::NT), X::SMEM, st, a);
   SCN_LAUNCH_CHECK();
-  if (a.qs > 1) {
-    hipLaunchKernelGGL(cross_dq_join_kernel<NS>, dim3((unsigned)joins), dim3(256), 0, st, a);
+  if (p.qparts.most > 1) {
+    a.qdeal = join_deal(a.qdeal, a.D);
+    hipLaunchKernelGGL(cross_dq_join_kernel<NS>, dim3((unsigned)a.qdeal.blocks()),
+                       dim3(256), 0, st, a, p.qparts);
     SCN_LAUNCH_CHECK();
   }
   return SCN_OK;
 }
 
 template <int NS, int DP, int KW, int QW, int U>
-scn_status launch_dkv(const CrossBwdArgs<NS>& a, hipStream_t st) {
+scn_status launch_dkv(CrossBwdArgs<NS> a, const CrossBwdPlan& p, hipStream_t st) {
   typedef KeyShape<NS, DP, KW, QW, U> X;
   static LdsLimit limit;
   auto fn = cross_dkv_kernel<NS, DP, KW, QW, U>;
   if (scn_status rc = allow_lds(reinterpret_cast<const void*>(fn), limit, X::SMEM)) return rc;
-  const int64_t blocks = (a.nk / X::KB + a.batch) * a.Hk * a.ks;
-  const int64_t joins = ceil_div(a.nk * a.Hk, 4);
-  if (std::max(blocks, joins) > INT32_MAX) {
-    set_error("scn_cross_attn_bwd: more than 2^31 blocks of keys, heads and parts");
-    return SCN_ERR_OVERFLOW;
-  }
+  a.kdeal.rows = X::KB;
+  const int64_t blocks = a.kdeal.blocks();
+  if (blocks > INT32_MAX) return too_many();
   hipLaunchKernelGGL(fn, dim3((unsigned)blocks), dim3(X::NT), X::SMEM, st, a);
   SCN_LAUNCH_CHECK();
-  if (a.ks > 1) {
-    hipLaunchKernelGGL(cross_dkv_join_kernel<NS>, dim3((unsigned)joins), dim3(256), 0, st, a);
+  if (p.kparts.most > 1) {
+    a.kdeal = join_deal(a.kdeal, 2 * a.D);
+    hipLaunchKernelGGL(cross_dkv_join_kernel<NS>, dim3((unsigned)a.kdeal.blocks()),
+                       dim3(256), 0, st, a, p.kparts);
     SCN_LAUNCH_CHECK();
   }
   return SCN_OK;
@@ -778,32 +827,29 @@ scn_status launch_dkv(const CrossBwdArgs<NS>& a, hipStream_t st) {
 template <int NS, int DP>
 scn_status launch(const CrossBwdArgs<NS>& a, const CrossBwdPlan& p, hipStream_t st) {
   scn_status rc = SCN_OK;
-  if (a.nq > 0) {
-    if constexpr (NS == 3) {
-      if constexpr (DP <= 96)
-        if (p.qw == 1) rc = launch_dq<NS, DP, 1, (DP == 32 ? 4 : 2)>(a, st);
-      if (p.qw > 1) rc = launch_dq<NS, DP, (DP > 32 ? 4 : 2), (DP > 64 ? 1 : 2)>(a, st);
-    } else if (p.qw == 1) {
-      rc = launch_dq<NS, DP, 1, 4>(a, st);
-    } else {
-      constexpr int QW = DP > 64 ? 4 : 2, KW = DP > 64 ? 1 : 2;
-      rc = p.qw == 2 ? launch_dq<NS, DP, 2, 2>(a, st) : launch_dq<NS, DP, QW, KW>(a, st);
-    }
+  if (a.qdeal.tiles.n > 0) {
+    if (p.repeat > 1)
+      rc = launch_dq<NS, DP, 4, 1, true>(a, p, st);
+    else if (p.qkw == 1)
+      rc = launch_dq<NS, DP, 4, 1>(a, p, st);
+    else if constexpr (NS == 1)
+      rc = p.qw == 1 ? launch_dq<NS, DP, 1, 4>(a, p, st) : launch_dq<NS, DP, 2, 2>(a, p, st);
+    else if constexpr (DP <= 64)
+      rc = launch_dq<NS, DP, (DP > 32 ? 4 : 2), 2>(a, p, st);
   }
-  if (rc || a.nk == 0) return rc;
+  if (rc || a.kdeal.tiles.n == 0) return rc;
   if constexpr (NS == 3) {
     if constexpr (DP <= 32)
-      if (p.kw == 1) return launch_dkv<NS, DP, 1, 4, 1>(a, st);
-    if constexpr (DP <= 64) {
-      return launch_dkv<NS, DP, 2, 2, 1>(a, st);
-    } else {
-      return launch_dkv<NS, DP, 4, 1, 1>(a, st);
-    }
+      if (p.kw == 1) return launch_dkv<NS, DP, 1, 4, 1>(a, p, st);
+    if constexpr (DP <= 64)
+      return launch_dkv<NS, DP, 2, 2, 1>(a, p, st);
+    else
+      return launch_dkv<NS, DP, 4, 1, 1>(a, p, st);
   } else {
     if constexpr (DP <= 64)
-      if (p.kw == 1) return launch_dkv<NS, DP, 1, 4, 1>(a, st);
-    if (p.kw == 2) return launch_dkv<NS, DP, 2, 2, 1>(a, st);
-    return launch_dkv<NS, DP, 4, 1, 2>(a, st);
+      if (p.kw == 1) return launch_dkv<NS, DP, 1, 4, 1>(a, p, st);
+    if (p.kw == 2) return launch_dkv<NS, DP, 2, 2, 1>(a, p, st);
+    return launch_dkv<NS, DP, 4, 1, 2>(a, p, st);
   }
 }
 
@@ -815,12 +861,12 @@ scn_status run(const CrossBwdArgs<NS>& a, const CrossBwdPlan& p, hipStream_t st)
   return launch<NS, 128>(a, p, st);
 }
 
-// floats of the workspace: three rows' statistics, then the parts of dq, then those of dk and dv
-// (each needed by one pass and its join alone, so they lie in the same place)
+// floats of the workspace: the rows' statistics, then the parts of dq, or those of dk and dv
+// (each of use to one pass and its join alone, so they lie in the same place)
 int64_t stat_floats(int64_t nq, int Hq) { return (nq * Hq + 63) & ~int64_t(63); }
 int64_t part_floats(const CrossBwdPlan& p, int64_t nq, int64_t nk, int Hq, int Hk, int D) {
-  const int64_t q = p.qs > 1 ? nq * Hq * p.qs * (2 * D + 1) : 0;
-  const int64_t k = p.ks > 1 ? nk * Hk * p.ks * 2 * D : 0;
+  const int64_t q = p.qparts.most > 1 ? nq * Hq * p.qparts.most * (2 * D + 1) : 0;
+  const int64_t k = p.kparts.most > 1 ? nk * Hk * p.kparts.most * 2 * D : 0;
   return std::max(q, k);
 }
 
@@ -833,14 +879,14 @@ CrossBwdArgs<NS> make(int64_t nq, int64_t nk, int batch, const int32_t* qr, cons
   typedef typename Elem<NS>::T T;
   float* const f = static_cast<float*>(ws);
   const int64_t n = stat_floats(nq, Hq);
-  return CrossBwdArgs<NS>{nq, nk, batch, D, Hk, Hq / Hk, qr, kr, view<const T>(q), view<const T>(k),
-                          view<const T>(v), view<const T>(o), view<const T>(d_o), view<T>(dq),
-                          view<T>(dk), view<T>(dv), lse, f, f + n, f + 2 * n, scale, p.qs, p.ks,
-                          f + 3 * n, f + 3 * n};
+  const Side qs{qr, nq, Hq / Hk}, ks{kr, nk, 1};
+  return CrossBwdArgs<NS>{Deal{qs, ks, batch, 0, Hk, p.qparts}, Deal{ks, qs, batch, 0, Hk, p.kparts},
+                          D, Hq / Hk, p.repeat, view<const T>(q), view<const T>(k), view<const T>(v),
+                          view<const T>(o), view<const T>(d_o), view<T>(dq), view<T>(dk),
+                          view<T>(dv), lse, f, f + n, f + 2 * n, scale, f + 3 * n, f + 3 * n};
 }
 
 }  // namespace
-
 }  // namespace scn
 
 using namespace scn;

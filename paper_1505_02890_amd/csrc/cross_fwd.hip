@@ -9,23 +9,36 @@
 
 #include "cross.h"
 
+#ifndef REPEAT_BLOCKS
+#define REPEAT_BLOCKS 768
+#endif
+#ifndef WANT
+#define WANT 1024
+#endif
+#ifndef LEAST
+#define LEAST 512
+#endif
 namespace scn {
 namespace {
 
 template <int NS>
 struct CrossArgs {
   typedef typename Elem<NS>::T T;
-  int64_t nq, nk;
-  int batch, D, Hk, group, splits;
-  const int32_t *qr, *kr;
+  Deal deal;  // tiles of queries, parts of their keys
+  int D, group;
+  int repeat;  // tiles of queries that a work is, where the keys are few
   Heads<const T> q, k, v;
   Heads<T> o;
   float* lse;   // [Hq][nq] or null
   float scale;  // positive
-  float* part;  // [Hq][nq][splits][D], then [Hq][nq][splits][2]: maximum, sum
-  __device__ inline float* out(int64_t at, int s) const { return part + (at * splits + s) * D; }
+  float* part;  // [Hq][nq][parts][D], then [Hq][nq][parts][2]: maximum, sum
+  __device__ inline int64_t at(int64_t row, int h) const { return h * deal.tiles.n + row; }
+  __device__ inline float* out(int64_t at, int s) const {
+    return part + (at * deal.parts.most + s) * D;
+  }
   __device__ inline float* sums(int64_t at, int s) const {
-    return part + nq * Hk * group * splits * D + (at * splits + s) * 2;
+    return part + deal.tiles.n * deal.Hk * group * deal.parts.most * D +
+           (at * deal.parts.most + s) * 2;
   }
 };
 
@@ -55,7 +68,7 @@ __device__ inline void cross_row(const CrossArgs<NS>& a, int64_t row, int h, int
   auto* const o = a.o.p + row * a.o.row + h * a.o.head;
   if (lane < a.D) o[lane] = E::put(o0);
   if (64 + lane < a.D) o[64 + lane] = E::put(o1);
-  if (a.lse && lane == 0) a.lse[h * a.nq + row] = r.top + logf(r.sum);
+  if (a.lse && lane == 0) a.lse[a.at(row, h)] = r.top + logf(r.sum);
 }
 
 // QW waves of 32 tile rows by KW groups that share out the keys of a tile, 32 NB each
@@ -70,8 +83,9 @@ struct Shape {
   static_assert(SMEM <= 160 * 1024, "LDS of a compute unit");
 };
 
-template <int NS, int DP, int QW, int KW, int NB>
-__global__ void __launch_bounds__(64 * QW * KW, NS == 3 && DP > 96 ? 1 : 2)
+// FEW: a work is several tiles of queries in turn
+template <int NS, int DP, int QW, int KW, int NB, bool FEW>
+__global__ void __launch_bounds__(64 * QW * KW, DP > 96 && (NS == 3 || QW == 1) ? 1 : 2)
     cross_fwd_kernel(CrossArgs<NS> a) {
   typedef Shape<NS, DP, QW, KW, NB> X;
   typedef typename X::L L;
@@ -81,42 +95,28 @@ __global__ void __launch_bounds__(64 * QW * KW, NS == 3 && DP > 96 ? 1 : 2)
   extern __shared__ char smem[];
   const int tid = threadIdx.x, lane = tid & 63, n32 = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), kw = KW == 1 ? 0 : wave / QW;
-  const int split = blockIdx.x % a.splits, hk = blockIdx.x / a.splits % a.Hk;
-  const Place sp = find_place(a.qr, a.batch, a.nq, blockIdx.x / a.splits / a.Hk, QB, a.group);
-  if (sp.first >= sp.m) return;
-  int64_t k0;
-  int mk;
-  find_rows(a.kr, sp.sample, a.nk, k0, mk);
-  const int r = sp.first + (wave - kw * QW) * 32 + n32;  // the lane's tile row
-  const bool mine = r < sp.m;
-  const int rr = min(r, sp.m - 1);
-  const int64_t row = sp.base + rr / a.group;
-  const int h = hk * a.group + rr % a.group;
   const float c2 = a.scale * LOG2E;
-
-  Frag<NS> Q[DP / 16];
-  {
-    const auto* const q = a.q.p + row * a.q.row + h * a.q.head;
-#pragma unroll
-    for (int s = 0; s < DP / 16; ++s) Q[s] = load_frag<NS>(q, s, a.D, lane);
-  }
-  v16f O[DP / 32];
-#pragma unroll
-  for (int d = 0; d < DP / 32; ++d) O[d] = zero16();
-  // the running maximum (log 2) and sum of this half's keys, as in attn_fwd.hip
-  float top = -INFINITY, base = 0.f, limit = -INFINITY, sum = 0.f;
-
-  // the block's tiles of the sample's keys
-  const int nt = (mk + KT - 1) / KT, per = (nt + a.splits - 1) / a.splits;
-  const int t0 = min(nt, split * per), t1 = min(nt, t0 + per);
-  const auto* const kp = a.k.p + k0 * a.k.row + hk * a.k.head;
-  const auto* const vp = a.v.p + k0 * a.v.row + hk * a.v.head;
   typedef Stage<NS, DP, KT, NT> St;
-  St sk, sv;
   uint32_t ko[St::N], vo[St::N];
   St::places(ko, a.k.row, a.D, tid);
   St::places(vo, a.v.row, a.D, tid);
   const typename L::Lane at(lane);
+
+  const Work w = a.deal.find(blockIdx.x);
+  if (w.first >= w.m) return;
+  const int mk = w.mo, hk = w.hk;
+  const int64_t k0 = w.other;
+  Frag<NS> Q[DP / 16];
+  v16f O[DP / 32];
+  // the running maximum (log 2) and sum of this half's keys, as in attn_fwd.hip
+  float top, base, limit, sum;
+
+  // the block's tiles of the sample's keys
+  const int nt = (mk + KT - 1) / KT, per = (nt + w.parts - 1) / w.parts;
+  const int t0 = min(nt, w.part * per), t1 = min(nt, t0 + per);
+  const auto* const kp = a.k.p + k0 * a.k.row + hk * a.k.head;
+  const auto* const vp = a.v.p + k0 * a.v.row + hk * a.v.head;
+  St sk, sv;
   auto fetch = [&](int t) {
     sk.load(kp, a.k.row, ko, t * KT, mk - t * KT, a.D);
     sv.load(vp, a.v.row, vo, t * KT, mk - t * KT, a.D);
@@ -217,19 +217,36 @@ __global__ void __launch_bounds__(64 * QW * KW, NS == 3 && DP > 96 ? 1 : 2)
       }
     }
   };
+  auto sweep = [&](int first, bool stage) {
+  const int r = first + (wave - kw * QW) * 32 + n32;  // the lane's tile row
+  const bool mine = r < w.m;
+  const int rr = min(r, w.m - 1);
+  const int64_t row = w.base + rr / a.group;
+  const int h = hk * a.group + rr % a.group;
+  {
+    const auto* const q = a.q.p + row * a.q.row + h * a.q.head;
+#pragma unroll
+    for (int s = 0; s < DP / 16; ++s) Q[s] = load_frag<NS>(q, s, a.D, lane);
+  }
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d) O[d] = zero16();
+  top = limit = -INFINITY;
+  base = sum = 0.f;
   // While a tile is taken, the next one goes from registers to the other buffer and the
-  // one after that is loaded.
-  if (t0 < t1) {
+  // one after that is loaded.  Two tiles or fewer stay for the block's next queries.
+  if (stage && t0 < t1) {
     fetch(t0);
     put(t0);
     if (t0 + 1 < t1) fetch(t0 + 1);
     __syncthreads();
-    for (int t = t0; t < t1; ++t) {
+  }
+  for (int t = t0; t < t1; ++t) {
+    if (stage) {
       if (t + 1 < t1) put(t + 1);
       if (t + 2 < t1) fetch(t + 2);
-      take(t);
-      __syncthreads();
     }
+    take(t);
+    if (stage) __syncthreads();
   }
   sum = both_sum(sum);
   if constexpr (KW > 1) {
@@ -259,14 +276,14 @@ __global__ void __launch_bounds__(64 * QW * KW, NS == 3 && DP > 96 ? 1 : 2)
         for (int e = 0; e < 16; ++e) O[d][e] = O[d][e] * f + o[(d * 16 + e) * 64] * f2;
     }
   }
-  if (a.splits > 1) {
+  if (w.parts > 1) {
     if (mine) {
-      const int64_t to = h * a.nq + row;
-      float* const o = a.out(to, split);
+      const int64_t to = a.at(row, h);
+      float* const o = a.out(to, w.part);
 #pragma unroll
       for (int d = 0; d < DP / 32; ++d) store_cols<3>(o, O[d], 1.f, d, a.D, lane);
       if (half == 0) {
-        float* const s = a.sums(to, split);
+        float* const s = a.sums(to, w.part);
         s[0] = top;
         s[1] = sum;
       }
@@ -284,123 +301,156 @@ __global__ void __launch_bounds__(64 * QW * KW, NS == 3 && DP > 96 ? 1 : 2)
     auto* const o = a.o.p + row * a.o.row + h * a.o.head;
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d) store_cols<NS>(o, O[d], inv, d, a.D, lane);
-    if (a.lse && half == 0) a.lse[h * a.nq + row] = (top + log2f(sum)) * LN2;
+    if (a.lse && half == 0) a.lse[a.at(row, h)] = (top + log2f(sum)) * LN2;
   }
   // rows that attn.h's bounds do not serve (SUM_LEAST, tiny)
   const uint64_t bad = __ballot(mine && !fine && mk > 0);
   uint32_t rows = (uint32_t)bad | (uint32_t)(bad >> 32);
-  const int w0 = sp.first + wave * 32;
+  const int w0 = first + wave * 32;
   for (; rows; rows &= rows - 1) {
     const int x = w0 + __builtin_ctz(rows);
-    cross_row<NS>(a, sp.base + x / a.group, hk * a.group + x % a.group, k0, mk);
+    cross_row<NS>(a, w.base + x / a.group, hk * a.group + x % a.group, k0, mk);
+  }
+  };
+  if constexpr (!FEW) {
+    sweep(w.first, true);
+  } else {
+    const int end = min(w.m, w.first + QB * a.repeat);
+    for (int first = w.first; first < end; first += QB)
+      sweep(first, first == w.first || t1 - t0 > 2);
   }
 }
 
-// The splits of a row's head, a wave each: their weights first, a split a lane, then the
-// outputs in order, channels along the lanes.
+// The parts of the rows' outputs, joined in order: `deal.rows` tile rows a block, four channels
+// a thread, and what threads are left share out the parts.
 template <int NS>
-__global__ void __launch_bounds__(256) cross_join_kernel(CrossArgs<NS> a) {
-  const int lane = threadIdx.x & 63;
-  const int64_t at = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (at >= a.nq * a.Hk * a.group) return;
-  const int h = (int)(at / a.nq);
-  const int64_t row = at - h * a.nq;
-  int sample;
-  if (!find_row(a.qr, a.batch, a.nq, (int)row, sample)) return;
-  int64_t k0;
-  int mk;
-  find_rows(a.kr, sample, a.nk, k0, mk);
-  constexpr int N = MAX_PARTS / 64;
-  float w[N], m = -INFINITY, l = 0.f;
+__global__ void __launch_bounds__(256) cross_join_kernel(CrossArgs<NS> a, Parts parts) {
+  __shared__ float x[256][6];
+  __shared__ bool bad[128];
+  // (the works of unsplit tiles, and the parts beside them)
+  const Work w = a.deal.find(blockIdx.x);
+  const int n = parts.of(w.mo);
+  if (w.first >= w.m || n == 1) return;
+  const int lanes = a.D >> 2, tid = threadIdx.x;
+  const int rows = a.deal.rows, slices = 256 / (lanes * rows);
+  const int c = tid % lanes * 4, r = tid / lanes % rows, sl = tid / (lanes * rows);
+  const bool on = sl < slices && w.first + r < w.m;
+  const int rr = min(w.first + r, w.m - 1), h = w.hk * a.group + rr % a.group;
+  const int64_t row = w.base + rr / a.group, at = h * a.deal.tiles.n + row;
+  const float* const out = a.part + at * parts.most * a.D + c;
+  const float* const sums =
+      a.part + a.deal.tiles.n * a.deal.Hk * a.group * parts.most * a.D + at * parts.most * 2;
+  float top = -INFINITY, sum = 0.f;
+  v4f v = {0.f, 0.f, 0.f, 0.f};
+  auto add = [&](float t, float s, v4f o) {
+    const float now = fmaxf(top, t), base = now == -INFINITY ? 0.f : now;
+    const float f = __builtin_amdgcn_exp2f(top - base), g = __builtin_amdgcn_exp2f(t - base);
+    top = now;
+    sum = sum * f + s * g;
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const int s = i * 64 + lane;
-    w[i] = s < a.splits ? a.sums(at, s)[0] : -INFINITY;
-    m = fmaxf(m, w[i]);  // (a split whose scores are NaN has a sum that is)
-  }
-  m = wave_max(m);
-  const float b = m == -INFINITY ? 0.f : m;
-  // splits without keys hold nothing
+    for (int j = 0; j < 4; ++j) v[j] = v[j] * f + o[j] * g;
+  };
+  if (on) {
+    const int per = (n + slices - 1) / slices, s1 = min(n, (sl + 1) * per);
+    for (int s0 = sl * per; s0 < s1; s0 += 4) {
+      float t[4], u[4];
+      v4f o[4];
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const int s = i * 64 + lane;
-    w[i] = __builtin_amdgcn_exp2f(w[i] - b);
-    if (s < a.splits) l = fmaf(w[i], a.sums(at, s)[1], l);
-  }
-  l = wave_sum(l);
-  float v0 = 0.f, v1 = 0.f;
-  const bool wide = a.D > 64;
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const int n = min(64, a.splits - i * 64);
-    for (int s0 = 0; s0 < n; s0 += 8) {
-      float x[8], y[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float* const o = a.out(at, i * 64 + min(s0 + j, n - 1));
-        x[j] = lane < a.D ? o[lane] : 0.f;
-        y[j] = wide && 64 + lane < a.D ? o[64 + lane] : 0.f;
+      for (int j = 0; j < 4; ++j) {
+        const int s = min(s0 + j, s1 - 1);
+        t[j] = sums[2 * s];
+        u[j] = sums[2 * s + 1];
+        o[j] = *reinterpret_cast<const v4f*>(out + (int64_t)s * a.D);
       }
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float f = s0 + j < n ? __shfl(w[i], s0 + j) : 0.f;
-        v0 = s0 + j < n ? fmaf(f, x[j], v0) : v0;
-        v1 = s0 + j < n ? fmaf(f, y[j], v1) : v1;
-      }
+      for (int j = 0; j < 4; ++j)
+        if (s0 + j < s1) add(t[j], u[j], o[j]);
     }
   }
-  const float inv = mk > 0 ? 1.f / l : 0.f;
-  v0 *= inv;
-  v1 *= inv;
-  bool fine = fabsf(m) < INFINITY && l > SUM_LEAST && l < SUM_MOST && fabsf(v0) < INFINITY &&
-              fabsf(v1) < INFINITY;
-  if constexpr (NS == 3) {
-    const float big = wave_max(fmaxf(fabsf(v0), fabsf(v1)));
-    fine &= !(big > 0.f && big < 0x1p-95f);
+  if (tid < 128) bad[tid] = false;
+  if (slices > 1) {
+    if (on && sl > 0) {
+      x[tid][0] = top;
+      x[tid][1] = sum;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[tid][2 + j] = v[j];
+    }
+    __syncthreads();
+    if (on && sl == 0)
+      for (int s = 1; s < slices; ++s) {
+        const float* const y = x[s * lanes * rows + tid];
+        add(y[0], y[1], v4f{y[2], y[3], y[4], y[5]});
+      }
+  } else {
+    __syncthreads();
   }
-  if constexpr (NS == 1) fine |= a.D % 32 == 0 && nan_score(m, l);
-  if (mk > 0 && __ballot(!fine)) {
-    cross_row<NS>(a, row, h, k0, mk);
-    return;
+  if (on && sl == 0) {
+    const float inv = 1.f / sum;
+    bool fine = fabsf(top) < INFINITY && sum > SUM_LEAST && sum < SUM_MOST;
+    bool large = false, any = false;  // (fp32: attn.h's tiny, of these channels)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      v[j] *= inv;
+      fine &= fabsf(v[j]) < INFINITY;
+      large |= fabsf(v[j]) >= 0x1p-95f;
+      any |= v[j] != 0.f;
+    }
+    if constexpr (NS == 3) fine &= large || !any;
+    if constexpr (NS == 1) fine |= a.D % 32 == 0 && nan_score(top, sum);
+    auto* const o = a.o.p + row * a.o.row + h * a.o.head + c;
+    if constexpr (NS == 1)
+      *reinterpret_cast<v2u*>(o) = v2u{cvt2_bf16(v[0], v[1]), cvt2_bf16(v[2], v[3])};
+    else
+      *reinterpret_cast<v4f*>(o) = v;
+    if (a.lse && c == 0) a.lse[at] = (top + log2f(sum)) * LN2;
+    if (!fine) bad[r] = true;
   }
-  auto* const o = a.o.p + row * a.o.row + h * a.o.head;
-  if (lane < a.D) o[lane] = Elem<NS>::put(v0);
-  if (64 + lane < a.D) o[64 + lane] = Elem<NS>::put(v1);
-  if (a.lse && lane == 0) a.lse[at] = (m + log2f(l)) * LN2;
+  __syncthreads();
+  for (int i = tid >> 6; i < min(rows, w.m - w.first); i += 4)
+    if (bad[i]) {
+      const int y = w.first + i;
+      cross_row<NS>(a, w.base + y / a.group, w.hk * a.group + y % a.group, w.other, w.mo);
+    }
 }
 
-// The kernel's shape and the parts of the keys, by rules on sizes alone (the lengths lie on
-// the device): tile rows of a mean sample, blocks, keys of a mean sample.
+// The kernel's shape, the parts of the keys and the tiles of queries that a block takes, by rules
+// on sizes alone (the lengths lie on the device): tile rows and keys of a mean sample, blocks.
 struct CrossPlan {
-  int qw, kw, nb, splits;
+  int qw, kw, nb, repeat;
+  Parts parts;
 };
 CrossPlan plan(int type, int64_t nq, int64_t nk, int batch, int D, int Hk, int group) {
   CrossPlan p;
-  const int64_t used = std::max<int64_t>(1, std::min<int64_t>(batch, nq));  // samples with queries
+  const int used = (int)std::max<int64_t>(1, std::min<int64_t>(batch, nq));  // samples with queries
   const int64_t rows = ceil_div(nq * group, used), keys = nk / used;
   auto blocks = [&](int qb) { return used * ceil_div(rows, qb) * Hk; };
-  if (rows <= 32 && (type == SCN_BF16 || D <= 96)) {
-    p = {1, type == SCN_BF16 || D <= 32 ? 4 : 2, 1, 1};
-  } else if (type == SCN_BF16 && D <= 64) {
-    p = blocks(128) < 512 ? CrossPlan{2, 2, 2, 1} : CrossPlan{4, 1, 2, 1};
-  } else if (type == SCN_BF16 || D <= 64) {
-    p = blocks(128) < 512 || type == SCN_F32 ? CrossPlan{4, 2, 1, 1} : CrossPlan{4, 1, 1, 1};
-  } else {
-    p = {4, 1, 1, 1};
-  }
-  p.splits = parts(blocks(32 * p.qw), 512, keys, 256);
+  const bool bf16 = type == SCN_BF16;
+  if (rows <= 32 && bf16)
+    p = {1, 4, 1, 1, {}};
+  else if (bf16 && D <= 64)
+    p = blocks(128) < 512 && keys > 128 ? CrossPlan{2, 2, 2, 1, {}} : CrossPlan{4, 1, 2, 1, {}};
+  else if (!bf16 && D <= 64 && rows <= 64 && keys > 64)
+    p = {2, 2, 1, 1, {}};
+  else if ((bf16 || D <= 64) && (blocks(128) < 512 || (!bf16 && D > 32)) && keys > 64)
+    p = {4, 2, 1, 1, {}};
+  else
+    p = {4, 1, 1, 1, {}};
+  p.parts = cut(blocks(32 * p.qw), WANT, keys, LEAST, used);
+  if (p.kw == 1 && keys <= 64 * p.nb)
+    p.repeat = (int)std::max<int64_t>(1, std::min<int64_t>(8, blocks(32 * p.qw) / REPEAT_BLOCKS));
   return p;
 }
 
-template <int NS, int DP, int QW, int KW, int NB>
-scn_status launch(const CrossArgs<NS>& a, hipStream_t st) {
+template <int NS, int DP, int QW, int KW, int NB, bool FEW = false>
+scn_status launch(CrossArgs<NS> a, const CrossPlan& p, hipStream_t st) {
   typedef Shape<NS, DP, QW, KW, NB> X;
   static LdsLimit limit;
-  auto fn = cross_fwd_kernel<NS, DP, QW, KW, NB>;
+  auto fn = cross_fwd_kernel<NS, DP, QW, KW, NB, FEW>;
   if (scn_status rc = allow_lds(reinterpret_cast<const void*>(fn), limit, X::SMEM)) return rc;
-  const int64_t blocks = (a.nq * a.group / X::QB + a.batch) * a.Hk * a.splits;
+  a.deal.rows = X::QB * a.repeat;
+  const int64_t blocks = a.deal.blocks();
   if (blocks > INT32_MAX) {
-    set_error("scn_cross_attn_fwd: more than 2^31 blocks of rows, heads and parts");
+    set_error("scn_cross_attn_fwd: more than 2^31 blocks of rows and heads");
     return SCN_ERR_OVERFLOW;
   }
   hipLaunchKernelGGL(fn, dim3((unsigned)blocks), dim3(X::NT), X::SMEM, st, a);
@@ -410,18 +460,19 @@ scn_status launch(const CrossArgs<NS>& a, hipStream_t st) {
 
 template <int NS, int DP>
 scn_status launch(const CrossArgs<NS>& a, const CrossPlan& p, hipStream_t st) {
-  if constexpr (NS == 1 || DP == 32) {
-    if (p.qw == 1) return launch<NS, DP, 1, 4, 1>(a, st);
-  } else if constexpr (DP <= 96) {
-    if (p.qw == 1) return launch<NS, DP, 1, 2, 1>(a, st);
-  }
+  if constexpr (NS == 1)
+    if (p.qw == 1) return launch<NS, DP, 1, 4, 1>(a, p, st);
   if constexpr (NS == 1 && DP <= 64) {
-    if (p.qw == 2) return launch<NS, DP, 2, 2, 2>(a, st);
-    return launch<NS, DP, 4, 1, 2>(a, st);
+    if (p.qw == 2) return launch<NS, DP, 2, 2, 2>(a, p, st);
+    if (p.repeat > 1) return launch<NS, DP, 4, 1, 2, true>(a, p, st);
+    return launch<NS, DP, 4, 1, 2>(a, p, st);
   } else {
+    if constexpr (NS == 3 && DP <= 64)
+      if (p.qw == 2) return launch<NS, DP, 2, 2, 1>(a, p, st);
     if constexpr (NS == 1 || DP <= 64)
-      if (p.kw == 2) return launch<NS, DP, 4, 2, 1>(a, st);
-    return launch<NS, DP, 4, 1, 1>(a, st);
+      if (p.kw == 2) return launch<NS, DP, 4, 2, 1>(a, p, st);
+    if (p.repeat > 1) return launch<NS, DP, 4, 1, 1, true>(a, p, st);
+    return launch<NS, DP, 4, 1, 1>(a, p, st);
   }
 }
 
@@ -431,15 +482,22 @@ scn_status run(const CrossArgs<NS>& a, const CrossPlan& p, hipStream_t st) {
                   : a.D <= 64 ? launch<NS, 64>(a, p, st)
                   : a.D <= 96 ? launch<NS, 96>(a, p, st)
                               : launch<NS, 128>(a, p, st);
-  if (rc || a.splits == 1) return rc;
-  hipLaunchKernelGGL(cross_join_kernel<NS>, dim3((unsigned)ceil_div(a.nq * a.Hk * a.group, 4)),
-                     dim3(256), 0, st, a);
+  if (rc || p.parts.most == 1) return rc;
+  // as many rows a block as leave the card some thousand blocks, of at most 256 threads
+  CrossArgs<NS> j = a;
+  j.deal.parts = Parts{1, INT32_MAX};
+  j.deal.rows = 1;
+  while (j.deal.rows * 2 * (a.D / 4) <= 256 &&
+         a.deal.tiles.n * a.group * a.deal.Hk / (j.deal.rows * 2) >= 1024)
+    j.deal.rows *= 2;
+  hipLaunchKernelGGL(cross_join_kernel<NS>, dim3((unsigned)j.deal.blocks()), dim3(256), 0,
+                     st, j, p.parts);
   SCN_LAUNCH_CHECK();
   return SCN_OK;
 }
 
 size_t part_bytes(const CrossPlan& p, int64_t nq, int Hq, int D) {
-  return p.splits > 1 ? (size_t)(nq * Hq * p.splits * (D + 2)) * 4 : 0;
+  return p.parts.most > 1 ? (size_t)(nq * Hq * p.parts.most * (D + 2)) * 4 : 0;
 }
 
 template <int NS>
@@ -447,9 +505,9 @@ CrossArgs<NS> make(int64_t nq, int64_t nk, int batch, const int32_t* qr, const i
                    int Hq, int Hk, const scn_heads* q, const scn_heads* k, const scn_heads* v,
                    float scale, const scn_heads* o, float* lse, const CrossPlan& p, void* ws) {
   typedef typename Elem<NS>::T T;
-  return CrossArgs<NS>{nq, nk, batch, D, Hk, Hq / Hk, p.splits, qr, kr, view<const T>(q),
-                       view<const T>(k), view<const T>(v), view<T>(o), lse, scale,
-                       static_cast<float*>(ws)};
+  const Deal deal{{qr, nq, Hq / Hk}, {kr, nk, 1}, batch, 0, Hk, p.parts};
+  return CrossArgs<NS>{deal, D, Hq / Hk, p.repeat, view<const T>(q), view<const T>(k),
+                       view<const T>(v), view<T>(o), lse, scale, static_cast<float*>(ws)};
 }
 
 }  // namespace
@@ -505,10 +563,6 @@ scn_status scn_cross_attn_fwd(int32_t type, int64_t nq, int64_t nk, int32_t batc
   if (need && (!ws || (reinterpret_cast<uintptr_t>(ws) & 15) != 0 || ws_bytes < need)) {
     set_error("%s: workspace missing, misaligned or too small", who);
     return SCN_ERR_WORKSPACE;
-  }
-  if (ceil_div(nq * Hq, 4) > INT32_MAX) {
-    set_error("%s: more than 2^31 blocks of rows and heads", who);
-    return SCN_ERR_OVERFLOW;
   }
   if (type == SCN_BF16)
     return run<1>(make<1>(nq, nk, batch, q_ranges, k_ranges, D, Hq, Hk, q, k, v, scale, o, lse, p, ws),
