@@ -640,8 +640,9 @@ typedef struct scn_tensor {
   int32_t type;
 } scn_tensor;
 
-/* Bytes of device workspace scn_grad_clip needs for `count` tensors. */
-size_t scn_grad_clip_workspace_bytes(int64_t count);
+/* Bytes of device workspace scn_grad_clip needs for `count` tensors of `elements` in all (0:
+ * none). */
+size_t scn_grad_clip_workspace_bytes(int64_t count, int64_t elements);
 
 /*
  * The norm of all gradients of a model taken together, and their clipping by it:

@@ -9,7 +9,9 @@ not been built the first call raises; there is no fallback.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
+from array import array
 from typing import Optional, Sequence
 
 import numpy as np
@@ -145,7 +147,7 @@ def lib() -> ctypes.CDLL:
         "scn_block_norm_bwd_workspace_bytes": (sz, [i64, i32]),
         "scn_block_norm_bwd": (st, [i32, i32, i64, i32, P, P, P, P, P, f32, f32, P, P, P, P, P, P,
                                     P, P, sz, P]),
-        "scn_grad_clip_workspace_bytes": (sz, [i64]),
+        "scn_grad_clip_workspace_bytes": (sz, [i64, i64]),
         "scn_grad_clip": (st, [i64, P, P, ctypes.c_double, P, P, sz, P]),
         "scn_set_allocator": (None, [_ALLOC_FN, _FREE_FN, P]),
         "scn_set_dense_forward": (st, [i64, i32]),
@@ -691,6 +693,12 @@ def attn_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_cache: torch.
     return o
 
 
+@functools.lru_cache(maxsize=4096)
+def _sized(name: str, *sizes) -> int:
+    """Workspace bytes of a call, a function of its sizes."""
+    return getattr(lib(), name)(*sizes)
+
+
 def _cross(q, k, v, q_ranges, k_ranges, scale):
     shape, dtype, dev = _first(q, "q")
     n, hq, d = shape
@@ -727,7 +735,7 @@ def cross_attn_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_ranges: 
     o, vo = _out_rows(out, q, (n, hq, d), "out")
     lse = torch.empty((hq, n), dtype=torch.float32, device=q.device)
     if ws is None:
-        need = lib().scn_cross_attn_fwd_workspace_bytes(SCN_TYPE[dtype], n, m, batch, d, hq, hk)
+        need = _sized("scn_cross_attn_fwd_workspace_bytes", SCN_TYPE[dtype], n, m, batch, d, hq, hk)
         ws = _bytes(need, q.device) if need else None
     _check(lib().scn_cross_attn_fwd(
         SCN_TYPE[dtype], n, m, batch, pq, pk, d, hq, hk, _ref(vq), _ref(vk), _ref(vv), scale,
@@ -753,8 +761,8 @@ def cross_attn_bwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.T
     dk, wk = _out_rows(out[1], q, (m, hk, d), "out[1]")
     dv, wv = _out_rows(out[2], q, (m, hk, d), "out[2]")
     if ws is None:
-        ws = _bytes(lib().scn_cross_attn_bwd_workspace_bytes(SCN_TYPE[dtype], n, m, batch, d, hq,
-                                                             hk), q.device)
+        ws = _bytes(_sized("scn_cross_attn_bwd_workspace_bytes", SCN_TYPE[dtype], n, m, batch, d,
+                           hq, hk), q.device)
     _check(lib().scn_cross_attn_bwd(
         SCN_TYPE[dtype], n, m, batch, pq, pk, d, hq, hk, _ref(vq), _ref(vk), _ref(vv), _ref(vo), pl,
         _ref(vg), scale, _ref(wq), _ref(wk), _ref(wv), ws.data_ptr(), ws.numel(),
@@ -855,12 +863,22 @@ def block_norm_bwd(x: torch.Tensor, f: Optional[torch.Tensor], z: Optional[torch
             res[name] = torch.empty(shape[1], dtype=torch.float32, device=x.device)
             pw[name] = res[name].data_ptr()
     if ws is None:
-        ws = _bytes(lib().scn_block_norm_bwd_workspace_bytes(*shape) if pw else 0, x.device)
+        ws = _bytes(_sized("scn_block_norm_bwd_workspace_bytes", *shape) if pw else 0, x.device)
     _check(lib().scn_block_norm_bwd(
         SCN_TYPE[x.dtype], SCN_TYPE[typ], shape[0], shape[1], _ref(vx), _ref(vf), _ref(vz), pf, ph,
         alpha, eps, _ref(vgy), _ref(vgh), _ref(vdx), _ref(vdf), _ref(vdz), pw.get("dwf"),
         pw.get("dwh"), ws.data_ptr(), ws.numel(), _raw_stream(dev)), "scn_block_norm_bwd")
     return res
+
+
+def _refuse_grad(t, dev: int, name: str):
+    """What `clip_grads` does not take."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype not in SCN_TYPE:
+        _refuse_rows(t, None, -1, (), name)
+    if t.get_device() != dev:
+        raise ValueError(f"{name} is on cuda:{t.get_device()}, which is not the current device")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
 
 
 def clip_grads(grads: Sequence[torch.Tensor], max_norm: float,
@@ -872,30 +890,36 @@ def clip_grads(grads: Sequence[torch.Tensor], max_norm: float,
     bfloat16 in any mix.  Returns the norm before, a float32 scalar on the device;
     nothing waits for it."""
     dev = torch.cuda.current_device()
-    rows, outs = [], None
-    for i, t in enumerate(grads):
-        if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype not in SCN_TYPE:
-            _refuse_rows(t, None, -1, (), f"grads[{i}]")
-        if t.get_device() != dev:
-            raise ValueError(f"grads[{i}] is on cuda:{t.get_device()}, which is not the current "
-                             "device")
-        if not t.is_contiguous():
-            raise ValueError(f"grads[{i}] must be contiguous")
-        rows.append((t.data_ptr(), t.numel(), SCN_TYPE[t.dtype]))
+    try:  # whole lists at a time: many tensors are looked over with each call
+        sizes = [t.numel() for t in grads]
+        rows = [x for r in zip([t.data_ptr() for t in grads], sizes,
+                               [SCN_TYPE[t.dtype] for t in grads]) for x in r]  # scn_tensor
+        fine = all([t.get_device() == dev and t.is_contiguous() for t in grads])
+    except (AttributeError, KeyError):
+        fine = False
+    if not fine:
+        for i, t in enumerate(grads):
+            _refuse_grad(t, dev, f"grads[{i}]")
+    n, outs = len(sizes), None
     if out is not None:
-        if len(out) != len(rows):
-            raise ValueError(f"out must hold {len(rows)} tensors, got {len(out)}")
+        if len(out) != n:
+            raise ValueError(f"out must hold {n} tensors, got {len(out)}")
         for i, (o, t) in enumerate(zip(out, grads)):
-            if _vector(o, t.dtype, dev, t.shape, f"out[{i}]") is None:
-                raise TypeError(f"out[{i}] must be a CUDA (HIP) tensor")
-        outs = np.array([o.data_ptr() for o in out], dtype=np.uint64)
-    table = np.array(rows, dtype=np.int64).reshape(len(rows), 3)  # scn_tensor
-    norm = torch.empty((), dtype=torch.float32, device=f"cuda:{dev}")
+            if not (isinstance(o, torch.Tensor) and o.dtype == t.dtype and o.shape == t.shape and
+                    o.get_device() == dev and o.is_contiguous()):
+                _dev_tensor(o, t.dtype, t.shape, f"out[{i}]")
+                raise TypeError(f"out[{i}] must be on cuda:{dev}, got {o.device}")
+        outs = array("Q", [o.data_ptr() for o in out])
+    rows = array("q", rows)
+    device = torch.device("cuda", dev)
+    norm = torch.empty((), dtype=torch.float32, device=device)
     if ws is None:
-        ws = _bytes(lib().scn_grad_clip_workspace_bytes(len(rows)), norm.device)
+        need = lib().scn_grad_clip_workspace_bytes(n, sum(sizes))
+        ws = _bytes(need, device) if need else None
     _check(lib().scn_grad_clip(
-        len(rows), table.ctypes.data, None if outs is None else outs.ctypes.data, max_norm,
-        norm.data_ptr(), ws.data_ptr(), ws.numel(), _raw_stream(dev)), "scn_grad_clip")
+        n, rows.buffer_info()[0], None if outs is None else outs.buffer_info()[0], max_norm,
+        norm.data_ptr(), None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(),
+        _raw_stream(dev)), "scn_grad_clip")
     return norm
 
 
