@@ -44,14 +44,21 @@ struct Work {
 // attn.h's, tile t of sample b being ranges[b] many / rows + b + t, and no block has to know more
 // than its own sample.  Split, each block counts the samples' tiles and parts, 64 samples at a
 // time, so that the blocks without work are the last ones: each costs 2 us of a place on the
-// card.
+// card.  Work-groups go to the XCDs in turn, which spreads the key heads of a tile over them;
+// `near` has them follow each other on one XCD, for few rows of heads that share cache lines
+// (one row over 262,144 states, 4 heads of 32 bf16 channels: 37 us, 53 otherwise; many tiles
+// of rows with whole lines to each head lose 6%, for an XCD then reads all heads' states).
 struct Deal {
   Side tiles, steps;
   int batch, rows, Hk;
   Parts parts;
+  bool near;
 
   // blocks of a launch
-  int64_t blocks() const { return (tiles.n * tiles.many / rows + batch) * Hk * parts.most; }
+  int64_t blocks() const {
+    const int64_t n = (tiles.n * tiles.many / rows + batch) * parts.most;
+    return (near ? ceil_div(n, 8) * 8 : n) * Hk;
+  }
   __device__ inline int count(int b) const {
     if (b >= batch) return 0;
     const int m = tiles.at(b + 1) - tiles.at(b), o = steps.at(b + 1) - steps.at(b);
@@ -60,8 +67,9 @@ struct Deal {
            parts.of(max(o, 0) * (int64_t)steps.many) * Hk;
   }
   // Every lane of the wave takes part.
-  __device__ inline Work find(int item) const {
+  __device__ inline Work find(int block) const {
     const int lane = threadIdx.x & 63;
+    const int item = near ? (block / (8 * Hk) * 8 + block % 8) * Hk + block / 8 % Hk : block;
     int sample = 0, local = 0;
     bool none = false;  // past the last work
     Work w;

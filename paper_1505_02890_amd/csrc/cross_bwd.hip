@@ -880,7 +880,8 @@ CrossBwdArgs<NS> make(int64_t nq, int64_t nk, int batch, const int32_t* qr, cons
   float* const f = static_cast<float*>(ws);
   const int64_t n = stat_floats(nq, Hq);
   const Side qs{qr, nq, Hq / Hk}, ks{kr, nk, 1};
-  return CrossBwdArgs<NS>{Deal{qs, ks, batch, 0, Hk, p.qparts}, Deal{ks, qs, batch, 0, Hk, p.kparts},
+  return CrossBwdArgs<NS>{Deal{qs, ks, batch, 0, Hk, p.qparts, false},
+                          Deal{ks, qs, batch, 0, Hk, p.kparts, false},
                           D, Hq / Hk, p.repeat, view<const T>(q), view<const T>(k), view<const T>(v),
                           view<const T>(o), view<const T>(d_o), view<T>(dq), view<T>(dk),
                           view<T>(dv), lse, f, f + n, f + 2 * n, scale, f + 3 * n, f + 3 * n};

@@ -12,12 +12,6 @@
 #ifndef REPEAT_BLOCKS
 #define REPEAT_BLOCKS 768
 #endif
-#ifndef WANT
-#define WANT 1024
-#endif
-#ifndef LEAST
-#define LEAST 512
-#endif
 namespace scn {
 namespace {
 
@@ -71,6 +65,57 @@ __device__ inline void cross_row(const CrossArgs<NS>& a, int64_t row, int h, int
   if (a.lse && lane == 0) a.lse[a.at(row, h)] = r.top + logf(r.sum);
 }
 
+// m, l: maximum (log 2) and sum of the terms that an output holds; f, f2: what both outputs are
+// taken times.  A side without terms has m = -inf and l = 0.
+__device__ inline void join(float& m, float& l, float m2, float l2, float& f, float& f2) {
+  const float t = fmaxf(m, m2), b = t == -INFINITY ? 0.f : t;
+  f = __builtin_amdgcn_exp2f(m - b);
+  f2 = __builtin_amdgcn_exp2f(m2 - b);
+  l = l * f + l2 * f2;
+  m = t;
+}
+// A wave's 32 tile rows from `first` on: out, or to the workspace where the keys are split, and
+// those that attn.h's bounds do not serve once more.
+template <int NS, int DP>
+__device__ __forceinline__ void finish(const CrossArgs<NS>& a, const Work& w, const v16f (&O)[DP / 32],
+                              float top, float sum, int first, bool mine, int64_t row, int h) {
+  const int lane = threadIdx.x & 63, half = lane >> 5;
+  if (w.parts > 1) {
+    if (mine) {
+      const int64_t to = a.at(row, h);
+      float* const o = a.out(to, w.part);
+#pragma unroll
+      for (int d = 0; d < DP / 32; ++d) store_cols<3>(o, O[d], 1.f, d, a.D, lane);
+      if (half == 0) {
+        float* const s = a.sums(to, w.part);
+        s[0] = top;
+        s[1] = sum;
+      }
+    }
+    return;
+  }
+  // (no key seen: nothing, and a log sum of -inf)
+  const float inv = w.mo > 0 ? 1.f / sum : 0.f;
+  bool fine = fabsf(top) < INFINITY && sum > SUM_LEAST && sum < SUM_MOST;
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d) fine &= finite16(O[d]);
+  if constexpr (NS == 3) fine &= !tiny(O, inv);
+  if constexpr (NS == 1) fine |= a.D == DP && nan_score(top, sum);  // NaN, as it stands
+  if (mine) {
+    auto* const o = a.o.p + row * a.o.row + h * a.o.head;
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d) store_cols<NS>(o, O[d], inv, d, a.D, lane);
+    if (a.lse && half == 0) a.lse[a.at(row, h)] = (top + log2f(sum)) * LN2;
+  }
+  // rows that attn.h's bounds do not serve (SUM_LEAST, tiny)
+  const uint64_t bad = __ballot(mine && !fine && w.mo > 0);
+  uint32_t rows = (uint32_t)bad | (uint32_t)(bad >> 32);
+  for (; rows; rows &= rows - 1) {
+    const int x = first + __builtin_ctz(rows);
+    cross_row<NS>(a, w.base + x / a.group, w.hk * a.group + x % a.group, w.other, w.mo);
+  }
+}
+
 // QW waves of 32 tile rows by KW groups that share out the keys of a tile, 32 NB each
 template <int NS, int DP, int QW_, int KW_, int NB_>
 struct Shape {
@@ -85,13 +130,11 @@ struct Shape {
 
 // FEW: a work is several tiles of queries in turn
 template <int NS, int DP, int QW, int KW, int NB, bool FEW>
-__global__ void __launch_bounds__(64 * QW * KW, DP > 96 && (NS == 3 || QW == 1) ? 1 : 2)
+__global__ void __launch_bounds__(64 * QW * KW, NS == 3 && DP > 96 ? 1 : 2)
     cross_fwd_kernel(CrossArgs<NS> a) {
   typedef Shape<NS, DP, QW, KW, NB> X;
   typedef typename X::L L;
   constexpr int QB = X::QB, KT = X::KT, NT = X::NT;
-  // Single rows' weights keep 16 bits, in two parts: the matrix cores wait for memory there.
-  constexpr bool TWO = NS == 1 && QW == 1;
   extern __shared__ char smem[];
   const int tid = threadIdx.x, lane = tid & 63, n32 = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), kw = KW == 1 ? 0 : wave / QW;
@@ -201,19 +244,9 @@ __global__ void __launch_bounds__(64 * QW * KW, DP > 96 && (NS == 3 || QW == 1) 
 #pragma unroll
         for (int j = 0; j < 8; ++j) p[j] = S[b][8 * s + j];
         const Frag<NS> P = to_frag<NS>(p);
-        Frag<NS> P2;
-        if constexpr (TWO) {
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
-            P2.s[0][j] = cvt2_bf16(p[2 * j] - __uint_as_float(P.s[0][j] << 16),
-                                   p[2 * j + 1] - __uint_as_float(P.s[0][j] & 0xffff0000u));
-        }
-#pragma unroll
-        for (int d = 0; d < DP / 32; ++d) {
-          const Frag<NS> W = EARLY ? V[b][s][d] : L::cols(vt, at, 32 * b + 16 * s, d);
-          if constexpr (TWO) O[d] = mma<NS>(W, P2, O[d]);
-          O[d] = mma<NS>(W, P, O[d]);
-        }
+        for (int d = 0; d < DP / 32; ++d)
+          O[d] = mma<NS>(EARLY ? V[b][s][d] : L::cols(vt, at, 32 * b + 16 * s, d), P, O[d]);
       }
     }
   };
@@ -276,41 +309,7 @@ __global__ void __launch_bounds__(64 * QW * KW, DP > 96 && (NS == 3 || QW == 1) 
         for (int e = 0; e < 16; ++e) O[d][e] = O[d][e] * f + o[(d * 16 + e) * 64] * f2;
     }
   }
-  if (w.parts > 1) {
-    if (mine) {
-      const int64_t to = a.at(row, h);
-      float* const o = a.out(to, w.part);
-#pragma unroll
-      for (int d = 0; d < DP / 32; ++d) store_cols<3>(o, O[d], 1.f, d, a.D, lane);
-      if (half == 0) {
-        float* const s = a.sums(to, w.part);
-        s[0] = top;
-        s[1] = sum;
-      }
-    }
-    return;
-  }
-  // (no key seen: nothing, and a log sum of -inf)
-  const float inv = mk > 0 ? 1.f / sum : 0.f;
-  bool fine = fabsf(top) < INFINITY && sum > SUM_LEAST && sum < SUM_MOST;
-#pragma unroll
-  for (int d = 0; d < DP / 32; ++d) fine &= finite16(O[d]);
-  if constexpr (NS == 3) fine &= !tiny(O, inv);
-  if constexpr (NS == 1) fine |= a.D == DP && nan_score(top, sum);  // NaN, as it stands
-  if (mine) {
-    auto* const o = a.o.p + row * a.o.row + h * a.o.head;
-#pragma unroll
-    for (int d = 0; d < DP / 32; ++d) store_cols<NS>(o, O[d], inv, d, a.D, lane);
-    if (a.lse && half == 0) a.lse[a.at(row, h)] = (top + log2f(sum)) * LN2;
-  }
-  // rows that attn.h's bounds do not serve (SUM_LEAST, tiny)
-  const uint64_t bad = __ballot(mine && !fine && mk > 0);
-  uint32_t rows = (uint32_t)bad | (uint32_t)(bad >> 32);
-  const int w0 = first + wave * 32;
-  for (; rows; rows &= rows - 1) {
-    const int x = w0 + __builtin_ctz(rows);
-    cross_row<NS>(a, w.base + x / a.group, hk * a.group + x % a.group, k0, mk);
-  }
+  finish<NS, DP>(a, w, O, top, sum, first + wave * 32, mine, row, h);
   };
   if constexpr (!FEW) {
     sweep(w.first, true);
@@ -319,6 +318,270 @@ __global__ void __launch_bounds__(64 * QW * KW, DP > 96 && (NS == 3 || QW == 1) 
     for (int first = w.first; first < end; first += QB)
       sweep(first, first == w.first || t1 - t0 > 2);
   }
+}
+
+// Few bf16 rows: one tile of 32 a block, whose waves take 32 keys at a time each, through its own
+// part of LDS and without a barrier (attn_step.hip), up to AHEAD tiles ahead in registers.  The
+// weights keep 16 bits, in two parts: the matrix cores wait for memory here, and one
+// row's output is all that a step of a stream gives.
+template <int DP>
+struct Thin {
+  static constexpr int WAVES = 4, NT = 64 * WAVES, AHEAD = DP <= 64 ? 2 : 1;
+  typedef Tile<1, DP, 32> L;
+  static constexpr int JOIN = DP / 32 * 16 + 2;
+  static constexpr int SMEM = std::max(WAVES * 2 * L::BYTES, (WAVES - 1) * JOIN * 256);
+};
+template <int DP>
+__global__ void __launch_bounds__(Thin<DP>::NT, 2) cross_thin_kernel(CrossArgs<1> a) {
+  typedef Thin<DP> X;
+  typedef typename X::L L;
+  typedef Stage<1, DP, 32, 64> St;
+  constexpr int WAVES = X::WAVES, AHEAD = X::AHEAD;
+  __shared__ __align__(16) char smem[X::SMEM];
+  const Work w = a.deal.find(blockIdx.x);
+  if (w.first >= w.m) return;
+  const int tid = threadIdx.x, lane = tid & 63, n32 = lane & 31, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const bool mine = w.first + n32 < w.m;
+  const int rr = min(w.first + n32, w.m - 1), h = w.hk * a.group + rr % a.group;
+  const int64_t row = w.base + rr / a.group;
+  const float c2 = a.scale * LOG2E;
+  Frag<1> Q[DP / 16];
+#pragma unroll
+  for (int s = 0; s < DP / 16; ++s)
+    Q[s] = load_frag<1>(a.q.p + row * a.q.row + h * a.q.head, s, a.D, lane);
+  v16f O[DP / 32];
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d) O[d] = zero16();
+  float top = -INFINITY, base = 0.f, sum = 0.f;
+
+  const int nt = (w.mo + 31) / 32, per = (nt + w.parts - 1) / w.parts;
+  const int t1 = min(nt, (w.part + 1) * per);
+  const uint16_t* const kp = a.k.p + w.other * a.k.row + w.hk * a.k.head;
+  const uint16_t* const vp = a.v.p + w.other * a.v.row + w.hk * a.v.head;
+  St sk[AHEAD], sv[AHEAD];
+  uint32_t ko[St::N], vo[St::N];
+  St::places(ko, a.k.row, a.D, lane);
+  St::places(vo, a.v.row, a.D, lane);
+  const typename L::Lane at(lane);
+  char* const kt = smem + wave * 2 * L::BYTES;
+  char* const vt = kt + L::BYTES;
+  auto fetch = [&](int u, int t) {
+    if (t < t1) {
+      sk[u].load(kp, a.k.row, ko, t * 32, w.mo - t * 32, a.D);
+      sv[u].load(vp, a.v.row, vo, t * 32, w.mo - t * 32, a.D);
+    }
+  };
+  auto take = [&](int u, int t) {
+    sk[u].store(kt, lane);
+    sv[u].store(vt, lane);
+    fetch(u, t + AHEAD * WAVES);
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    v16f S = zero16();
+#pragma unroll
+    for (int c = 0; c < DP / 16; ++c) S = mma<1>(L::rows(kt, at, 0, c), Q[c], S);
+    const int left = w.mo - t * 32;
+    if (left < 32)
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        S[r] = 8 * (r / 4) + 4 * half + r % 4 < left ? S[r] : -INFINITY;
+    float m = larger(S[0], S[1]);
+#pragma unroll
+    for (int r = 2; r < 16; ++r) m = larger(m, S[r]);
+    m = both_larger(m) * c2;
+    if (__ballot(m > top + 8.f)) {
+      const float next = fmaxf(top, m);
+      const float f = next == top ? 1.f : __builtin_amdgcn_exp2f(top - next);
+      top = next;
+      base = next == -INFINITY ? 0.f : next;
+      sum *= f;
+#pragma unroll
+      for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) O[d][r] *= f;
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      S[r] = __builtin_amdgcn_exp2f(fmaf(S[r], c2, -base));
+      sum += S[r];
+    }
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      Frag<1> P[2];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float x = S[8 * e + 2 * j], y = S[8 * e + 2 * j + 1];
+        const uint32_t hi = cvt2_bf16(x, y);
+        P[0].s[0][j] = hi;
+        P[1].s[0][j] = cvt2_bf16(x - __uint_as_float(hi << 16), y - __uint_as_float(hi & 0xffff0000u));
+      }
+#pragma unroll
+      for (int d = 0; d < DP / 32; ++d) {
+        const Frag<1> V = L::cols(vt, at, 16 * e, d);
+        O[d] = mma<1>(V, P[1], O[d]);
+        O[d] = mma<1>(V, P[0], O[d]);
+      }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  };
+  const int t0 = w.part * per + wave;
+#pragma unroll
+  for (int u = 0; u < AHEAD; ++u) fetch(u, t0 + u * WAVES);
+  for (int t = t0; t < t1; t += AHEAD * WAVES) {
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+      if (t + u * WAVES < t1) take(u, t + u * WAVES);
+  }
+  sum = both_sum(sum);
+  // the waves, joined in order
+  float* const x = reinterpret_cast<float*>(smem) + lane;
+  __syncthreads();
+  if (wave > 0) {
+    float* const o = x + (wave - 1) * X::JOIN * 64;
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[(d * 16 + r) * 64] = O[d][r];
+    o[(X::JOIN - 2) * 64] = top;
+    o[(X::JOIN - 1) * 64] = sum;
+  }
+  __syncthreads();
+  if (wave > 0) return;
+  for (int g = 0; g < WAVES - 1; ++g) {
+    const float* const o = x + g * X::JOIN * 64;
+    float f, f2;
+    join(top, sum, o[(X::JOIN - 2) * 64], o[(X::JOIN - 1) * 64], f, f2);
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) O[d][r] = O[d][r] * f + o[(d * 16 + r) * 64] * f2;
+  }
+  finish<1, DP>(a, w, O, top, sum, w.first, mine, row, h);
+}
+
+// Few fp32 rows, on the vector unit (attn_step.hip): LP lanes hold a key's channels, eight a lane,
+// straight from memory, and take GC tile rows while its row is in registers.  Each group of
+// LP lanes keeps a running maximum, sum and output of its own, which join within the wave
+// and the block.
+constexpr int FEW_NT = 256;
+template <int LP, int GC>
+__global__ void __launch_bounds__(FEW_NT) cross_few_kernel(CrossArgs<3> a) {
+  constexpr int U = 4;                    // keys of a lane group in flight
+  constexpr int KW = 64 / LP;             // keys of a wave at once
+  constexpr int KB = KW * (FEW_NT / 64);  // ... of the block
+  __shared__ float red[FEW_NT / 64][GC][LP * 8 + 2];
+  __shared__ bool bad[GC];
+  const Work w = a.deal.find(blockIdx.x);
+  if (w.first >= w.m) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int c = lane % LP * 8;
+  const bool on = c < a.D;
+  const int nh = min(GC, w.m - w.first);
+  const int per = (w.mo + w.parts - 1) / w.parts;
+  const int x0 = min(w.mo, w.part * per), x1 = min(w.mo, x0 + per);
+  const float* const k = a.k.p + w.other * a.k.row + w.hk * a.k.head + c;
+  const float* const v = a.v.p + w.other * a.v.row + w.hk * a.v.head + c;
+  auto row = [&](int g) { return w.base + (w.first + g) / a.group; };
+  auto head = [&](int g) { return w.hk * a.group + (w.first + g) % a.group; };
+
+  float q[GC][8], o[GC][8], m[GC], l[GC];
+#pragma unroll
+  for (int g = 0; g < GC; ++g) {
+    m[g] = -INFINITY;
+    l[g] = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) q[g][j] = o[g][j] = 0.f;
+    if (on && g < nh) load8<3>(a.q.p + row(g) * a.q.row + head(g) * a.q.head + c, q[g]);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) q[g][j] *= a.scale * LOG2E;
+  }
+  for (int x = x0 + wave * KW + lane / LP; x - lane / LP < x1; x += KB * U) {
+    float kk[U][8], vv[U][8];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int y = x + u * KB;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) kk[u][j] = vv[u][j] = 0.f;
+      if (on && y < x1) {
+        load8<3>(k + y * a.k.row, kk[u]);
+        load8<3>(v + y * a.v.row, vv[u]);
+      }
+    }
+#pragma unroll
+    for (int g = 0; g < GC; ++g) {
+      float sc[U], top = m[g];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        float d = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) d = fmaf(q[g][j], kk[u][j], d);
+        d = group_sum<LP>(d);
+        sc[u] = x + u * KB < x1 ? d : -INFINITY;
+        top = fmaxf(top, sc[u]);
+      }
+      const float b = top == -INFINITY ? 0.f : top;
+      const float f = __builtin_amdgcn_exp2f(m[g] - b);
+      m[g] = top;
+      l[g] *= f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) o[g][j] *= f;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const float e = __builtin_amdgcn_exp2f(sc[u] - b);
+        l[g] += e;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) o[g][j] = fmaf(e, vv[u][j], o[g][j]);
+      }
+    }
+  }
+  // the lane groups of the wave, then the waves
+#pragma unroll
+  for (int g = 0; g < GC; ++g) {
+#pragma unroll
+    for (int d = LP; d < 64; d <<= 1) {
+      float f, f2;
+      join(m[g], l[g], __shfl_xor(m[g], d), __shfl_xor(l[g], d), f, f2);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) o[g][j] = o[g][j] * f + __shfl_xor(o[g][j], d) * f2;
+    }
+    if (lane < LP) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) red[wave][g][c + j] = o[g][j];
+      red[wave][g][LP * 8] = m[g];
+      red[wave][g][LP * 8 + 1] = l[g];
+    }
+  }
+  if (tid < GC) bad[tid] = false;
+  __syncthreads();
+  for (int i = tid; i < nh * a.D; i += FEW_NT) {
+    const int g = i / a.D, ch = i % a.D;
+    float mm = red[0][g][LP * 8], ll = red[0][g][LP * 8 + 1], y = red[0][g][ch], f, f2;
+#pragma unroll
+    for (int u = 1; u < FEW_NT / 64; ++u) {
+      join(mm, ll, red[u][g][LP * 8], red[u][g][LP * 8 + 1], f, f2);
+      y = y * f + red[u][g][ch] * f2;
+    }
+    const int64_t at = a.at(row(g), head(g));
+    if (w.parts > 1) {
+      a.out(at, w.part)[ch] = y;
+      if (ch == 0) {
+        a.sums(at, w.part)[0] = mm;
+        a.sums(at, w.part)[1] = ll;
+      }
+    } else {
+      y = w.mo > 0 ? y / ll : 0.f;
+      a.o.p[row(g) * a.o.row + head(g) * a.o.head + ch] = y;
+      if (a.lse && ch == 0) a.lse[at] = (mm + log2f(ll)) * LN2;
+      // (a sum that is NaN says that the row is)
+      if (w.mo > 0 && !(fabsf(y) < INFINITY || ll != ll)) bad[g] = true;
+    }
+  }
+  if (w.parts > 1) return;
+  __syncthreads();
+  for (int g = wave; g < nh; g += FEW_NT / 64)
+    if (bad[g]) cross_row<3>(a, row(g), head(g), w.other, w.mo);
 }
 
 // The parts of the rows' outputs, joined in order: `deal.rows` tile rows a block, four channels
@@ -416,7 +679,8 @@ __global__ void __launch_bounds__(256) cross_join_kernel(CrossArgs<NS> a, Parts 
 // The kernel's shape, the parts of the keys and the tiles of queries that a block takes, by rules
 // on sizes alone (the lengths lie on the device): tile rows and keys of a mean sample, blocks.
 struct CrossPlan {
-  int qw, kw, nb, repeat;
+  int qw, kw, nb;  // qw 0: cross_few_kernel of nb tile rows
+  int repeat;
   Parts parts;
 };
 CrossPlan plan(int type, int64_t nq, int64_t nk, int batch, int D, int Hk, int group) {
@@ -425,7 +689,9 @@ CrossPlan plan(int type, int64_t nq, int64_t nk, int batch, int D, int Hk, int g
   const int64_t rows = ceil_div(nq * group, used), keys = nk / used;
   auto blocks = [&](int qb) { return used * ceil_div(rows, qb) * Hk; };
   const bool bf16 = type == SCN_BF16;
-  if (rows <= 32 && bf16)
+  if (!bf16 && rows <= 8)
+    p = {0, 0, rows <= 1 ? 1 : rows <= 2 ? 2 : rows <= 4 ? 4 : 8, 1, {}};
+  else if (rows <= 32 && bf16)
     p = {1, 4, 1, 1, {}};
   else if (bf16 && D <= 64)
     p = blocks(128) < 512 && keys > 128 ? CrossPlan{2, 2, 2, 1, {}} : CrossPlan{4, 1, 2, 1, {}};
@@ -435,10 +701,18 @@ CrossPlan plan(int type, int64_t nq, int64_t nk, int batch, int D, int Hk, int g
     p = {4, 2, 1, 1, {}};
   else
     p = {4, 1, 1, 1, {}};
-  p.parts = cut(blocks(32 * p.qw), WANT, keys, LEAST, used);
+  // Two blocks a CU, which is what resides; four where there are nearly as many anyway, for
+  // samples' lengths differ.
+  const int64_t n = p.qw ? blocks(32 * p.qw) : blocks(p.nb);
+  p.parts = cut(n, n >= 256 && p.qw > 1 ? 1024 : 512, keys, p.qw ? 512 : 256, used);
   if (p.kw == 1 && keys <= 64 * p.nb)
-    p.repeat = (int)std::max<int64_t>(1, std::min<int64_t>(8, blocks(32 * p.qw) / REPEAT_BLOCKS));
+    p.repeat = (int)std::max<int64_t>(1, std::min<int64_t>(8, n / REPEAT_BLOCKS));
   return p;
+}
+
+scn_status too_many() {
+  set_error("scn_cross_attn_fwd: more than 2^31 blocks of rows and heads");
+  return SCN_ERR_OVERFLOW;
 }
 
 template <int NS, int DP, int QW, int KW, int NB, bool FEW = false>
@@ -449,11 +723,39 @@ scn_status launch(CrossArgs<NS> a, const CrossPlan& p, hipStream_t st) {
   if (scn_status rc = allow_lds(reinterpret_cast<const void*>(fn), limit, X::SMEM)) return rc;
   a.deal.rows = X::QB * a.repeat;
   const int64_t blocks = a.deal.blocks();
-  if (blocks > INT32_MAX) {
-    set_error("scn_cross_attn_fwd: more than 2^31 blocks of rows and heads");
-    return SCN_ERR_OVERFLOW;
-  }
+  if (blocks > INT32_MAX) return too_many();
   hipLaunchKernelGGL(fn, dim3((unsigned)blocks), dim3(X::NT), X::SMEM, st, a);
+  SCN_LAUNCH_CHECK();
+  return SCN_OK;
+}
+
+template <int LP>
+scn_status launch_few(CrossArgs<3> a, const CrossPlan& p, hipStream_t st) {
+  a.deal.rows = p.nb;
+  const int64_t blocks = a.deal.blocks();
+  if (blocks > INT32_MAX) return too_many();
+  const dim3 grid((unsigned)blocks), block(FEW_NT);
+  if (p.nb == 1) hipLaunchKernelGGL((cross_few_kernel<LP, 1>), grid, block, 0, st, a);
+  if (p.nb == 2) hipLaunchKernelGGL((cross_few_kernel<LP, 2>), grid, block, 0, st, a);
+  if (p.nb == 4) hipLaunchKernelGGL((cross_few_kernel<LP, 4>), grid, block, 0, st, a);
+  if (p.nb == 8) hipLaunchKernelGGL((cross_few_kernel<LP, 8>), grid, block, 0, st, a);
+  SCN_LAUNCH_CHECK();
+  return SCN_OK;
+}
+scn_status launch_few(const CrossArgs<3>& a, const CrossPlan& p, hipStream_t st) {
+  if (a.D <= 8) return launch_few<1>(a, p, st);
+  if (a.D <= 16) return launch_few<2>(a, p, st);
+  if (a.D <= 32) return launch_few<4>(a, p, st);
+  if (a.D <= 64) return launch_few<8>(a, p, st);
+  return launch_few<16>(a, p, st);
+}
+
+template <int DP>
+scn_status launch_thin(CrossArgs<1> a, const CrossPlan& p, hipStream_t st) {
+  a.deal.rows = 32;
+  const int64_t blocks = a.deal.blocks();
+  if (blocks > INT32_MAX) return too_many();
+  hipLaunchKernelGGL(cross_thin_kernel<DP>, dim3((unsigned)blocks), dim3(Thin<DP>::NT), 0, st, a);
   SCN_LAUNCH_CHECK();
   return SCN_OK;
 }
@@ -461,7 +763,7 @@ scn_status launch(CrossArgs<NS> a, const CrossPlan& p, hipStream_t st) {
 template <int NS, int DP>
 scn_status launch(const CrossArgs<NS>& a, const CrossPlan& p, hipStream_t st) {
   if constexpr (NS == 1)
-    if (p.qw == 1) return launch<NS, DP, 1, 4, 1>(a, p, st);
+    if (p.qw == 1) return launch_thin<DP>(a, p, st);
   if constexpr (NS == 1 && DP <= 64) {
     if (p.qw == 2) return launch<NS, DP, 2, 2, 2>(a, p, st);
     if (p.repeat > 1) return launch<NS, DP, 4, 1, 2, true>(a, p, st);
@@ -478,14 +780,20 @@ scn_status launch(const CrossArgs<NS>& a, const CrossPlan& p, hipStream_t st) {
 
 template <int NS>
 scn_status run(const CrossArgs<NS>& a, const CrossPlan& p, hipStream_t st) {
-  scn_status rc = a.D <= 32   ? launch<NS, 32>(a, p, st)
-                  : a.D <= 64 ? launch<NS, 64>(a, p, st)
-                  : a.D <= 96 ? launch<NS, 96>(a, p, st)
-                              : launch<NS, 128>(a, p, st);
+  scn_status rc = SCN_OK;
+  bool few = false;
+  if constexpr (NS == 3)
+    if ((few = p.qw == 0)) rc = launch_few(a, p, st);
+  if (!few)
+    rc = a.D <= 32   ? launch<NS, 32>(a, p, st)
+         : a.D <= 64 ? launch<NS, 64>(a, p, st)
+         : a.D <= 96 ? launch<NS, 96>(a, p, st)
+                     : launch<NS, 128>(a, p, st);
   if (rc || p.parts.most == 1) return rc;
   // as many rows a block as leave the card some thousand blocks, of at most 256 threads
   CrossArgs<NS> j = a;
   j.deal.parts = Parts{1, INT32_MAX};
+  j.deal.near = false;
   j.deal.rows = 1;
   while (j.deal.rows * 2 * (a.D / 4) <= 256 &&
          a.deal.tiles.n * a.group * a.deal.Hk / (j.deal.rows * 2) >= 1024)
@@ -505,7 +813,8 @@ CrossArgs<NS> make(int64_t nq, int64_t nk, int batch, const int32_t* qr, const i
                    int Hq, int Hk, const scn_heads* q, const scn_heads* k, const scn_heads* v,
                    float scale, const scn_heads* o, float* lse, const CrossPlan& p, void* ws) {
   typedef typename Elem<NS>::T T;
-  const Deal deal{{qr, nq, Hq / Hk}, {kr, nk, 1}, batch, 0, Hk, p.parts};
+  const Deal deal{{qr, nq, Hq / Hk}, {kr, nk, 1}, batch, 0, Hk, p.parts,
+                  p.qw <= 1 && D * sizeof(T) < 128};
   return CrossArgs<NS>{deal, D, Hq / Hk, p.repeat, view<const T>(q), view<const T>(k),
                        view<const T>(v), view<T>(o), lse, scale, static_cast<float*>(ws)};
 }
