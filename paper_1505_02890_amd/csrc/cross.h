@@ -127,6 +127,10 @@ struct Deal {
   }
 };
 
+// Blocks that works of several tiles leave at least (up to 8 tiles to one: 120,011 rows of 4 fp32
+// heads on 2 of 32 over 40 states each, forward 53 us in works of 4 tiles, 56 of 2, 70 of 7).
+constexpr int FEW_BLOCKS = 768;
+
 // `blocks` blocks over samples of about `mean` steps, cut for `want` blocks in all where there
 // are fewer, in parts of `least` steps or more; a sample of twice the mean has all parts that it
 // would have by its length.
@@ -137,6 +141,57 @@ inline Parts cut(int64_t blocks, int64_t want, int64_t mean, int64_t least, int 
   const int64_t most = ceil_div(mean, least) * (samples > 1 ? 2 : 1);
   return Parts{(int)std::min<int64_t>(most, MAX_PARTS), (int)std::min<int64_t>(least, INT32_MAX)};
 }
+
+// What eight floats' rounding to bf16 left.  Weights and dS are rounded for their products,
+// which leaves a sum 1.4 times as far off as its own rounding, and more where one term holds
+// it; sums of few terms, which memory bounds, take them in two parts.
+__device__ inline Frag<1> low_part(const float (&v)[8], const Frag<1>& hi) {
+  Frag<1> f;
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    f.s[0][j] = cvt2_bf16(v[2 * j] - __uint_as_float(hi.s[0][j] << 16),
+                          v[2 * j + 1] - __uint_as_float(hi.s[0][j] & 0xffff0000u));
+  return f;
+}
+
+// A lane's row of an operand on its way from memory (load_frag in two steps).
+template <int NS, int DP>
+struct Ahead {
+  static constexpr int N = NS == 1 ? 1 : 2;
+  v4u r[DP / 16][N];
+  __device__ inline void load(const typename Elem<NS>::T* row, int D, int lane) {
+#pragma unroll
+    for (int s = 0; s < DP / 16; ++s) {
+      const int c = 16 * s + 8 * (lane >> 5);
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        r[s][i] = c < D ? *reinterpret_cast<const v4u*>(row + c + 4 * i) : v4u{0, 0, 0, 0};
+    }
+  }
+  __device__ inline void floats(int s, float (&v)[8]) const {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if constexpr (NS == 1) {
+        v[2 * j] = __uint_as_float(r[s][0][j] << 16);
+        v[2 * j + 1] = __uint_as_float(r[s][0][j] & 0xffff0000u);
+      } else {
+        v[j] = __uint_as_float(r[s][0][j]);
+        v[4 + j] = __uint_as_float(r[s][N - 1][j]);
+      }
+    }
+  }
+  __device__ inline Frag<NS> frag(int s) const {
+    if constexpr (NS == 1) {
+      Frag<NS> f;
+      f.s[0] = r[s][0];
+      return f;
+    } else {
+      float v[8];
+      floats(s, v);
+      return to_frag<NS>(v);
+    }
+  }
+};
 
 // host checks of both directions
 scn_status check_cross(const char* who, int32_t type, int64_t nq, int64_t nk, int32_t batch,

@@ -155,6 +155,7 @@ __global__ void __launch_bounds__(64 * QW * KW, (NS == 3 && DP > 32) || DP > 64 
   typedef typename X::L L;
   constexpr int KT = X::KT, NT = X::NT, QB = X::QB;
   constexpr bool EXACT = X::EXACT;
+  constexpr bool TWO = NS == 1 && (FEW || QW == 1);  // few terms, or few rows: low_part
   extern __shared__ char smem[];
   const int tid = threadIdx.x, lane = tid & 63, n32 = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), kw = KW == 1 ? 0 : wave / QW;
@@ -223,22 +224,55 @@ __global__ void __launch_bounds__(64 * QW * KW, (NS == 3 && DP > 32) || DP > 64 
         y[j] = P[8 * s + j];
       }
       const Frag<NS> X = to_frag<NS>(x), Y = to_frag<NS>(y);
+      Frag<NS> low;
+      if constexpr (TWO) low = low_part(y, Y);
 #pragma unroll
       for (int d = 0; d < DP / 32; ++d) {
         const Frag<NS> K = EXACT ? KC[s][d] : L::cols(kt, pl, 16 * s, d);
+        if constexpr (TWO) dQ[d] = mma<NS>(K, low, dQ[d]);
         dQ[d] = mma<NS>(K, Y, dQ[d]);
         if constexpr (EXACT) PK[d] = mma<NS>(K, X, PK[d]);
       }
     }
   };
+  // Works of several tiles load the next one's rows while they take one.
+  constexpr bool PRE = FEW && DP <= 32;
+  Ahead<NS, PRE ? DP : 16> nq, ng, no;
+  float nl;
+  auto ahead = [&](int first) {
+    const int r = min(first + (wave - kw * QW) * 32 + n32, w.m - 1);
+    const int h = hk * a.group + r % a.group;
+    const int64_t row = w.base + r / a.group;
+    nq.load(a.q.p + row * a.q.row + h * a.q.head, a.D, lane);
+    ng.load(a.d_o.p + row * a.d_o.row + h * a.d_o.head, a.D, lane);
+    no.load(a.o.p + row * a.o.row + h * a.o.head, a.D, lane);
+    nl = a.lse[a.at(row, h)];
+  };
   auto sweep = [&](int first, bool stage) {
-  const int r = first + (wave - kw * QW) * 32 + n32;
-  const bool mine = r < w.m;
-  const int rr = min(r, w.m - 1);
-  const int64_t row = w.base + rr / a.group;
-  const int h = hk * a.group + rr % a.group;
-  delta = over = 0.f;
-  {
+    const int r = first + (wave - kw * QW) * 32 + n32;
+    const bool mine = r < w.m;
+    const int rr = min(r, w.m - 1);
+    const int64_t row = w.base + rr / a.group;
+    const int h = hk * a.group + rr % a.group;
+    delta = over = 0.f;
+    float lse;
+    auto dot8 = [&](const float (&x)[8], const float (&y)[8]) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) delta = fmaf(x[j], y[j], delta);
+  };
+  if constexpr (PRE) {
+#pragma unroll
+    for (int s = 0; s < DP / 16; ++s) {
+      Q[s] = nq.frag(s);
+      G[s] = ng.frag(s);
+      float x[8], y[8];
+      ng.floats(s, x);
+      no.floats(s, y);
+      dot8(x, y);
+    }
+    lse = nl;
+    ahead(first + QB);
+  } else {
     const auto* const q = a.q.p + row * a.q.row + h * a.q.head;
     const auto* const g = a.d_o.p + row * a.d_o.row + h * a.d_o.head;
     const auto* const o = a.o.p + row * a.o.row + h * a.o.head;
@@ -251,14 +285,13 @@ __global__ void __launch_bounds__(64 * QW * KW, (NS == 3 && DP > 32) || DP > 64 
         float x[8], y[8];
         load8<NS>(g + c, x);
         load8<NS>(o + c, y);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) delta = fmaf(x[j], y[j], delta);
+        dot8(x, y);
       }
     }
+    lse = a.lse[a.at(row, h)];
   }
   delta = both_sum(delta);
   const int64_t at = a.at(row, h);
-  const float lse = a.lse[at];
   lse2 = lse * LOG2E;
   const bool far = !(fabsf(lse) <= LSE_MOST);  // the row is formed again ...
   const bool none = lse != lse;                 // ... if it has weights at all
@@ -368,6 +401,7 @@ __global__ void __launch_bounds__(64 * QW * KW, (NS == 3 && DP > 32) || DP > 64 
     sweep(w.first, true);
   } else {
     const int end = min(w.m, w.first + QB * a.repeat);
+    if constexpr (PRE) ahead(w.first);
     for (int first = w.first; first < end; first += QB)
       sweep(first, first == w.first || t1 - t0 > 2);
   }
@@ -475,7 +509,7 @@ __global__ void __launch_bounds__(256) cross_dq_join_kernel(CrossBwdArgs<NS> a, 
 // What a wave with 32 keys does with 32 queries of a tile: dV += P^T dO, dK += dS^T Q
 // (transposed).  Queries past the sample's last have a log sum of +inf, and so no weight.
 // EARLY reads each pair of products' operands ahead of them, for some 60 registers more.
-template <int NS, int DP, int TB, bool EARLY>
+template <int NS, int DP, int TB, bool EARLY, bool TWO>
 __device__ inline void key_block(char* qt, char* gt, const typename Tile<NS, DP, TB>::Lane& pl,
                                  const float* lse2, const float* delta, int r0,
                                  const Frag<NS> (&K)[DP / 16], const Frag<NS> (&V)[DP / 16],
@@ -533,10 +567,21 @@ __device__ inline void key_block(char* qt, char* gt, const typename Tile<NS, DP,
       y[j] = P[8 * s + j];
     }
     const Frag<NS> X = to_frag<NS>(x), Y = to_frag<NS>(y);
+    Frag<NS> xl, yl;
+    if constexpr (TWO) {
+      xl = low_part(x, X);
+      yl = low_part(y, Y);
+    }
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d) {
-      dV[d] = mma<NS>(EARLY ? GC[s][d] : L::cols(gt, pl, r0 + 16 * s, d), X, dV[d]);
-      dK[d] = mma<NS>(EARLY ? QC[s][d] : L::cols(qt, pl, r0 + 16 * s, d), Y, dK[d]);
+      const Frag<NS> G = EARLY ? GC[s][d] : L::cols(gt, pl, r0 + 16 * s, d);
+      const Frag<NS> Q = EARLY ? QC[s][d] : L::cols(qt, pl, r0 + 16 * s, d);
+      if constexpr (TWO) {
+        dV[d] = mma<NS>(G, xl, dV[d]);
+        dK[d] = mma<NS>(Q, yl, dK[d]);
+      }
+      dV[d] = mma<NS>(G, X, dV[d]);
+      dK[d] = mma<NS>(Q, Y, dK[d]);
     }
   }
 }
@@ -554,14 +599,14 @@ struct KeyShape {
   static_assert(SMEM <= 160 * 1024, "LDS of a compute unit");
 };
 
-template <int NS, int DP, int KW, int QW, int U>
+template <int NS, int DP, int KW, int QW, int U, bool TWO>
 __global__ void __launch_bounds__(64 * KW * QW, NS == 3 || DP > 64 ? 1 : 2)
     cross_dkv_kernel(CrossBwdArgs<NS> a) {
   typedef KeyShape<NS, DP, KW, QW, U> X;
   typedef typename X::L L;
   typedef typename X::St St;
   constexpr int TB = X::TB;
-  constexpr bool EARLY = NS == 1 && DP == 64 && QW < 4;
+  constexpr bool EARLY = NS == 1 && DP == 64 && QW < 4 && !TWO;
   extern __shared__ char smem[];
   const int tid = threadIdx.x, lane = tid & 63, n32 = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), qw = QW == 1 ? 0 : wave / KW;
@@ -632,7 +677,7 @@ __global__ void __launch_bounds__(64 * KW * QW, NS == 3 || DP > 64 ? 1 : 2)
       const float* const f = reinterpret_cast<const float*>(b + 2 * L::BYTES);
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        key_block<NS, DP, TB, EARLY>(b, b + L::BYTES, pl, f, f + TB, (qw * U + u) * 32, K, V, c2, dK,
+        key_block<NS, DP, TB, EARLY, TWO>(b, b + L::BYTES, pl, f, f + TB, (qw * U + u) * 32, K, V, c2, dK,
                                      dV);
       __syncthreads();
     }
@@ -721,19 +766,12 @@ __global__ void __launch_bounds__(256) cross_dkv_join_kernel(CrossBwdArgs<NS> a,
     if (bad[i]) dkv_row<NS>(a, w.base + w.first + i, w.hk, w.other, w.mo);
 }
 
-#ifndef WANT
-#define WANT 1024
-#endif
-#ifndef LEAST
-#define LEAST 512
-#endif
-#ifndef REPEAT_BLOCKS
-#define REPEAT_BLOCKS 768
-#endif
 // Shapes and parts of both passes, by rules on sizes alone (cross_fwd.hip)
 struct CrossBwdPlan {
-  int qw, qkw, repeat;  // queries' pass: waves of queries, groups of keys, tiles of a work
-  int kw, kqw;          // keys' pass: waves of keys, groups of queries
+  int qw, qkw, repeat;  // queries' pass: waves of queries, groups of keys; tiles of a work
+                        // where the keys are few, or 0
+  int kw;               // keys' pass: waves of keys (the others share out the queries)
+  bool two;             // ... few of which need their weights in two parts
   Parts qparts, kparts;
 };
 CrossBwdPlan plan(int type, int64_t nq, int64_t nk, int batch, int D, int Hk, int group) {
@@ -754,19 +792,21 @@ CrossBwdPlan plan(int type, int64_t nq, int64_t nk, int batch, int D, int Hk, in
     p.qw = keys <= 64 || (D > 64 && qblocks(128) >= 512) ? 4 : 2;
     p.qkw = p.qw == 4 ? 1 : 2;
   }
-  p.qparts = cut(qblocks(32 * p.qw), WANT, nk / usedq, LEAST, usedq);
-  p.repeat = 1;
+  p.qparts = cut(qblocks(32 * p.qw), 1024, nk / usedq, 512, usedq);
+  p.repeat = 0;
   if (p.qkw == 1 && keys <= 64)
-    p.repeat = (int)std::max<int64_t>(1, std::min<int64_t>(8, qblocks(32 * p.qw) / REPEAT_BLOCKS));
+    p.repeat = (int)std::max<int64_t>(1, std::min<int64_t>(8, qblocks(32 * p.qw) / FEW_BLOCKS));
+  p.two = bf16 && nq * group / usedk <= 128;
   if (!bf16) {
     p.kw = keys <= 32 && D <= 32 ? 1 : D <= 64 ? 2 : 4;
+  } else if (p.two) {
+    p.kw = 2;
   } else {
     p.kw = D <= 64 && (keys <= 32 || kblocks(128) < 128) ? 1
            : kblocks(128) < (D <= 64 ? 1024 : 384)       ? 2
                                                          : 4;
   }
-  p.kqw = 4 / p.kw;
-  p.kparts = cut(kblocks(32 * p.kw), WANT, nq * group / usedk, LEAST, usedk);
+  p.kparts = cut(kblocks(32 * p.kw), 1024, nq * group / usedk, 512, usedk);
   return p;
 }
 
@@ -790,7 +830,7 @@ scn_status launch_dq(CrossBwdArgs<NS> a, const CrossBwdPlan& p, hipStream_t st) 
   static LdsLimit limit;
   auto fn = cross_dq_kernel<NS, DP, QW, KW, FEW>;
   if (scn_status rc = allow_lds(reinterpret_cast<const void*>(fn), limit, X::SMEM)) return rc;
-  a.qdeal.rows = X::QB * a.repeat;
+  a.qdeal.rows = X::QB * std::max(1, a.repeat);
   const int64_t blocks = a.qdeal.blocks();
   if (blocks > INT32_MAX) return too_many();
   hipLaunchKernelGGL(fn, dim3((unsigned)blocks), dim3(X::NT), X::SMEM, st, a);
@@ -804,11 +844,11 @@ scn_status launch_dq(CrossBwdArgs<NS> a, const CrossBwdPlan& p, hipStream_t st) 
   return SCN_OK;
 }
 
-template <int NS, int DP, int KW, int QW, int U>
+template <int NS, int DP, int KW, int QW, int U, bool TWO>
 scn_status launch_dkv(CrossBwdArgs<NS> a, const CrossBwdPlan& p, hipStream_t st) {
   typedef KeyShape<NS, DP, KW, QW, U> X;
   static LdsLimit limit;
-  auto fn = cross_dkv_kernel<NS, DP, KW, QW, U>;
+  auto fn = cross_dkv_kernel<NS, DP, KW, QW, U, TWO>;
   if (scn_status rc = allow_lds(reinterpret_cast<const void*>(fn), limit, X::SMEM)) return rc;
   a.kdeal.rows = X::KB;
   const int64_t blocks = a.kdeal.blocks();
@@ -828,28 +868,31 @@ template <int NS, int DP>
 scn_status launch(const CrossBwdArgs<NS>& a, const CrossBwdPlan& p, hipStream_t st) {
   scn_status rc = SCN_OK;
   if (a.qdeal.tiles.n > 0) {
-    if (p.repeat > 1)
-      rc = launch_dq<NS, DP, 4, 1, true>(a, p, st);
-    else if (p.qkw == 1)
-      rc = launch_dq<NS, DP, 4, 1>(a, p, st);
-    else if constexpr (NS == 1)
+    if (p.qkw == 1) {
+      if constexpr (DP <= 64)  // (narrow heads take four waves side by side for few keys alone)
+        rc = launch_dq<NS, DP, 4, 1, true>(a, p, st);
+      else
+        rc = p.repeat ? launch_dq<NS, DP, 4, 1, true>(a, p, st) : launch_dq<NS, DP, 4, 1>(a, p, st);
+    } else if constexpr (NS == 1) {
       rc = p.qw == 1 ? launch_dq<NS, DP, 1, 4>(a, p, st) : launch_dq<NS, DP, 2, 2>(a, p, st);
-    else if constexpr (DP <= 64)
+    } else if constexpr (DP <= 64) {
       rc = launch_dq<NS, DP, (DP > 32 ? 4 : 2), 2>(a, p, st);
+    }
   }
   if (rc || a.kdeal.tiles.n == 0) return rc;
   if constexpr (NS == 3) {
     if constexpr (DP <= 32)
-      if (p.kw == 1) return launch_dkv<NS, DP, 1, 4, 1>(a, p, st);
+      if (p.kw == 1) return launch_dkv<NS, DP, 1, 4, 1, false>(a, p, st);
     if constexpr (DP <= 64)
-      return launch_dkv<NS, DP, 2, 2, 1>(a, p, st);
+      return launch_dkv<NS, DP, 2, 2, 1, false>(a, p, st);
     else
-      return launch_dkv<NS, DP, 4, 1, 1>(a, p, st);
+      return launch_dkv<NS, DP, 4, 1, 1, false>(a, p, st);
   } else {
+    if (p.two) return launch_dkv<NS, DP, 2, 2, 1, true>(a, p, st);
     if constexpr (DP <= 64)
-      if (p.kw == 1) return launch_dkv<NS, DP, 1, 4, 1>(a, p, st);
-    if (p.kw == 2) return launch_dkv<NS, DP, 2, 2, 1>(a, p, st);
-    return launch_dkv<NS, DP, 4, 1, 2>(a, p, st);
+      if (p.kw == 1) return launch_dkv<NS, DP, 1, 4, 1, false>(a, p, st);
+    if (p.kw == 2) return launch_dkv<NS, DP, 2, 2, 1, false>(a, p, st);
+    return launch_dkv<NS, DP, 4, 1, 2, false>(a, p, st);
   }
 }
 

@@ -9,9 +9,6 @@
 
 #include "cross.h"
 
-#ifndef REPEAT_BLOCKS
-#define REPEAT_BLOCKS 768
-#endif
 namespace scn {
 namespace {
 
@@ -135,6 +132,7 @@ __global__ void __launch_bounds__(64 * QW * KW, NS == 3 && DP > 96 ? 1 : 2)
   typedef Shape<NS, DP, QW, KW, NB> X;
   typedef typename X::L L;
   constexpr int QB = X::QB, KT = X::KT, NT = X::NT;
+  constexpr bool TWO = NS == 1 && FEW;  // few keys: low_part
   extern __shared__ char smem[];
   const int tid = threadIdx.x, lane = tid & 63, n32 = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), kw = KW == 1 ? 0 : wave / QW;
@@ -244,77 +242,95 @@ __global__ void __launch_bounds__(64 * QW * KW, NS == 3 && DP > 96 ? 1 : 2)
 #pragma unroll
         for (int j = 0; j < 8; ++j) p[j] = S[b][8 * s + j];
         const Frag<NS> P = to_frag<NS>(p);
+        Frag<NS> low;
+        if constexpr (TWO) low = low_part(p, P);
 #pragma unroll
-        for (int d = 0; d < DP / 32; ++d)
-          O[d] = mma<NS>(EARLY ? V[b][s][d] : L::cols(vt, at, 32 * b + 16 * s, d), P, O[d]);
+        for (int d = 0; d < DP / 32; ++d) {
+          const Frag<NS> W = EARLY ? V[b][s][d] : L::cols(vt, at, 32 * b + 16 * s, d);
+          if constexpr (TWO) O[d] = mma<NS>(W, low, O[d]);
+          O[d] = mma<NS>(W, P, O[d]);
+        }
       }
     }
   };
+  // Works of several tiles load the next one's queries while they take one.
+  constexpr bool PRE = FEW && DP <= 64;
+  Ahead<NS, PRE ? DP : 16> next;
+  auto ahead = [&](int first) {
+    const int r = min(first + (wave - kw * QW) * 32 + n32, w.m - 1);
+    next.load(a.q.p + (w.base + r / a.group) * a.q.row + (hk * a.group + r % a.group) * a.q.head, a.D,
+              lane);
+  };
   auto sweep = [&](int first, bool stage) {
-  const int r = first + (wave - kw * QW) * 32 + n32;  // the lane's tile row
-  const bool mine = r < w.m;
-  const int rr = min(r, w.m - 1);
-  const int64_t row = w.base + rr / a.group;
-  const int h = hk * a.group + rr % a.group;
-  {
-    const auto* const q = a.q.p + row * a.q.row + h * a.q.head;
+    const int r = first + (wave - kw * QW) * 32 + n32;  // the lane's tile row
+    const bool mine = r < w.m;
+    const int rr = min(r, w.m - 1);
+    const int64_t row = w.base + rr / a.group;
+    const int h = hk * a.group + rr % a.group;
+    if constexpr (PRE) {
 #pragma unroll
-    for (int s = 0; s < DP / 16; ++s) Q[s] = load_frag<NS>(q, s, a.D, lane);
-  }
+      for (int s = 0; s < DP / 16; ++s) Q[s] = next.frag(s);
+      ahead(first + QB);
+    } else {
+      const auto* const q = a.q.p + row * a.q.row + h * a.q.head;
 #pragma unroll
-  for (int d = 0; d < DP / 32; ++d) O[d] = zero16();
-  top = limit = -INFINITY;
-  base = sum = 0.f;
-  // While a tile is taken, the next one goes from registers to the other buffer and the
-  // one after that is loaded.  Two tiles or fewer stay for the block's next queries.
-  if (stage && t0 < t1) {
-    fetch(t0);
-    put(t0);
-    if (t0 + 1 < t1) fetch(t0 + 1);
-    __syncthreads();
-  }
-  for (int t = t0; t < t1; ++t) {
-    if (stage) {
-      if (t + 1 < t1) put(t + 1);
-      if (t + 2 < t1) fetch(t + 2);
+      for (int s = 0; s < DP / 16; ++s) Q[s] = load_frag<NS>(q, s, a.D, lane);
     }
-    take(t);
-    if (stage) __syncthreads();
-  }
-  sum = both_sum(sum);
-  if constexpr (KW > 1) {
-    // the groups' shares of the keys, joined in order
-    float* const x = reinterpret_cast<float*>(smem) + lane;
-    if (kw > 0) {
-      float* const o = x + (wave - QW) * X::JOIN * 64;
 #pragma unroll
-      for (int d = 0; d < DP / 32; ++d)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) o[(d * 16 + e) * 64] = O[d][e];
-      o[(X::JOIN - 2) * 64] = top;
-      o[(X::JOIN - 1) * 64] = sum;
+    for (int d = 0; d < DP / 32; ++d) O[d] = zero16();
+    top = limit = -INFINITY;
+    base = sum = 0.f;
+    // While a tile is taken, the next one goes from registers to the other buffer and the
+    // one after that is loaded.  Two tiles or fewer stay for the block's next queries.
+    if (stage && t0 < t1) {
+      fetch(t0);
+      put(t0);
+      if (t0 + 1 < t1) fetch(t0 + 1);
+      __syncthreads();
     }
-    __syncthreads();
-    if (kw > 0) return;
-    for (int g = 1; g < KW; ++g) {
-      const float* const o = x + ((g - 1) * QW + wave) * X::JOIN * 64;
-      const float top2 = o[(X::JOIN - 2) * 64], now = fmaxf(top, top2);
-      const float base = now == -INFINITY ? 0.f : now;
-      const float f = __builtin_amdgcn_exp2f(top - base), f2 = __builtin_amdgcn_exp2f(top2 - base);
-      top = now;
-      sum = sum * f + o[(X::JOIN - 1) * 64] * f2;
-#pragma unroll
-      for (int d = 0; d < DP / 32; ++d)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) O[d][e] = O[d][e] * f + o[(d * 16 + e) * 64] * f2;
+    for (int t = t0; t < t1; ++t) {
+      if (stage) {
+        if (t + 1 < t1) put(t + 1);
+        if (t + 2 < t1) fetch(t + 2);
+      }
+      take(t);
+      if (stage) __syncthreads();
     }
-  }
-  finish<NS, DP>(a, w, O, top, sum, first + wave * 32, mine, row, h);
+    sum = both_sum(sum);
+    if constexpr (KW > 1) {
+      // the groups' shares of the keys, joined in order
+      float* const x = reinterpret_cast<float*>(smem) + lane;
+      if (kw > 0) {
+        float* const o = x + (wave - QW) * X::JOIN * 64;
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[(d * 16 + e) * 64] = O[d][e];
+        o[(X::JOIN - 2) * 64] = top;
+        o[(X::JOIN - 1) * 64] = sum;
+      }
+      __syncthreads();
+      if (kw > 0) return;
+      for (int g = 1; g < KW; ++g) {
+        const float* const o = x + ((g - 1) * QW + wave) * X::JOIN * 64;
+        const float top2 = o[(X::JOIN - 2) * 64], now = fmaxf(top, top2);
+        const float base = now == -INFINITY ? 0.f : now;
+        const float f = __builtin_amdgcn_exp2f(top - base), f2 = __builtin_amdgcn_exp2f(top2 - base);
+        top = now;
+        sum = sum * f + o[(X::JOIN - 1) * 64] * f2;
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) O[d][e] = O[d][e] * f + o[(d * 16 + e) * 64] * f2;
+      }
+    }
+    finish<NS, DP>(a, w, O, top, sum, first + wave * 32, mine, row, h);
   };
   if constexpr (!FEW) {
     sweep(w.first, true);
   } else {
     const int end = min(w.m, w.first + QB * a.repeat);
+    if constexpr (PRE) ahead(w.first);
     for (int first = w.first; first < end; first += QB)
       sweep(first, first == w.first || t1 - t0 > 2);
   }
@@ -322,8 +338,7 @@ __global__ void __launch_bounds__(64 * QW * KW, NS == 3 && DP > 96 ? 1 : 2)
 
 // Few bf16 rows: one tile of 32 a block, whose waves take 32 keys at a time each, through its own
 // part of LDS and without a barrier (attn_step.hip), up to AHEAD tiles ahead in registers.  The
-// weights keep 16 bits, in two parts: the matrix cores wait for memory here, and one
-// row's output is all that a step of a stream gives.
+// weights keep 16 bits (low_part): the matrix cores wait for memory here.
 template <int DP>
 struct Thin {
   static constexpr int WAVES = 4, NT = 64 * WAVES, AHEAD = DP <= 64 ? 2 : 1;
@@ -408,19 +423,15 @@ __global__ void __launch_bounds__(Thin<DP>::NT, 2) cross_thin_kernel(CrossArgs<1
     }
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      Frag<1> P[2];
+      float p[8];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float x = S[8 * e + 2 * j], y = S[8 * e + 2 * j + 1];
-        const uint32_t hi = cvt2_bf16(x, y);
-        P[0].s[0][j] = hi;
-        P[1].s[0][j] = cvt2_bf16(x - __uint_as_float(hi << 16), y - __uint_as_float(hi & 0xffff0000u));
-      }
+      for (int j = 0; j < 8; ++j) p[j] = S[8 * e + j];
+      const Frag<1> P = to_frag<1>(p), low = low_part(p, P);
 #pragma unroll
       for (int d = 0; d < DP / 32; ++d) {
         const Frag<1> V = L::cols(vt, at, 16 * e, d);
-        O[d] = mma<1>(V, P[1], O[d]);
-        O[d] = mma<1>(V, P[0], O[d]);
+        O[d] = mma<1>(V, low, O[d]);
+        O[d] = mma<1>(V, P, O[d]);
       }
     }
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
@@ -680,7 +691,7 @@ __global__ void __launch_bounds__(256) cross_join_kernel(CrossArgs<NS> a, Parts 
 // on sizes alone (the lengths lie on the device): tile rows and keys of a mean sample, blocks.
 struct CrossPlan {
   int qw, kw, nb;  // qw 0: cross_few_kernel of nb tile rows
-  int repeat;
+  int repeat;      // tiles of a work where the keys are few, or 0
   Parts parts;
 };
 CrossPlan plan(int type, int64_t nq, int64_t nk, int batch, int D, int Hk, int group) {
@@ -690,23 +701,23 @@ CrossPlan plan(int type, int64_t nq, int64_t nk, int batch, int D, int Hk, int g
   auto blocks = [&](int qb) { return used * ceil_div(rows, qb) * Hk; };
   const bool bf16 = type == SCN_BF16;
   if (!bf16 && rows <= 8)
-    p = {0, 0, rows <= 1 ? 1 : rows <= 2 ? 2 : rows <= 4 ? 4 : 8, 1, {}};
+    p = {0, 0, rows <= 1 ? 1 : rows <= 2 ? 2 : rows <= 4 ? 4 : 8, 0, {}};
   else if (rows <= 32 && bf16)
-    p = {1, 4, 1, 1, {}};
+    p = {1, 4, 1, 0, {}};
   else if (bf16 && D <= 64)
-    p = blocks(128) < 512 && keys > 128 ? CrossPlan{2, 2, 2, 1, {}} : CrossPlan{4, 1, 2, 1, {}};
+    p = blocks(128) < 512 && keys > 128 ? CrossPlan{2, 2, 2, 0, {}} : CrossPlan{4, 1, 2, 0, {}};
   else if (!bf16 && D <= 64 && rows <= 64 && keys > 64)
-    p = {2, 2, 1, 1, {}};
+    p = {2, 2, 1, 0, {}};
   else if ((bf16 || D <= 64) && (blocks(128) < 512 || (!bf16 && D > 32)) && keys > 64)
-    p = {4, 2, 1, 1, {}};
+    p = {4, 2, 1, 0, {}};
   else
-    p = {4, 1, 1, 1, {}};
+    p = {4, 1, 1, 0, {}};
   // Two blocks a CU, which is what resides; four where there are nearly as many anyway, for
   // samples' lengths differ.
   const int64_t n = p.qw ? blocks(32 * p.qw) : blocks(p.nb);
   p.parts = cut(n, n >= 256 && p.qw > 1 ? 1024 : 512, keys, p.qw ? 512 : 256, used);
   if (p.kw == 1 && keys <= 64 * p.nb)
-    p.repeat = (int)std::max<int64_t>(1, std::min<int64_t>(8, n / REPEAT_BLOCKS));
+    p.repeat = (int)std::max<int64_t>(1, std::min<int64_t>(8, n / FEW_BLOCKS));
   return p;
 }
 
@@ -721,7 +732,7 @@ scn_status launch(CrossArgs<NS> a, const CrossPlan& p, hipStream_t st) {
   static LdsLimit limit;
   auto fn = cross_fwd_kernel<NS, DP, QW, KW, NB, FEW>;
   if (scn_status rc = allow_lds(reinterpret_cast<const void*>(fn), limit, X::SMEM)) return rc;
-  a.deal.rows = X::QB * a.repeat;
+  a.deal.rows = X::QB * std::max(1, a.repeat);
   const int64_t blocks = a.deal.blocks();
   if (blocks > INT32_MAX) return too_many();
   hipLaunchKernelGGL(fn, dim3((unsigned)blocks), dim3(X::NT), X::SMEM, st, a);
@@ -766,15 +777,15 @@ scn_status launch(const CrossArgs<NS>& a, const CrossPlan& p, hipStream_t st) {
     if (p.qw == 1) return launch_thin<DP>(a, p, st);
   if constexpr (NS == 1 && DP <= 64) {
     if (p.qw == 2) return launch<NS, DP, 2, 2, 2>(a, p, st);
-    if (p.repeat > 1) return launch<NS, DP, 4, 1, 2, true>(a, p, st);
+    if (p.repeat) return launch<NS, DP, 4, 1, 2, true>(a, p, st);
     return launch<NS, DP, 4, 1, 2>(a, p, st);
   } else {
     if constexpr (NS == 3 && DP <= 64)
       if (p.qw == 2) return launch<NS, DP, 2, 2, 1>(a, p, st);
     if constexpr (NS == 1 || DP <= 64)
       if (p.kw == 2) return launch<NS, DP, 4, 2, 1>(a, p, st);
-    if (p.repeat > 1) return launch<NS, DP, 4, 1, 1, true>(a, p, st);
-    return launch<NS, DP, 4, 1, 1>(a, p, st);
+    if (p.repeat || (NS == 3 && DP == 64)) return launch<NS, DP, 4, 1, 1, true>(a, p, st);
+    if constexpr (!(NS == 3 && DP == 64)) return launch<NS, DP, 4, 1, 1>(a, p, st);
   }
 }
 
