@@ -6,6 +6,11 @@
 // dQ^T += K^T dS^T.  Keys' pass: S = Q K^T and dP = dO V^T with a key per lane,
 // dV^T += dO^T P and dK^T += Q^T dS over the queries of each head in turn.
 // Split axes leave their sums in a workspace, and a join kernel adds them up in order.
+//
+// Seven products where the mathematics takes five (S and dP twice), for sums without atomics.
+// On long samples the passes wait for data and to issue by turns: one sample of 16,384 rows and
+// states, 2 bf16 heads of 128, 431 TFLOP/s by the flops of
+// five; 120,011 rows of 4 fp32 heads on 2 of 32 over 40 states: 78 and 67 us.
 #include "cross.h"
 
 namespace scn {
@@ -259,143 +264,143 @@ __global__ void __launch_bounds__(64 * QW * KW, (NS == 3 && DP > 32) || DP > 64 
     auto dot8 = [&](const float (&x)[8], const float (&y)[8]) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) delta = fmaf(x[j], y[j], delta);
-  };
-  if constexpr (PRE) {
+    };
+    if constexpr (PRE) {
 #pragma unroll
-    for (int s = 0; s < DP / 16; ++s) {
-      Q[s] = nq.frag(s);
-      G[s] = ng.frag(s);
-      float x[8], y[8];
-      ng.floats(s, x);
-      no.floats(s, y);
-      dot8(x, y);
-    }
-    lse = nl;
-    ahead(first + QB);
-  } else {
-    const auto* const q = a.q.p + row * a.q.row + h * a.q.head;
-    const auto* const g = a.d_o.p + row * a.d_o.row + h * a.d_o.head;
-    const auto* const o = a.o.p + row * a.o.row + h * a.o.head;
-#pragma unroll
-    for (int s = 0; s < DP / 16; ++s) {
-      Q[s] = load_frag<NS>(q, s, a.D, lane);
-      G[s] = load_frag<NS>(g, s, a.D, lane);
-      const int c = 16 * s + 8 * half;
-      if (c < a.D) {
+      for (int s = 0; s < DP / 16; ++s) {
+        Q[s] = nq.frag(s);
+        G[s] = ng.frag(s);
         float x[8], y[8];
-        load8<NS>(g + c, x);
-        load8<NS>(o + c, y);
+        ng.floats(s, x);
+        no.floats(s, y);
         dot8(x, y);
       }
-    }
-    lse = a.lse[a.at(row, h)];
-  }
-  delta = both_sum(delta);
-  const int64_t at = a.at(row, h);
-  lse2 = lse * LOG2E;
-  const bool far = !(fabsf(lse) <= LSE_MOST);  // the row is formed again ...
-  const bool none = lse != lse;                 // ... if it has weights at all
+      lse = nl;
+      ahead(first + QB);
+    } else {
+      const auto* const q = a.q.p + row * a.q.row + h * a.q.head;
+      const auto* const g = a.d_o.p + row * a.d_o.row + h * a.d_o.head;
+      const auto* const o = a.o.p + row * a.o.row + h * a.o.head;
 #pragma unroll
-  for (int d = 0; d < DP / 32; ++d) dQ[d] = zero16();
-  if constexpr (EXACT)
-#pragma unroll
-    for (int d = 0; d < DP / 32; ++d) PK[d] = zero16();
-  // the keys, as in cross_fwd.hip
-  if (stage && t0 < t1) {
-    fetch(t0);
-    put(t0);
-    if (t0 + 1 < t1) fetch(t0 + 1);
-    __syncthreads();
-  }
-  for (int t = t0; t < t1; ++t) {
-    if (stage) {
-      if (t + 1 < t1) put(t + 1);
-      if (t + 2 < t1) fetch(t + 2);
+      for (int s = 0; s < DP / 16; ++s) {
+        Q[s] = load_frag<NS>(q, s, a.D, lane);
+        G[s] = load_frag<NS>(g, s, a.D, lane);
+        const int c = 16 * s + 8 * half;
+        if (c < a.D) {
+          float x[8], y[8];
+          load8<NS>(g + c, x);
+          load8<NS>(o + c, y);
+          dot8(x, y);
+        }
+      }
+      lse = a.lse[a.at(row, h)];
     }
-    take(t);
-    if (stage) __syncthreads();
-  }
-  // the groups' sums, joined in order
-  over = both_sum(over);
-  if constexpr (KW > 1) {
-    float* const x = reinterpret_cast<float*>(smem) + lane;
+    delta = both_sum(delta);
+    const int64_t at = a.at(row, h);
+    lse2 = lse * LOG2E;
+    const bool far = !(fabsf(lse) <= LSE_MOST);  // the row is formed again ...
+    const bool none = lse != lse;                 // ... if it has weights at all
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d) dQ[d] = zero16();
+    if constexpr (EXACT)
+#pragma unroll
+      for (int d = 0; d < DP / 32; ++d) PK[d] = zero16();
+    // the keys, as in cross_fwd.hip
+    if (stage && t0 < t1) {
+      fetch(t0);
+      put(t0);
+      if (t0 + 1 < t1) fetch(t0 + 1);
+      __syncthreads();
+    }
+    for (int t = t0; t < t1; ++t) {
+      if (stage) {
+        if (t + 1 < t1) put(t + 1);
+        if (t + 2 < t1) fetch(t + 2);
+      }
+      take(t);
+      if (stage) __syncthreads();
+    }
+    // the groups' sums, joined in order
+    over = both_sum(over);
+    if constexpr (KW > 1) {
+      float* const x = reinterpret_cast<float*>(smem) + lane;
+      if constexpr (EXACT) {
+        x[wave * 64] = over;
+        __syncthreads();
+        over = 0.f;
+        for (int g = 0; g < KW; ++g) over += x[(g * QW + wave - kw * QW) * 64];
+        __syncthreads();
+      }
+      float* const o = x + (wave - QW) * X::SUMS * 64;
+      if (kw > 0) {
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            o[(d * 16 + e) * 64] = dQ[d][e];
+            if constexpr (EXACT) o[((DP / 32 + d) * 16 + e) * 64] = PK[d][e];
+          }
+      }
+      __syncthreads();
+      if (kw > 0) return;
+      for (int g = 0; g < KW - 1; ++g) {
+        const float* const o = x + (g * QW + wave) * X::SUMS * 64;
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            dQ[d][e] += o[(d * 16 + e) * 64];
+            if constexpr (EXACT) PK[d][e] += o[((DP / 32 + d) * 16 + e) * 64];
+          }
+      }
+    }
+    if (w.parts > 1) {
+      if (mine) {
+        const int64_t to = at * a.qdeal.parts.most + w.part;
+        float* const o = a.qpart + to * 2 * a.D;
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d) {
+          store_cols<3>(o, dQ[d], 1.f, d, a.D, lane);
+          if constexpr (EXACT) store_cols<3>(o + a.D, PK[d], 1.f, d, a.D, lane);
+        }
+        if (half == 0) {
+          over_part(a)[to] = over;
+          if (w.part == 0) {
+            a.delta[at] = delta;
+            a.lse2[at] = far ? NAN : lse2;
+          }
+        }
+      }
+      return;
+    }
     if constexpr (EXACT) {
-      x[wave * 64] = over;
-      __syncthreads();
-      over = 0.f;
-      for (int g = 0; g < KW; ++g) over += x[(g * QW + wave - kw * QW) * 64];
-      __syncthreads();
-    }
-    float* const o = x + (wave - QW) * X::SUMS * 64;
-    if (kw > 0) {
+      over = fabsf(over) < INFINITY ? over : 0.f;
+      delta += over;
 #pragma unroll
       for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          o[(d * 16 + e) * 64] = dQ[d][e];
-          if constexpr (EXACT) o[((DP / 32 + d) * 16 + e) * 64] = PK[d][e];
-        }
+        for (int e = 0; e < 16; ++e) dQ[d][e] = fmaf(-over, PK[d][e], dQ[d][e]);
     }
-    __syncthreads();
-    if (kw > 0) return;
-    for (int g = 0; g < KW - 1; ++g) {
-      const float* const o = x + (g * QW + wave) * X::SUMS * 64;
+    bool fine = true;
 #pragma unroll
-      for (int d = 0; d < DP / 32; ++d)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          dQ[d][e] += o[(d * 16 + e) * 64];
-          if constexpr (EXACT) PK[d][e] += o[((DP / 32 + d) * 16 + e) * 64];
-        }
-    }
-  }
-  if (w.parts > 1) {
+    for (int d = 0; d < DP / 32; ++d) fine &= finite16(dQ[d]);
+    if constexpr (NS == 3) fine &= !tiny(dQ, 1.f);
     if (mine) {
-      const int64_t to = at * a.qdeal.parts.most + w.part;
-      float* const o = a.qpart + to * 2 * a.D;
-#pragma unroll
-      for (int d = 0; d < DP / 32; ++d) {
-        store_cols<3>(o, dQ[d], 1.f, d, a.D, lane);
-        if constexpr (EXACT) store_cols<3>(o + a.D, PK[d], 1.f, d, a.D, lane);
-      }
       if (half == 0) {
-        over_part(a)[to] = over;
-        if (w.part == 0) {
-          a.delta[at] = delta;
-          a.lse2[at] = far ? NAN : lse2;
-        }
+        a.delta[at] = delta;
+        a.lse2[at] = far ? NAN : lse2;  // keys that see the row are formed again
       }
+      auto* const o = a.dq.p + row * a.dq.row + h * a.dq.head;
+#pragma unroll
+      for (int d = 0; d < DP / 32; ++d) store_cols<NS>(o, dQ[d], a.scale, d, a.D, lane);
     }
-    return;
-  }
-  if constexpr (EXACT) {
-    over = fabsf(over) < INFINITY ? over : 0.f;
-    delta += over;
-#pragma unroll
-    for (int d = 0; d < DP / 32; ++d)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) dQ[d][e] = fmaf(-over, PK[d][e], dQ[d][e]);
-  }
-  bool fine = true;
-#pragma unroll
-  for (int d = 0; d < DP / 32; ++d) fine &= finite16(dQ[d]);
-  if constexpr (NS == 3) fine &= !tiny(dQ, 1.f);
-  if (mine) {
-    if (half == 0) {
-      a.delta[at] = delta;
-      a.lse2[at] = far ? NAN : lse2;  // keys that see the row are formed again
+    const uint64_t bad = __ballot(mine && !none && (far || !fine) && mk > 0);
+    uint32_t rows = (uint32_t)bad | (uint32_t)(bad >> 32);
+    const int w0 = first + wave * 32;
+    for (; rows; rows &= rows - 1) {
+      const int x = w0 + __builtin_ctz(rows);
+      dq_row<NS>(a, w.base + x / a.group, hk * a.group + x % a.group, k0, mk);
     }
-    auto* const o = a.dq.p + row * a.dq.row + h * a.dq.head;
-#pragma unroll
-    for (int d = 0; d < DP / 32; ++d) store_cols<NS>(o, dQ[d], a.scale, d, a.D, lane);
-  }
-  const uint64_t bad = __ballot(mine && !none && (far || !fine) && mk > 0);
-  uint32_t rows = (uint32_t)bad | (uint32_t)(bad >> 32);
-  const int w0 = first + wave * 32;
-  for (; rows; rows &= rows - 1) {
-    const int x = w0 + __builtin_ctz(rows);
-    dq_row<NS>(a, w.base + x / a.group, hk * a.group + x % a.group, k0, mk);
-  }
   };
   if constexpr (!FEW) {
     sweep(w.first, true);
@@ -766,7 +771,8 @@ __global__ void __launch_bounds__(256) cross_dkv_join_kernel(CrossBwdArgs<NS> a,
     if (bad[i]) dkv_row<NS>(a, w.base + w.first + i, w.hk, w.other, w.mo);
 }
 
-// Shapes and parts of both passes, by rules on sizes alone (cross_fwd.hip)
+// Shapes and parts of both passes, by rules on sizes alone (cross_fwd.hip).  Few keys stay in LDS
+// for several tiles of queries (the case of 40 states above: 85 us, 133 loading them for each).
 struct CrossBwdPlan {
   int qw, qkw, repeat;  // queries' pass: waves of queries, groups of keys; tiles of a work
                         // where the keys are few, or 0

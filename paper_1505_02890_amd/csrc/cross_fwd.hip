@@ -5,6 +5,10 @@
 // sum of the softmax, S^T = K Q^T and O^T += V^T P^T, 32 tile rows a wave (cross.h).  Where
 // there are few queries the keys are split over blocks, whose outputs, maxima and sums a
 // second kernel joins in order.
+//
+// Long samples are bound by the matrix cores and the vector unit in turn (one sample of 16,384
+// rows and states, 2 bf16 heads of 128: 834 TFLOP/s), few rows by memory: 128 streams of 2,000
+// states, 34 us and 7 for the join; one row over 262,144 states, 4 heads of 32 bf16, 37 us.
 #include <cmath>
 
 #include "cross.h"
@@ -689,6 +693,9 @@ __global__ void __launch_bounds__(256) cross_join_kernel(CrossArgs<NS> a, Parts 
 
 // The kernel's shape, the parts of the keys and the tiles of queries that a block takes, by rules
 // on sizes alone (the lengths lie on the device): tile rows and keys of a mean sample, blocks.
+// Few bf16 rows: waves that take tiles alone, 34 us for 128 streams of 2,000 states, 36 in the
+// general kernel.  Few keys that stay in LDS for several tiles of queries: 120,011 rows of 4 fp32
+// heads on 2 of 32 over 40 states each, 56 us, 85 loading them for each.
 struct CrossPlan {
   int qw, kw, nb;  // qw 0: cross_few_kernel of nb tile rows
   int repeat;      // tiles of a work where the keys are few, or 0
