@@ -214,6 +214,10 @@ __global__ void __launch_bounds__(Group<LP>::THREADS) block_fwd_kernel(BlockArgs
         x[j] = fmaf(s, u[j] * wf[j], x[j]);
       }
     }
+    // (y may lie over x, and a row's last lane reads channels that the lane before it writes too:
+    // where that is another wave's, and no norm of f has had all waves past their loads, they wait)
+    if constexpr (LP > 64)
+      if (!a.f.p) __syncthreads();
     if (a.y.p && ch.on) put8<RS>(a.y.p + t * a.y.row + ch.c, ch.n, x);
     if (!a.h.p) continue;
     float u[8];
