@@ -649,8 +649,9 @@ size_t scn_grad_clip_workspace_bytes(int64_t count, int64_t elements);
 /*
  * The norm of all gradients of a model taken together, and their clipping by it:
  *   norm = sqrt(sum over all tensors of t^2),   out = norm > most ? t most / norm : t
- * The sum is in 64 bits, always in the same order.  A norm that is not finite leaves all
- * gradients as they are (the caller sees it in `norm`).  Nothing waits for the device.
+ * The sum is in 64 bits, always in the same order.  A norm that is not finite, or past fp32's
+ * largest number, leaves all gradients as they are (the caller sees it in `norm`).  Nothing
+ * waits for the device.
  *  grads      host array of `count` tensors (the addresses are read during the call alone).
  *  out        host array of `count` device pointers for the results, of the gradients' types;
  *             NULL: in place.  An entry may be its gradient's own place.

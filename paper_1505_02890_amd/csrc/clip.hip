@@ -113,12 +113,13 @@ __device__ inline void add_squares(const Table& t, int i, int64_t first, int n, 
   }
 }
 
-// what the norm `all` makes of the tensors (a norm that is not finite leaves all as it is)
+// what the norm `all` makes of the tensors (a norm that the caller sees as not finite leaves all
+// as it is)
 struct Scale {
   bool clip;
   double by;
   __device__ inline Scale(double all, double most)
-      : clip(all > most && all < (double)INFINITY), by(clip ? most / all : 1.) {}
+      : clip(all > most && (float)all < INFINITY), by(clip ? most / all : 1.) {}
 };
 template <int THREADS, int SIZE>
 __device__ inline void scale_to(const Table& t, int i, int64_t first, int n, int tid, Scale z) {
