@@ -124,10 +124,11 @@ struct Scale {
 template <int THREADS, int SIZE>
 __device__ inline void scale_to(const Table& t, int i, int64_t first, int n, int tid, Scale z) {
   if (!z.clip && t.in[i] == t.out[i]) return;
+  // (products in 64 bits: the scale itself may leave fp32's range)
+  auto by = [&](float v) { return (float)(v * z.by); };
   if (t.n[i] & IS_BF16) {
     const uint16_t* const p = static_cast<const uint16_t*>(t.in[i]) + first;
     uint16_t* const o = static_cast<uint16_t*>(t.out[i]) + first;
-    const float by = (float)z.by;
     constexpr int N = SIZE / THREADS / 8;
     v4u x[N];
 #pragma unroll
@@ -137,7 +138,7 @@ __device__ inline void scale_to(const Table& t, int i, int64_t first, int n, int
     }
     if (tid < (n & 7)) {
       const int e = (n & ~7) + tid;
-      o[e] = z.clip ? Elem<1>::put(Elem<1>::get(p[e]) * by) : p[e];
+      o[e] = z.clip ? Elem<1>::put(by(Elem<1>::get(p[e]))) : p[e];
     }
 #pragma unroll
     for (int u = 0; u < N; ++u) {
@@ -146,8 +147,8 @@ __device__ inline void scale_to(const Table& t, int i, int64_t first, int n, int
       if (z.clip)
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          x[u][j] = cvt2_bf16(__uint_as_float(x[u][j] << 16) * by,
-                              __uint_as_float(x[u][j] & 0xffff0000u) * by);
+          x[u][j] = cvt2_bf16(by(__uint_as_float(x[u][j] << 16)),
+                              by(__uint_as_float(x[u][j] & 0xffff0000u)));
       *reinterpret_cast<v4u_any*>(o + e) = x[u];
     }
   } else {
@@ -162,15 +163,14 @@ __device__ inline void scale_to(const Table& t, int i, int64_t first, int n, int
     }
     if (tid < (n & 3)) {
       const int e = (n & ~3) + tid;
-      o[e] = (float)(p[e] * z.by);
+      o[e] = by(p[e]);
     }
-    // (products in 64 bits round once)
 #pragma unroll
     for (int u = 0; u < N; ++u) {
       const int e = (u * THREADS + tid) * 4;
       if (e + 4 > n) continue;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) x[u][j] = (float)(x[u][j] * z.by);
+      for (int j = 0; j < 4; ++j) x[u][j] = by(x[u][j]);
       *reinterpret_cast<v4f_any*>(o + e) = x[u];
     }
   }

@@ -1,5 +1,5 @@
-"""Clipping at the ends of fp32's range: norms on both sides of its largest number.  In one
-launch and in two kernels."""
+"""Clipping at the ends of fp32's range: norms on both sides of its largest number, scales
+below its smallest.  In one launch and in two kernels."""
 from __future__ import annotations
 
 import math
@@ -10,7 +10,7 @@ import pytest
 torch = pytest.importorskip("torch")
 
 from test_gpu_attention import f64  # noqa: E402
-from test_gpu_clip import B, F, check  # noqa: E402
+from test_gpu_clip import B, F, check, make  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 
@@ -56,3 +56,16 @@ def test_two_numbers_near_the_largest(scn):
         keep = t.clone()
         assert math.isinf(float(scn.clip_grads([t], 1.0)))
         assert torch.equal(t, keep)
+
+
+@pytest.mark.parametrize("kinds", [[F], [B], [F, B]], ids=["f32", "bf16", "both"])
+@pytest.mark.parametrize("sizes", [FEW, MANY], ids=["few", "many"])
+@pytest.mark.parametrize("most", [1e-3, 1e-6, 1e-8])
+def test_scales_below_the_smallest_number(scn, sizes, kinds, most):
+    # a norm of 1e37: the scale has few bits or none in fp32, the results are ordinary numbers
+    grads = make(sizes, kinds, 3, std=1e37 / math.sqrt(sum(sizes)))
+    exact = [f64(t) for t in grads]
+    out = [torch.zeros_like(t) for t in grads]
+    check(scn.clip_grads(grads, most, out=out), out, exact, most)
+    assert all(float(t.abs().max()) > 0 for t in out)
+    check(scn.clip_grads(grads, most), grads, exact, most)
