@@ -12,7 +12,7 @@ import ctypes
 import functools
 import os
 from array import array
-from typing import Optional, Sequence
+from typing import Iterable, Optional, Sequence
 
 import numpy as np
 import torch
@@ -881,8 +881,8 @@ def _refuse_grad(t, dev: int, name: str):
         raise ValueError(f"{name} must be contiguous")
 
 
-def clip_grads(grads: Sequence[torch.Tensor], max_norm: float,
-               out: Optional[Sequence[torch.Tensor]] = None,
+def clip_grads(grads: Iterable[torch.Tensor], max_norm: float,
+               out: Optional[Iterable[torch.Tensor]] = None,
                ws: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Clips gradients by the norm of all of them together (``scn_grad_clip``), in
     place or into ``out``: where the norm is finite and above ``max_norm`` (infinity:
@@ -890,6 +890,10 @@ def clip_grads(grads: Sequence[torch.Tensor], max_norm: float,
     bfloat16 in any mix.  Returns the norm before, a float32 scalar on the device;
     nothing waits for it."""
     dev = torch.cuda.current_device()
+    if not isinstance(grads, (list, tuple)):  # (a generator can be gone through once)
+        grads = list(grads)
+    if out is not None and not isinstance(out, (list, tuple)):
+        out = list(out)
     try:  # whole lists at a time: many tensors are looked over with each call
         sizes = [t.numel() for t in grads]
         rows = [x for r in zip([t.data_ptr() for t in grads], sizes,
