@@ -610,7 +610,8 @@ typedef struct scn_rows {
  *  z          NULL: no gate.
  *  wf, wh     device float[C], or NULL for ones.
  *  y, h       written; NULL: not wanted (f or h must be given).  y may be x; h may be f or z.
- * Sums are in fp32, and in 64 bits for rows whose squares leave fp32's range.
+ * Sums are in fp32; rows whose squares leave fp32's range are scaled by a power of two and summed
+ * again.
  * Errors: SCN_ERR_INVALID, SCN_ERR_UNSUPPORTED (C, types), SCN_ERR_OVERFLOW (n above 2^30),
  * SCN_ERR_HIP.
  */
