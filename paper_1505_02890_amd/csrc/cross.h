@@ -81,7 +81,9 @@ struct Deal {
         const int stride = (len + 63) >> 6, b = sample + lane * stride;
         const bool below = lane * stride < len &&
                            tiles.at(b) * (int64_t)tiles.many / rows + b <= tile;
-        const int step = max(__popcll(__ballot(below)) - 1, 0) * stride;
+        // (a signed count: a tile of rows in front of all samples has none below it)
+        const int c = __popcll(__ballot(below));
+        const int step = max(c - 1, 0) * stride;
         sample += step;
         len = min(stride, len - step);
       }
