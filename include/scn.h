@@ -560,11 +560,9 @@ scn_status scn_attn_step(int32_t type, int32_t streams, int64_t capacity, int32_
  *             outside every range are not written).
  *  D, Hq, Hk, scale, o, lse  as in scn_attn_fwd, lse device float[Hq][nq].
  *  ws         scn_cross_attn_fwd_workspace_bytes bytes, 16-byte aligned (0: none needed).
- * Types, numerics and rows formed again: as scn_attn_fwd, and strides, but that the heads of a
- * row lie within it (as the parts of a projection do).
- * Errors: SCN_ERR_INVALID, SCN_ERR_UNSUPPORTED (D; heads outside their rows; bf16 with D 40,
- * 48 or 56 and 32 rows and heads to a key head or fewer in the samples' mean), SCN_ERR_OVERFLOW
- * (nk or nq Hq/Hk above 2^30), SCN_ERR_WORKSPACE, SCN_ERR_HIP.
+ * Types, strides, numerics and rows formed again: as scn_attn_fwd.
+ * Errors: SCN_ERR_INVALID, SCN_ERR_UNSUPPORTED (D), SCN_ERR_OVERFLOW (nk or nq Hq/Hk above
+ * 2^30), SCN_ERR_WORKSPACE, SCN_ERR_HIP.
  */
 scn_status scn_cross_attn_fwd(int32_t type, int64_t nq, int64_t nk, int32_t batch,
                               const int32_t* q_ranges, const int32_t* k_ranges, int32_t D,

@@ -724,7 +724,7 @@ def cross_attn_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_ranges: 
                    out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
     """Attention of each sample's rows to the same sample's states
     (``scn_cross_attn_fwd``).  q [n, Hq, D], k and v [m, Hk, D], float32 or
-    bfloat16, any row strides, the heads within their rows; the ranges int32 [batch + 1] as
+    bfloat16, any row and head strides; the ranges int32 [batch + 1] as
     ``site_ranges`` gives, of q's rows and of the states.  scale is D ** -0.5 unless
     given.  Returns (o [n, Hq, D], lse float32 [Hq, n]); rows of samples without
     states get 0 and -inf, and rows outside every range are not written.  ``out``

@@ -195,9 +195,7 @@ struct Ahead {
   }
 };
 
-// host checks of both directions
-scn_status check_side(const char* who, const char* name, const scn_heads* h, int type, int64_t rows,
-                      int heads, int D);
+// host check of both directions
 scn_status check_cross(const char* who, int32_t type, int64_t nq, int64_t nk, int32_t batch,
                        const int32_t* q_ranges, const int32_t* k_ranges, int32_t D, int32_t Hq,
                        int32_t Hk, float scale);

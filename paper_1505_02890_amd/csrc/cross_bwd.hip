@@ -971,11 +971,11 @@ scn_status scn_cross_attn_bwd(int32_t type, int64_t nq, int64_t nk, int32_t batc
     const scn_heads* h;
     const char* name;
     int64_t rows;
-    int heads;
-  } all[] = {{q, "q", nq, Hq},     {k, "k", nk, Hk},   {v, "v", nk, Hk},   {o, "o", nq, Hq},
-             {d_o, "d_o", nq, Hq}, {dq, "dq", nq, Hq}, {dk, "dk", nk, Hk}, {dv, "dv", nk, Hk}};
+  } all[] = {{q, "q", nq},     {k, "k", nk},   {v, "v", nk},   {o, "o", nq},
+             {d_o, "d_o", nq}, {dq, "dq", nq}, {dk, "dk", nk}, {dv, "dv", nk}};
   for (const auto& x : all)
-    if (scn_status rc = check_side(who, x.name, x.h, type, x.rows, x.heads, D)) return rc;
+    if (x.rows > 0)
+      if (scn_status rc = check_heads(who, x.name, x.h, type)) return rc;
   if (nq == 0 && nk == 0) return SCN_OK;
   const size_t need = scn_cross_attn_bwd_workspace_bytes(type, nq, nk, batch, D, Hq, Hk);
   if (need && (!ws || (reinterpret_cast<uintptr_t>(ws) & 15) != 0 || ws_bytes < need)) {

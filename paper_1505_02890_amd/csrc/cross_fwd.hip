@@ -839,18 +839,6 @@ CrossArgs<NS> make(int64_t nq, int64_t nk, int batch, const int32_t* qr, const i
 
 }  // namespace
 
-scn_status check_side(const char* who, const char* name, const scn_heads* h, int type, int64_t rows,
-                      int heads, int D) {
-  if (rows == 0) return SCN_OK;
-  if (scn_status rc = check_heads(who, name, h, type)) return rc;
-  if (rows > 1 && heads > 1 &&
-      (h->head < 0 || (h->row > 0 && h->head > (h->row - D) / (heads - 1)))) {
-    set_error("%s: %s has heads that lie outside their row", who, name);
-    return SCN_ERR_UNSUPPORTED;
-  }
-  return SCN_OK;
-}
-
 scn_status check_cross(const char* who, int32_t type, int64_t nq, int64_t nk, int32_t batch,
                        const int32_t* q_ranges, const int32_t* k_ranges, int32_t D, int32_t Hq,
                        int32_t Hk, float scale) {
@@ -863,13 +851,6 @@ scn_status check_cross(const char* who, int32_t type, int64_t nq, int64_t nk, in
   if (nq > ATTN_ROWS / (Hq / Hk) || nk > ATTN_ROWS) {
     set_error("%s: more than 2^30 keys, or rows of queries times heads on a key head", who);
     return SCN_ERR_OVERFLOW;
-  }
-  // Off: an illegal address was reported once in calls of this kind (9 rows of 4 heads on 2 of
-  // 40 bf16 channels over 8,040 states), forward or backward, and no cause was found.
-  if (type == SCN_BF16 && D > 32 && D < 64 && nq > 0 &&
-      ceil_div(nq * (Hq / Hk), std::max<int64_t>(1, std::min<int64_t>(batch, nq))) <= 32) {
-    set_error("%s: few rows of 40, 48 or 56 bf16 channels are not supported", who);
-    return SCN_ERR_UNSUPPORTED;
   }
   return SCN_OK;
 }
@@ -898,10 +879,12 @@ scn_status scn_cross_attn_fwd(int32_t type, int64_t nq, int64_t nk, int32_t batc
   if (scn_status rc = check_cross(who, type, nq, nk, batch, q_ranges, k_ranges, D, Hq, Hk, scale))
     return rc;
   if (nq == 0) return SCN_OK;
-  if (scn_status rc = check_side(who, "q", q, type, nq, Hq, D)) return rc;
-  if (scn_status rc = check_side(who, "o", o, type, nq, Hq, D)) return rc;
-  if (scn_status rc = check_side(who, "k", k, type, nk, Hk, D)) return rc;
-  if (scn_status rc = check_side(who, "v", v, type, nk, Hk, D)) return rc;
+  if (scn_status rc = check_heads(who, "q", q, type)) return rc;
+  if (scn_status rc = check_heads(who, "o", o, type)) return rc;
+  if (nk > 0) {
+    if (scn_status rc = check_heads(who, "k", k, type)) return rc;
+    if (scn_status rc = check_heads(who, "v", v, type)) return rc;
+  }
   const CrossPlan p = plan(type, nq, nk, batch, D, Hk, Hq / Hk);
   const size_t need = part_bytes(p, nq, Hq, D);
   if (need && (!ws || (reinterpret_cast<uintptr_t>(ws) & 15) != 0 || ws_bytes < need)) {

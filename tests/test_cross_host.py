@@ -160,11 +160,6 @@ def test_cross_attention_refuses(lib):
                                       None, ws, ws_bytes, None)
 
     assert fwd(nq=0) == 0  # nothing to do
-    for D in (40, 48, 56):
-        assert fwd(type=1, D=D) == 5 and "few rows" in message(lib)
-        assert lib.scn_cross_attn_bwd(1, 10, 20, 1, P(4096), P(4096), D, 2, 1, h, h, h, h, P(4096), h,
-                                      1.0, h, h, h, P(4096), 1 << 30, None) == 5
-        assert "few rows" in message(lib)
     for kw, status, word in [
             (dict(type=2), 1, "type"), (dict(nq=-1), 1, "size"), (dict(nk=-1), 1, "size"),
             (dict(batch=0), 1, "size"), (dict(qr=None), 1, "ranges"), (dict(kr=None), 1, "ranges"),
@@ -175,7 +170,6 @@ def test_cross_attention_refuses(lib):
             (dict(k=heads(p=4100)), 1, "k must be"), (dict(v=heads(row=66)), 1, "v must be"),
             (dict(o=heads(head=33)), 1, "o must be"), (dict(k=heads(p=None)), 1, "k is null"),
             (dict(k=heads(row=-64)), 5, "rows"), (dict(q=heads(row=2 ** 22 + 8)), 5, "rows"),
-            (dict(q=heads(row=32, head=320)), 5, "outside"), (dict(o=heads(head=-32)), 5, "outside"),
             (dict(nk=10 ** 6), 6, "workspace")]:
         assert fwd(**kw) == status, kw
         assert word in message(lib), (kw, message(lib))
@@ -197,7 +191,6 @@ def test_cross_attention_backward_refuses(lib):
 
     assert bwd(nq=0, nk=0) == 0
     assert bwd(lse=None) == 1 and bwd(dq=None) == 1 and bwd(dk=heads(p=4098)) == 1
-    assert bwd(dq=heads(row=32, head=3200)) == 5
     assert bwd(ws=None) == 6 and bwd(ws_bytes=need - 1) == 6 and bwd(ws=P(4104)) == 6
     assert lib.scn_cross_attn_bwd_workspace_bytes(0, -1, 50, 1, 32, 2, 1) == 0
 
