@@ -76,8 +76,10 @@ class CrossBlock:
 
     def _queries(self, sites, h):
         qz = self._conv(sites, h, "Wqz")
-        q = qz[:, :self.wide].to(self.dtype).view(h.shape[0], self.heads, self.dim)
-        return q, qz[:, self.wide:]
+        q = qz[:, :self.wide].to(self.dtype)
+        if qz.shape[1] % 4:  # (the attention's rows lie whole 16 bytes apart)
+            q = q.contiguous()
+        return q.view(h.shape[0], self.heads, self.dim), qz[:, self.wide:]
 
     def _keys(self, sites, m):
         kv = self._conv(sites, m, "Wkv").to(self.dtype)
