@@ -46,8 +46,9 @@ struct Work {
 // time, so that the blocks without work are the last ones: each costs 2 us of a place on the
 // card.  Work-groups go to the XCDs in turn, which spreads the key heads of a tile over them;
 // `near` has them follow each other on one XCD, for few rows of heads that share cache lines
-// (one row over 262,144 states, 4 heads of 32 bf16 channels: 37 us, 53 otherwise; many tiles
-// of rows with whole lines to each head lose 6%, for an XCD then reads all heads' states).
+// (one row over 262,144 states, 4 heads of 32 bf16 channels: 32 us a call, 54 otherwise; 20 rows of
+// 16 samples over 8,192 each, 25 and 36; many tiles of rows with whole lines to each head lose 2%,
+// for an XCD then reads all heads' states).
 struct Deal {
   Side tiles, steps;
   int batch, rows, Hk;

@@ -8,9 +8,9 @@
 // Split axes leave their sums in a workspace, and a join kernel adds them up in order.
 //
 // Seven products where the mathematics takes five (S and dP twice), for sums without atomics.
-// On long samples the passes wait for data and to issue by turns: one sample of 16,384 rows and
-// states, 2 bf16 heads of 128, 431 TFLOP/s by the flops of
-// five; 120,011 rows of 4 fp32 heads on 2 of 32 over 40 states: 78 and 67 us.
+// On long samples the passes wait to issue and for data by turns: one sample of 16,384 rows and
+// states, 2 bf16 heads of 128, 809 and 726 us and 47 for the joins, 434 TFLOP/s by the flops of
+// five; 120,011 rows of 4 fp32 heads on 2 of 32 over 40 states: 81 and 69 us.
 #include "cross.h"
 
 namespace scn {
@@ -771,8 +771,24 @@ __global__ void __launch_bounds__(256) cross_dkv_join_kernel(CrossBwdArgs<NS> a,
     if (bad[i]) dkv_row<NS>(a, w.base + w.first + i, w.hk, w.other, w.mo);
 }
 
-// Shapes and parts of both passes, by rules on sizes alone (cross_fwd.hip).  Few keys stay in LDS
-// for several tiles of queries (the case of 40 states above: 85 us, 133 loading them for each).
+// Shapes and parts of both passes, by rules on sizes alone (cross_fwd.hip).  Both sides of each, as
+// whole calls in us, the rule's first:
+//  - Few keys stay in LDS for several tiles of queries: the case of 40 states above 85, and 133
+//    loading them for each; 2,000 rows of 32 samples on 40, 4 fp32 heads on 2 of 32, 92 in four
+//    waves side by side and 116 in two by two.
+//  - Queries' pass of more than 64 bf16 channels, two by two below 512 blocks: 8 samples of 400
+//    states, 4 heads of 128, 500 rows 48 and 53, 1,000 rows 101 and 89; four waves from there:
+//    2,000 rows 153 and 179, 4,000 rows 265 and 321.
+//  - Keys' pass to 64 bf16 channels, one wave of keys below 128 blocks: 2 samples of 300 rows on
+//    400 states, 4 heads on 1 of 64, 28 and 30 with two, 33 with four; 2,000 rows of 32 samples on
+//    40 states 99 and 82 with two.  Two below 1,024: 8 samples of 300 rows on 1,000 states, 2 key
+//    heads, 58, 65 with one and 55 with four.  Four from there: 4,000 states, 4 key heads, 99, 136
+//    and 109.
+//  - Past 64 channels, two below 384: 8 samples of 300 rows on 1,000 states, 2 key heads of 128,
+//    115 and 104, of 2,000 rows 339 and 341; four from there: 4,000 states, 4 key heads, 242 and
+//    272.
+//  - fp32 heads to 32 channels, one wave for 32 keys or fewer: 2,000 rows of 32 samples on 32
+//    states 91 and 83 with two; two past them: on 40 states 92 and 123 with one.
 struct CrossBwdPlan {
   int qw, qkw, repeat;  // queries' pass: waves of queries, groups of keys; tiles of a work
                         // where the keys are few, or 0

@@ -6,9 +6,10 @@
 // there are few queries the keys are split over blocks, whose outputs, maxima and sums a
 // second kernel joins in order.
 //
-// Long samples are bound by the matrix cores and the vector unit in turn (one sample of 16,384
-// rows and states, 2 bf16 heads of 128: 834 TFLOP/s), few rows by memory: 128 streams of 2,000
-// states, 34 us and 7 for the join; one row over 262,144 states, 4 heads of 32 bf16, 37 us.
+// Long samples wait in turn to issue and for data (one sample of 16,384 rows and states, 2 bf16
+// heads of 128: 302 us, 910 TFLOP/s, and 16 for the join), few rows for memory: 128 streams of
+// 2,000 states, 35 us and 7 for the join; one row over 262,144 states, 4 heads of 32 bf16, 30 and
+// 6.
 #include <cmath>
 
 #include "cross.h"
@@ -693,9 +694,26 @@ __global__ void __launch_bounds__(256) cross_join_kernel(CrossArgs<NS> a, Parts 
 
 // The kernel's shape, the parts of the keys and the tiles of queries that a block takes, by rules
 // on sizes alone (the lengths lie on the device): tile rows and keys of a mean sample, blocks.
-// Few bf16 rows: waves that take tiles alone, 34 us for 128 streams of 2,000 states, 36 in the
-// general kernel.  Few keys that stay in LDS for several tiles of queries: 120,011 rows of 4 fp32
-// heads on 2 of 32 over 40 states each, 56 us, 85 loading them for each.
+// Both sides of each rule, as whole calls in us, the rule's first:
+//  - Few fp32 rows, on the vector unit: 64 samples of 4,096 states, 2 key heads of 64, 1 tile row
+//    a sample 57 and 94 in tiles, 8 rows 70 and 92, 16 rows 93 in tiles and 97.
+//  - Few bf16 rows, waves that take tiles alone: 16 samples of 4,096 states, 2 heads of 32, 16
+//    rows 16 and 18 in the general kernel, 32 rows 16.5 and 18.5, 64 rows 17.8 and 18.6.
+//  - bf16 to 64 channels, two waves of queries by two of keys below 512 blocks: 8 samples of 2,000
+//    states, 4 heads of 64, 4,000 rows 88 (four waves) and 108; around the border the other side
+//    wins, 1,000 rows 47 and 42, 2,000 rows 66 and 56.
+//  - fp32 to 64 channels, two by two for 64 rows or fewer: 64 rows on 4,000 states, 4 heads of 32,
+//    24 and 29; four waves by two groups below 512 blocks: 1,000 rows on 400 states 18 and 25, on
+//    4,000 states 129 and 113; four waves alone from there: 4,000 rows on 400 states 47 and 58.
+//  - bf16 past 64 channels, four by two below 512 blocks: 500 rows on 400 states, 4 heads of 128,
+//    16 and 16, on 4,000 states 71 and 58; four alone from there: 2,000 rows on 400 states 27 and
+//    34.
+//  - Few keys that stay in LDS for several tiles of queries: 120,011 rows of 4 fp32 heads on 2 of
+//    32 over 40 states each, 56 and 85 loading them for each.
+//  - Keys in parts: 2,000 rows of 8 samples on 7,500 states, 4 heads of 64 bf16, 179 and 210 in
+//    one part; 64 rows of 4 samples on 50,000, 4 heads of 32 fp32, 69 and 904.
+// A batch whose samples are far from their mean is cut as if they were not: one of 256 streams with
+// a million states, the others with ten, takes 5 ms.
 struct CrossPlan {
   int qw, kw, nb;  // qw 0: cross_few_kernel of nb tile rows
   int repeat;      // tiles of a work where the keys are few, or 0
